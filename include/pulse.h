@@ -26,6 +26,9 @@
  *   bad index never turns into an out-of-bounds access.
  * Element types.  K, V and queries are fp16 or bf16 (pulse_dtype); they are
  *   passed as raw 16-bit element buffers.  Scores, outputs and LSE are fp32.
+ *   The blocks of the host store and the slot pool may be held in 4 bits
+ *   instead (PULSE_F16_KV4, PULSE_BF16_KV4): queries, digests and rows stay in
+ *   the named 16-bit type.
  * Indices.  Block and slot indices are int32; block offsets are int64.
  * Inputs must be finite.
  *
@@ -37,9 +40,29 @@
  *   K(h, t, c) at element ((0 * Hkv + h) * bs + t) * d + c      token-major
  *   V(h, t, c) at element Hkv*bs*d + (h * d + c) * bs + t       channel-major
  * so a block is U = 2 * Hkv * bs * d * 2 bytes (64 KiB at Hkv 8, bs 16).
- * Tokens past the end of a context inside its last block must be zero.
+ * Tokens past the end of a context inside its last block must be zero
+ * (4-bit blocks: may hold anything).
  * Requests are ragged: request r owns n_r = ceil(ctx_len[r] / bs) blocks,
  * its global blocks are blk_off[r] .. blk_off[r+1]-1 (blk_off[0] = 0).
+ *
+ * 4-bit KV block (PULSE_F16_KV4, PULSE_BF16_KV4).  The 128 channels of a
+ * token's key or value in one head are four groups of 32; a group is 32 e2m1
+ * codes c (sign bit, then the magnitudes 0, .5, 1, 1.5, 2, 3, 4, 6) and one
+ * byte e + 127; it stands for c * 2^e.  A block is Hkv regions of 136 * bs
+ * bytes, head after head (17 KiB at Hkv 8, bs 16):
+ *   keys          [bs][64] bytes: channels 2i (low half) and 2i + 1 of a token
+ *   values        [bs/8][16][8] 32-bit words: word [o][c % 16][c / 16] is
+ *                 channel c of tokens 8o .. 8o+7, token 8o in its lowest 4 bits
+ *   key scales    [bs][4] bytes        value scales  [4][bs] bytes
+ * Exponents lie in -23 .. 13 (fp16) or -100 .. 125 (bf16), so that every value
+ * is one of the 16-bit type; the scale byte 255 makes a group NaN.  Pools and
+ * stores of 4-bit blocks are 16-byte aligned.  The entry points that take
+ * these types: pulse_block_bytes, pulse_workspace_bytes, the selections,
+ * pulse_recall_gather, pulse_release_recalled, pulse_sparse_decode_attn,
+ * pulse_attention_workgroups, pulse_decode_layer(_noalloc), the offload layers
+ * of pulse_irq_step (without an engine), pulse_build_tables,
+ * pulse_qk_norm_rope, pulse_append_kv and pulse_load_kv.  The others return
+ * what they return for a dtype that they do not know.
  */
 #ifndef PULSE_H
 #define PULSE_H
@@ -68,14 +91,19 @@ typedef enum {
     PULSE_ERR_TIMEOUT = 8          /* host-side wait expired (gather-scatter engine) */
 } pulse_status;
 
-typedef enum { PULSE_F16 = 0, PULSE_BF16 = 1 } pulse_dtype;
+typedef enum {
+    PULSE_F16 = 0,
+    PULSE_BF16 = 1,
+    PULSE_F16_KV4 = 2, /* fp16 queries and rows, KV blocks in 4 bits */
+    PULSE_BF16_KV4 = 3 /* bf16 queries and rows, KV blocks in 4 bits */
+} pulse_dtype;
 
 typedef struct {
     int32_t num_q_heads;  /* Hq */
     int32_t num_kv_heads; /* Hkv */
     int32_t head_dim;     /* d, must be 128 */
     int32_t block_size;   /* bs, tokens per KV block: 16, 32 or 64 */
-    int32_t dtype;        /* pulse_dtype of K, V and q */
+    int32_t dtype;        /* pulse_dtype of q and of the KV blocks */
 } pulse_shape;
 
 /* Device-resident statistics written by the recall (device memory). */
@@ -463,6 +491,101 @@ PULSE_API pulse_status pulse_decode_layer(const pulse_layer_args* args, pulse_st
  */
 #define PULSE_NOALLOC_SCRATCH_BYTES ((size_t)32 << 20)
 PULSE_API pulse_status pulse_decode_layer_noalloc(const pulse_layer_args* args, pulse_stream_t stream);
+
+/* ---- The step around the attention: maps, positions, cache rows ---- */
+
+/*
+ * Block offsets, block tables and slot maps of a step, from request lengths
+ * (the table and free list of pulse_recall_gather).  Request r holds ctx_len[r]
+ * tokens, the last new_len[r] of them new in this step; n_r = ceil(ctx_len[r] /
+ * bs).  The blocks that hold new tokens and have no slot take the free list
+ * front to back in (request, block) order; blocks that have one keep it.
+ *   blk_off[r]   sum of n_i over i < r, r = 0 .. B          device int64 [B+1]
+ *   tok_off[r]   sum of new_len[i] over i < r               device int32 [B+1]
+ *   for the i-th new token of request r, at g = tok_off[r] + i:
+ *   positions[g] p = ctx_len[r] - new_len[r] + i       device int32 [max_tokens]
+ *   slot_map[g]  block_table[r][p / bs] * bs + p % bs  device int64 [max_tokens]
+ *                (the row's place in the pool, for pulse_append_kv); both -1
+ *                for g >= tok_off[B], so that a captured step may be padded
+ *   block_table  device int32 [B][max_blocks], -1 = not resident; updated
+ *   free_slots   device int32 [n_free];  free_head device int32, updated
+ *   ws           pulse_tables_workspace_bytes() bytes of device memory
+ * PULSE_ERR_POOL_EXHAUSTED if the free list has too few slots;
+ * PULSE_ERR_BAD_INDEX if ctx_len[r] is negative, new_len[r] is not in
+ * 0 .. ctx_len[r], n_r > max_blocks or the new tokens exceed max_tokens; if a
+ * table entry of a block with new tokens is below -1 or not below n_slots;
+ * if the first of those blocks holds earlier tokens and has no slot; if
+ * *free_head lies outside [0, n_free] or a slot to be taken outside
+ * [0, n_slots).  All of it is checked before anything is written: on an error
+ * the table and free_head stay as they are, both offset arrays are zero and
+ * both maps -1, so that what follows finds no block and no row.
+ * The rows of the table must not overlap what else is written.  B <= 4096 and
+ * max_tokens < 2^31 (else PULSE_ERR_UNSUPPORTED).  B = 0 clears the maps.
+ */
+PULSE_API size_t pulse_tables_workspace_bytes(const pulse_shape* shape, int32_t B, int64_t max_tokens);
+PULSE_API pulse_status pulse_build_tables(const pulse_shape* shape, const int32_t* ctx_len, const int32_t* new_len,
+                                          int32_t B, int32_t* block_table, int32_t max_blocks,
+                                          const int32_t* free_slots, int32_t* free_head, int32_t n_free,
+                                          int32_t n_slots, int64_t* blk_off, int32_t* tok_off, int64_t* slot_map,
+                                          int32_t* positions, int64_t max_tokens, int32_t* dev_status, void* ws,
+                                          size_t ws_bytes, pulse_stream_t stream);
+
+/*
+ * RMS norm of every query and key head and the position rotation, in one pass
+ * over n_rows rows (Hq heads of queries, Hkv of keys, 128 channels each):
+ *   y = x / sqrt(mean(x^2) + eps) * weight    (a NULL weight: y = x)
+ *   pair i < rot_dim / 2 of channels (a, b), t = positions[row] * inv_freq[i]:
+ *   (y_a, y_b) -> (y_a cos t - y_b sin t, y_a sin t + y_b cos t)
+ * with (a, b) = (i, i + rot_dim / 2), or (2i, 2i + 1) if interleaved is 1 (0
+ * otherwise); channels from rot_dim on are not rotated.  Statistics and
+ * rotation in fp32, angles in 64 bits, one rounding to the 16-bit type.
+ *   q, k         device rows of 16-bit elements; row r begins at r * q_stride
+ *                (k_stride) elements, its heads follow one another, so both may
+ *                be parts of one projection's output
+ *   positions    device int32 [n_rows]; rows of a negative position are
+ *                skipped and their output is left as it was
+ *   q_weight, k_weight   device, 128 elements of the 16-bit type, or NULL
+ *   inv_freq     device double [rot_dim / 2] (may be NULL if rot_dim is 0)
+ *   rot_dim      0, 16, 32, .. 128 (another multiple: PULSE_ERR_UNSUPPORTED)
+ *   q_out, k_out device rows as q and k; may be q and k themselves with the
+ *                same strides, else must overlap no input
+ * q, k, their outputs and the weights are 16-byte aligned, strides multiples
+ * of 8 that hold the heads, eps finite and not negative (else
+ * PULSE_ERR_INVALID_ARG).
+ */
+PULSE_API pulse_status pulse_qk_norm_rope(const pulse_shape* shape, const void* q, int64_t q_stride, const void* k,
+                                          int64_t k_stride, int32_t n_rows, const int32_t* positions,
+                                          const void* q_weight, const void* k_weight, float eps,
+                                          const double* inv_freq, int32_t rot_dim, int32_t interleaved, void* q_out,
+                                          int64_t q_out_stride, void* k_out, int64_t k_out_stride,
+                                          pulse_stream_t stream);
+
+/*
+ * Rows of keys and values into the KV blocks of a slot pool, and back.
+ * Row i (Hkv heads of 128 elements of the 16-bit type, at i * k_stride and
+ * i * v_stride elements) belongs to token slot_map[i] % bs of slot
+ * slot_map[i] / bs; -1: to none (append skips it, load leaves the output row as
+ * it was).  No place may be given twice in one call of pulse_append_kv (that
+ * token's contents, and no other's, would be undefined).
+ * A 16-bit pool holds the elements themselves.  A 4-bit pool holds of each
+ * group of 32 channels the exponent e, the least with max|x| <= 7 * 2^e (kept
+ * within the range given above), and the nearest code to x / 2^e (the even
+ * one of two, the largest beyond 6); a group with an infinity or a NaN becomes
+ * NaN as a whole.  pulse_load_kv returns c * 2^e, which the 16-bit type holds.
+ *   k, v         device, 16-byte aligned, strides multiples of 8 that hold the
+ *                heads (else PULSE_ERR_INVALID_ARG)
+ *   slot_map     device int64 [n_rows] (as pulse_build_tables writes it)
+ *   slot_pool    device [n_slots][block], 16-byte aligned; only the tokens that
+ *                the map names are written
+ * An entry of the map outside [-1, n_slots * bs) is reported as
+ * PULSE_ERR_BAD_INDEX and its row skipped.
+ */
+PULSE_API pulse_status pulse_append_kv(const pulse_shape* shape, const void* k, int64_t k_stride, const void* v,
+                                       int64_t v_stride, const int64_t* slot_map, int32_t n_rows, void* slot_pool,
+                                       int32_t n_slots, int32_t* dev_status, pulse_stream_t stream);
+PULSE_API pulse_status pulse_load_kv(const pulse_shape* shape, const void* slot_pool, int32_t n_slots,
+                                     const int64_t* slot_map, int32_t n_rows, void* k, int64_t k_stride, void* v,
+                                     int64_t v_stride, int32_t* dev_status, pulse_stream_t stream);
 
 /* ---- Interruptible layer-wise scheduling (IRQ, Sec. 4.2) ---- */
 

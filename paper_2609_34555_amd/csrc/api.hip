@@ -5,20 +5,21 @@
 
 #include <mutex>
 
-#include "pulse_internal.h"
+#include "kv4.h"
 
 namespace pulse {
 
-bool shape_supported(const pulse_shape* s) {
+bool kv_shape_supported(const pulse_shape* s) {
     if (!s) return false;
     if (s->head_dim != kHeadDim) return false;
     if (s->block_size != 16 && s->block_size != 32 && s->block_size != 64) return false;
     if (s->num_kv_heads < 1 || s->num_q_heads < s->num_kv_heads) return false;
     if (s->num_q_heads % s->num_kv_heads) return false;
     if (s->num_q_heads / s->num_kv_heads > kMaxGroup) return false;
-    if (s->dtype != PULSE_F16 && s->dtype != PULSE_BF16) return false;
-    return true;
+    return s->dtype == PULSE_F16 || s->dtype == PULSE_BF16 || is_kv4(s->dtype);
 }
+
+bool shape_supported(const pulse_shape* s) { return kv_shape_supported(s) && !is_kv4(s->dtype); }
 
 static size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -69,17 +70,18 @@ const char* pulse_status_string(pulse_status s) {
 }
 
 size_t pulse_block_bytes(const pulse_shape* shape) {
-    if (!shape_supported(shape)) return 0;
+    if (!kv_shape_supported(shape)) return 0;
+    if (is_kv4(shape->dtype)) return (size_t)shape->num_kv_heads * kv4_head_bytes(shape->block_size);
     return (size_t)2 * shape->num_kv_heads * shape->block_size * shape->head_dim * 2;
 }
 
 size_t pulse_workspace_bytes(const pulse_shape* shape, int32_t B, int32_t k_max, int64_t total_blocks) {
-    if (!shape_supported(shape) || B < 0 || k_max < 0 || total_blocks < 0) return 0;
+    if (!kv_shape_supported(shape) || B < 0 || k_max < 0 || total_blocks < 0) return 0;
     return ws_layout(*shape, B, k_max, total_blocks).total;
 }
 
 int32_t pulse_attention_workgroups(const pulse_shape* shape, int32_t B, int32_t k_max) {
-    if (!shape_supported(shape) || B < 1 || k_max < 1) return 0;
+    if (!kv_shape_supported(shape) || B < 1 || k_max < 1) return 0;
     const AttnPlan p = attn_plan(B, shape->num_kv_heads, k_max, shape->block_size);
     const int W = attn_waves(shape->num_q_heads / shape->num_kv_heads);
     return (p.n_split + W - 1) / W;
@@ -103,7 +105,7 @@ static pulse_status check_select_args(const pulse_shape* shape, const void* q, c
                                       const int32_t* k_mid, int32_t n_sink, int32_t n_local, int32_t k_max,
                                       int32_t* sel_idx, int32_t* sel_cnt, int32_t* dev_status) {
     PULSE_REQUIRE(shape, PULSE_ERR_INVALID_ARG);
-    PULSE_REQUIRE(shape_supported(shape), PULSE_ERR_UNSUPPORTED);
+    PULSE_REQUIRE(kv_shape_supported(shape), PULSE_ERR_UNSUPPORTED);
     PULSE_REQUIRE(B >= 0 && total_blocks >= 0 && k_max >= 1, PULSE_ERR_INVALID_ARG);
     PULSE_REQUIRE(n_sink >= 0 && n_local >= 0, PULSE_ERR_INVALID_ARG);
     PULSE_REQUIRE(solo >= 0 && solo < shape->num_kv_heads, PULSE_ERR_INVALID_ARG);
@@ -135,7 +137,7 @@ pulse_status pulse_select_solohead(const pulse_shape* shape, const void* q, cons
 }
 
 size_t pulse_headwise_workspace_bytes(const pulse_shape* shape, int32_t B, int32_t k_max, int64_t total_blocks) {
-    if (!shape_supported(shape) || B < 0 || k_max < 0 || total_blocks < 0) return 0;
+    if (!kv_shape_supported(shape) || B < 0 || k_max < 0 || total_blocks < 0) return 0;
     const size_t H = (size_t)shape->num_kv_heads;
     size_t o = 0;
     o = align_up(o + sizeof(float) * H * (size_t)total_blocks);    // scores [Hkv][total_blocks]
@@ -173,7 +175,7 @@ pulse_status pulse_select_headwise(const pulse_shape* shape, const void* q, cons
 }
 
 size_t pulse_average_workspace_bytes(const pulse_shape* shape, int32_t B, int32_t k_max, int64_t total_blocks) {
-    if (!shape_supported(shape) || B < 0 || k_max < 0 || total_blocks < 0) return 0;
+    if (!kv_shape_supported(shape) || B < 0 || k_max < 0 || total_blocks < 0) return 0;
     const size_t H = (size_t)shape->num_kv_heads;
     return align_up(sizeof(float) * H * (size_t)total_blocks) + align_up(sizeof(float) * (size_t)total_blocks);
 }
@@ -257,7 +259,7 @@ static pulse_status check_recall_args(const pulse_shape* shape, const void* host
                                       int32_t* free_head, int32_t n_free, void* slot_pool, int32_t n_slots,
                                       pulse_recall_stats* stats, int32_t* dev_status) {
     PULSE_REQUIRE(shape, PULSE_ERR_INVALID_ARG);
-    PULSE_REQUIRE(shape_supported(shape), PULSE_ERR_UNSUPPORTED);
+    PULSE_REQUIRE(kv_shape_supported(shape), PULSE_ERR_UNSUPPORTED);
     PULSE_REQUIRE(B >= 0 && k_max >= 1 && max_blocks >= 1 && n_free >= 0 && n_slots >= 1,
                   PULSE_ERR_INVALID_ARG);
     PULSE_REQUIRE(B <= kMaxBatch, PULSE_ERR_UNSUPPORTED);
@@ -299,7 +301,7 @@ pulse_status pulse_release_recalled(const pulse_shape* shape, int32_t B, int32_t
                                     pulse_recall_stats* stats, int32_t* dev_status, void* ws, size_t ws_bytes,
                                     pulse_stream_t stream) {
     PULSE_REQUIRE(shape, PULSE_ERR_INVALID_ARG);
-    PULSE_REQUIRE(shape_supported(shape), PULSE_ERR_UNSUPPORTED);
+    PULSE_REQUIRE(kv_shape_supported(shape), PULSE_ERR_UNSUPPORTED);
     PULSE_REQUIRE(B >= 0 && k_max >= 1 && max_blocks >= 1 && total_blocks >= 0, PULSE_ERR_INVALID_ARG);
     PULSE_REQUIRE(B <= kMaxBatch, PULSE_ERR_UNSUPPORTED);
     if (B == 0) return PULSE_OK;
@@ -316,7 +318,7 @@ pulse_status pulse_sparse_decode_attn(const pulse_shape* shape, const void* q, c
                                       float sm_scale, float* out, float* lse, int32_t* dev_status, void* ws,
                                       size_t ws_bytes, pulse_stream_t stream) {
     PULSE_REQUIRE(shape, PULSE_ERR_INVALID_ARG);
-    PULSE_REQUIRE(shape_supported(shape), PULSE_ERR_UNSUPPORTED);
+    PULSE_REQUIRE(kv_shape_supported(shape), PULSE_ERR_UNSUPPORTED);
     PULSE_REQUIRE(B >= 0 && k_max >= 1 && max_blocks >= 1 && n_slots >= 1, PULSE_ERR_INVALID_ARG);
     if (B == 0) return PULSE_OK;
     PULSE_REQUIRE(q && slot_pool && block_table && sel_idx && sel_cnt && ctx_len && out && dev_status,
@@ -439,7 +441,7 @@ pulse_status pulse_decode_layer_noalloc(const pulse_layer_args* args, pulse_stre
     PULSE_REQUIRE(!args->ws && args->ws_bytes == 0, PULSE_ERR_INVALID_ARG);
     pulse_layer_args a = *args;
     // other argument errors are reported by pulse_decode_layer's own checks
-    if (shape_supported(&a.shape) && a.B > 0 && a.B <= kMaxBatch && a.k_max >= 1 && a.total_blocks >= 0) {
+    if (kv_shape_supported(&a.shape) && a.B > 0 && a.B <= kMaxBatch && a.k_max >= 1 && a.total_blocks >= 0) {
         const size_t need = ws_layout(a.shape, a.B, a.k_max, a.total_blocks).total;
         PULSE_REQUIRE(need <= (size_t)PULSE_NOALLOC_SCRATCH_BYTES, PULSE_ERR_WORKSPACE);
         void* ws = scratch_for_current_device();
@@ -448,6 +450,91 @@ pulse_status pulse_decode_layer_noalloc(const pulse_layer_args* args, pulse_stre
         a.ws_bytes = need;
     }
     return pulse_decode_layer(&a, stream);
+}
+
+size_t pulse_tables_workspace_bytes(const pulse_shape* shape, int32_t B, int64_t max_tokens) {
+    if (!kv_shape_supported(shape) || B < 0 || max_tokens < 0 || max_tokens > INT32_MAX) return 0;
+    return tables_ws_bytes(B, shape->block_size, max_tokens);
+}
+
+pulse_status pulse_build_tables(const pulse_shape* shape, const int32_t* ctx_len, const int32_t* new_len, int32_t B,
+                                int32_t* block_table, int32_t max_blocks, const int32_t* free_slots,
+                                int32_t* free_head, int32_t n_free, int32_t n_slots, int64_t* blk_off,
+                                int32_t* tok_off, int64_t* slot_map, int32_t* positions, int64_t max_tokens,
+                                int32_t* dev_status, void* ws, size_t ws_bytes, pulse_stream_t stream) {
+    PULSE_REQUIRE(shape, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(kv_shape_supported(shape), PULSE_ERR_UNSUPPORTED);
+    PULSE_REQUIRE(B >= 0 && max_blocks >= 1 && n_free >= 0 && n_slots >= 1 && max_tokens >= 0, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(B <= kMaxBatch && max_tokens <= INT32_MAX, PULSE_ERR_UNSUPPORTED);
+    PULSE_REQUIRE((ctx_len && new_len && block_table) || B == 0, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(free_head && blk_off && tok_off && dev_status, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(free_slots || n_free == 0, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE((slot_map && positions) || max_tokens == 0, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(ws && ws_bytes >= tables_ws_bytes(B, shape->block_size, max_tokens), PULSE_ERR_WORKSPACE);
+    return hip_status(launch_tables(ctx_len, new_len, B, shape->block_size, block_table, max_blocks, free_slots,
+                                    free_head, n_free, n_slots, blk_off, tok_off, slot_map, positions, max_tokens,
+                                    dev_status, ws, (hipStream_t)stream));
+}
+
+// Rows of heads: whole 16-byte pieces, as long as the heads at least.
+static bool rows_ok(const void* p, int64_t stride, int32_t heads) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0 && stride >= (int64_t)heads * kHeadDim;
+}
+
+pulse_status pulse_qk_norm_rope(const pulse_shape* shape, const void* q, int64_t q_stride, const void* k,
+                                int64_t k_stride, int32_t n_rows, const int32_t* positions, const void* q_weight,
+                                const void* k_weight, float eps, const double* inv_freq, int32_t rot_dim,
+                                int32_t interleaved, void* q_out, int64_t q_out_stride, void* k_out,
+                                int64_t k_out_stride, pulse_stream_t stream) {
+    PULSE_REQUIRE(shape, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(kv_shape_supported(shape), PULSE_ERR_UNSUPPORTED);
+    PULSE_REQUIRE(n_rows >= 0 && rot_dim >= 0 && rot_dim <= kHeadDim, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(rot_dim % 16 == 0, PULSE_ERR_UNSUPPORTED);
+    PULSE_REQUIRE(interleaved == 0 || interleaved == 1, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(eps >= 0.f && eps < INFINITY, PULSE_ERR_INVALID_ARG);
+    if (n_rows == 0) return PULSE_OK;
+    PULSE_REQUIRE(q && k && positions && q_out && k_out && (inv_freq || rot_dim == 0), PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(rows_ok(q, q_stride, shape->num_q_heads) && rows_ok(q_out, q_out_stride, shape->num_q_heads) &&
+                      rows_ok(k, k_stride, shape->num_kv_heads) && rows_ok(k_out, k_out_stride, shape->num_kv_heads),
+                  PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(rows_ok(q_weight, kHeadDim, 1) && rows_ok(k_weight, kHeadDim, 1), PULSE_ERR_INVALID_ARG);
+    return hip_status(launch_qk_norm_rope(*shape, q, q_stride, k, k_stride, n_rows, positions, q_weight, k_weight, eps,
+                                          inv_freq, rot_dim, interleaved != 0, q_out, q_out_stride, k_out,
+                                          k_out_stride, (hipStream_t)stream));
+}
+
+static pulse_status check_cache_args(const pulse_shape* shape, const void* k, int64_t k_stride, const void* v,
+                                     int64_t v_stride, const int64_t* slot_map, int32_t n_rows, const void* pool,
+                                     int32_t n_slots, const int32_t* dev_status) {
+    PULSE_REQUIRE(shape, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(kv_shape_supported(shape), PULSE_ERR_UNSUPPORTED);
+    PULSE_REQUIRE(n_rows >= 0 && n_slots >= 1, PULSE_ERR_INVALID_ARG);
+    if (n_rows == 0) return PULSE_OK;
+    PULSE_REQUIRE(k && v && slot_map && pool && dev_status, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(rows_ok(k, k_stride, shape->num_kv_heads) && rows_ok(v, v_stride, shape->num_kv_heads),
+                  PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(reinterpret_cast<uintptr_t>(pool) % 16 == 0, PULSE_ERR_INVALID_ARG);
+    return PULSE_OK;
+}
+
+pulse_status pulse_append_kv(const pulse_shape* shape, const void* k, int64_t k_stride, const void* v,
+                             int64_t v_stride, const int64_t* slot_map, int32_t n_rows, void* slot_pool,
+                             int32_t n_slots, int32_t* dev_status, pulse_stream_t stream) {
+    const pulse_status st = check_cache_args(shape, k, k_stride, v, v_stride, slot_map, n_rows, slot_pool, n_slots,
+                                             dev_status);
+    if (st != PULSE_OK || n_rows == 0) return st;
+    return hip_status(launch_append_kv(*shape, k, k_stride, v, v_stride, slot_map, n_rows, slot_pool, n_slots,
+                                       dev_status, (hipStream_t)stream));
+}
+
+pulse_status pulse_load_kv(const pulse_shape* shape, const void* slot_pool, int32_t n_slots, const int64_t* slot_map,
+                           int32_t n_rows, void* k, int64_t k_stride, void* v, int64_t v_stride, int32_t* dev_status,
+                           pulse_stream_t stream) {
+    const pulse_status st = check_cache_args(shape, k, k_stride, v, v_stride, slot_map, n_rows, slot_pool, n_slots,
+                                             dev_status);
+    if (st != PULSE_OK || n_rows == 0) return st;
+    return hip_status(launch_load_kv(*shape, slot_pool, n_slots, slot_map, n_rows, k, k_stride, v, v_stride,
+                                     dev_status, (hipStream_t)stream));
 }
 
 pulse_status pulse_probe_hbm_read(const void* src, size_t bytes, void* sink, void* start_event, void* stop_event,

@@ -29,7 +29,7 @@
 // write-back on gfx950 measured at about 9 ns per workgroup, plus a merge on
 // the kernel's tail and counters that start at zero in the workspace: it would
 // save well under the combine launch's 3.6 us.)
-#include "pulse_internal.h"
+#include "kv4.h"
 
 namespace pulse {
 
@@ -300,10 +300,163 @@ __device__ inline void attend_split(const uint16_t* __restrict__ q, const uint16
     l_run = across_groups(l_run, [](float a, float b) { return a + b; });
 }
 
+// attend_split over the 4-bit cache (kv4.h).  A lane's 16 bytes of a key row are 32 channels under one scale,
+// decoded with it into the operands of four products; Q is loaded in the same channel order.  A value's scale
+// differs from token to token, which is the index the P.V product sums over, so it multiplies the probability
+// instead: P'[q][g][t] = P[q][t] * scale[t][g] for channel group g, and V is decoded without a scale.  The 16 rows
+// of the P operand hold GP = 4, 8 or 16 query heads for 4, 2 or 1 groups at once (row = g' * GP + q: the query
+// columns of S^T repeat), so P' costs a multiplication per row and token however many heads there are; the
+// product of channel tile t uses the rows of its group t / 2, the other rows of its result are left unused.
+// Codes are exact in bf16 and scales are powers of two, so P' is split into two bf16 parts for either 16-bit type
+// (fp16 would not hold the range of the scales).
+// Row 4 * grp + v of acc[t] is query head (4 * grp + v) % GP of group (4 * grp + v) / GP of the tile's set.
+template <int DT, int BS, int GP>
+__device__ inline void attend_split_kv4(const uint16_t* __restrict__ q, const uint8_t* __restrict__ pool,
+                                        int32_t n_slots, const int32_t* __restrict__ table, int32_t max_blocks,
+                                        int32_t j_lane, const int32_t* __restrict__ ctx_len, int32_t Hq, int32_t Hkv,
+                                        int32_t G, int r, int h, int ne, float scale_log2, int32_t* status, int lane,
+                                        float& m_run, float& l_run, f32x4 (&acc)[8]) {
+    constexpr int ET = elem_type(DT);
+    constexpr int kSets = GP / 4;  // P operands: rows hold 16 / GP groups each
+    using MQ = Mfma<ET>;
+    using MP = Mfma<PULSE_BF16>;
+    using vec = typename MQ::vec;
+    const int col = lane & 15;
+    const int grp = lane >> 4;
+    const int qc = col % GP;  // query head of this column
+#pragma unroll
+    for (int t = 0; t < 8; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m_run = -INFINITY;
+    l_run = 0.f;
+    if (ne <= 0) return;
+    const int32_t j = lane < ne ? j_lane : -1;
+    const int32_t sl = (j >= 0 && j < max_blocks) ? table[(size_t)r * max_blocks + j] : -1;
+    const int ctx = ctx_len[r];
+    const int64_t n_r = ((int64_t)ctx + BS - 1) / BS;
+    int my_slot = -1, my_nv = 0;
+    if (lane < ne) {
+        if (j < n_r && sl >= 0 && sl < n_slots) {
+            my_slot = sl;
+            const int64_t v = (int64_t)ctx - (int64_t)j * BS;
+            my_nv = v >= BS ? BS : (int)v;
+        }
+        if (my_slot < 0) report(status, PULSE_ERR_BAD_INDEX);
+    }
+    // Q^T operand: channels 32 * grp + 8 * kc .. + 7 of the column's query head
+    vec qb[4];
+    {
+        const uint16_t* qr = q + ((size_t)r * Hq + (size_t)h * G + qc) * kHeadDim + grp * kGroup;
+#pragma unroll
+        for (int kc = 0; kc < 4; ++kc) qb[kc] = qc < G ? load_vec<ET>(qr + 8 * kc) : zero_vec<ET>();
+    }
+    const size_t E = (size_t)Hkv * kv4_head_bytes(BS);
+    const uint8_t* head = pool + (size_t)h * kv4_head_bytes(BS);
+    const int tokens = ne * BS;
+
+#pragma unroll 1
+    for (int t0 = 0; t0 < tokens; t0 += kChunkTokens) {
+        // K: MFMA row m = col is token 8 * (col / 4) + 4 * sub + col % 4
+        u32x4 ka[2];
+        float ks[2];
+        {
+            const int seq = t0 + 8 * (col >> 2);
+            const int e = seq / BS;
+            const int slot = __shfl(my_slot, e < ne ? e : 0);
+            const bool ok = e < ne && slot >= 0;
+            const uint8_t* b = head + (size_t)(ok ? slot : 0) * E;
+#pragma unroll
+            for (int sub = 0; sub < 2; ++sub) {
+                const int row = seq % BS + 4 * sub + (col & 3);
+                ka[sub] = ok ? *reinterpret_cast<const u32x4*>(b + row * 64 + grp * 16) : u32x4{0, 0, 0, 0};
+                ks[sub] = ok ? kv4_scale(b[kv4_key_scales(BS) + row * kGroups + grp]) : 0.f;
+            }
+        }
+        // V: lane group grp holds tokens 8 * grp .. + 7, channels col + 16 * t in word t
+        const int pv_seq = t0 + 8 * grp;
+        const int pv_e = pv_seq / BS;
+        const int pv_slot = __shfl(my_slot, pv_e < ne ? pv_e : 0);
+        const int pv_nv = __shfl(my_nv, pv_e < ne ? pv_e : 0);
+        const int pv_row = pv_seq % BS;
+        const bool pv_ok = pv_e < ne && pv_slot >= 0;
+        const uint8_t* vb = head + (size_t)(pv_ok ? pv_slot : 0) * E;
+        u32x4 vw[2];
+        u32x2 vs[kSets];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            vw[i] = pv_ok ? reinterpret_cast<const u32x4*>(vb + kv4_values(BS) + pv_row * 64 + col * 32)[i]
+                          : u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < kSets; ++k) {
+            const int g = k * (16 / GP) + col / GP;
+            vs[k] = pv_ok ? *reinterpret_cast<const u32x2*>(vb + kv4_value_scales(BS) + g * BS + pv_row) : u32x2{0, 0};
+        }
+        // --- S^T = K . Q^T
+        f32x4 s[2];
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) {
+            s[sub] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kc = 0; kc < 4; ++kc) s[sub] = MQ::mac(kv4_decode8<ET>(ka[sub][kc], ks[sub]), qb[kc], s[sub]);
+        }
+        float x[8];
+        float cm = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[i] = s[i / 4][i % 4] * scale_log2;
+            if (!pv_ok || pv_row + i >= pv_nv) x[i] = -INFINITY;
+            cm = fmaxf(cm, x[i]);
+        }
+        cm = across_groups(cm, [](float a, float b) { return fmaxf(a, b); });
+        const float m_new = fmaxf(m_run, cm);
+        const float m_use = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = exp2_fast(m_run - m_use);
+        float psum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[i] = exp2_fast(x[i] - m_use);
+            psum += x[i];
+        }
+        l_run = l_run * alpha + psum;
+        m_run = m_new;
+        if (t0 > 0 && __ballot(alpha != 1.f)) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const float av = __shfl(alpha, 4 * grp + v);
+#pragma unroll
+                for (int t = 0; t < 8; ++t) acc[t][v] *= av;
+            }
+        }
+        // --- O += P' . V
+#pragma unroll
+        for (int k = 0; k < kSets; ++k) {
+            bf16x8 ph, pl;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                // what lies behind the last token is not read into a product, whatever its scale byte is
+                const float sc = pv_row + i < pv_nv ? kv4_scale(vs[k][i / 4] >> (8 * (i % 4)) & 0xFFu) : 0.f;
+                __bf16 hi, lo;
+                MP::split(x[i] * sc, hi, lo);
+                ph[i] = hi;
+                pl[i] = lo;
+            }
+#pragma unroll
+            for (int t = 8 / kSets * k; t < 8 / kSets * (k + 1); ++t) {
+                const bf16x8 v = kv4_decode8<PULSE_BF16>(vw[t / 4][t % 4], 1.0f);
+                acc[t] = MP::mac(ph, v, acc[t]);
+                acc[t] = MP::mac(pl, v, acc[t]);
+            }
+        }
+    }
+    l_run = across_groups(l_run, [](float a, float b) { return a + b; });
+    // a split whose every logit is NaN (keys of a NaN scale) keeps its weight in the merge
+    if (m_run == -INFINITY && l_run != l_run) m_run = 0.f;
+}
+
 // grid = (Hkv, n_wg, B), or (Hkv, B, n_wg) with light_last; in either, workgroup p is piece p / Hkv of KV head
 // p % Hkv of a plan; wave w of a request's workgroup wg owns split W * wg + w of eps entries.  Dynamic LDS:
 // O [W][G][128] floats then (m, l) [W][G] float2.
-template <int DT, int BS, int W>
+// GP: rows of the P operand that a channel group of the 4-bit cache takes.
+template <int DT, int BS, int W, int GP>
 __global__ __launch_bounds__(W * kWave) void attn_splitk_kernel(
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ pool, int32_t n_slots,
     const int32_t* __restrict__ table, int32_t max_blocks, const int32_t* __restrict__ sel_idx,
@@ -368,17 +521,22 @@ __global__ __launch_bounds__(W * kWave) void attn_splitk_kernel(
     const int ne = min(p.eps, p.cnt - (p.wg * W + wave) * p.eps);
     float m_run, l_run;
     f32x4 acc[8];
-    attend_split<DT, BS>(q, pool, n_slots, table, max_blocks, j_lane, ctx_len, Hq, Hkv, G, r, h, ne, scale_log2,
-                         status, lane, m_run, l_run, acc);
+    if constexpr (is_kv4(DT))
+        attend_split_kv4<DT, BS, GP>(q, reinterpret_cast<const uint8_t*>(pool), n_slots, table, max_blocks, j_lane,
+                                     ctx_len, Hq, Hkv, G, r, h, ne, scale_log2, status, lane, m_run, l_run, acc);
+    else
+        attend_split<DT, BS>(q, pool, n_slots, table, max_blocks, j_lane, ctx_len, Hq, Hkv, G, r, h, ne, scale_log2,
+                             status, lane, m_run, l_run, acc);
     // wave partials to LDS
     if (grp == 0 && col < G) s_ml[wave * G + col] = make_float2(m_run, l_run);
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-        const int g = 4 * grp + v;
+        const int g = (4 * grp + v) % GP;
         if (g < G) {
             float* o = s_o + (wave * G + g) * kHeadDim + col;
 #pragma unroll
-            for (int t = 0; t < 8; ++t) o[16 * t] = acc[t][v];
+            for (int t = 0; t < 8; ++t)
+                if (GP == 16 || t / 2 % (16 / GP) == (4 * grp + v) / GP) o[16 * t] = acc[t][v];
         }
     }
     __syncthreads();
@@ -512,13 +670,13 @@ AttnPlan attn_plan(int32_t B, int32_t Hkv, int32_t k_max, int32_t bs) {
 }
 
 // `done` (optional): the kernel's stop event, carried by the launch.
-template <int DT, int BS, int W>
+template <int DT, int BS, int W, int GP = kMaxGroup>
 static void launch_attn_t(dim3 grid, size_t lds, hipStream_t st, hipEvent_t done, const void* q, const void* pool,
                           int32_t n_slots, const int32_t* table, int32_t max_blocks, const int32_t* sel_idx,
                           const int32_t* sel_cnt, int32_t k_max, const int32_t* ctx_len, int32_t B, int32_t Hq,
                           int32_t Hkv, int32_t G, const SplitArgs& sp, float scale_log2, float* ws_o, float2* ws_ml,
                           float* out, float* lse, __bf16* x, int32_t* status) {
-    launch_timed(attn_splitk_kernel<DT, BS, W>, grid, dim3(W * kWave), (uint32_t)lds, st, nullptr, done,
+    launch_timed(attn_splitk_kernel<DT, BS, W, GP>, grid, dim3(W * kWave), (uint32_t)lds, st, nullptr, done,
                  (const uint16_t*)q, (const uint16_t*)pool, n_slots, table, max_blocks, sel_idx, sel_cnt, k_max,
                  ctx_len, B, Hq, Hkv, G, sp, scale_log2, ws_o, ws_ml, out, lse, x, status);
 }
@@ -549,20 +707,25 @@ hipError_t launch_attention(const pulse_shape& s, const void* q, const void* poo
     const float scale_log2 = sm_scale * 1.4426950408889634f;
     // stop event of the split-K kernel: split_done, or `done` when no combine follows it
     const hipEvent_t splitk_stop = split_done ? split_done : (n_wg <= 1 ? done : nullptr);
-#define PULSE_ATTN(DT, BS, W)                                                                                        \
-    launch_attn_t<DT, BS, W>(grid, lds, st, splitk_stop, q, pool, n_slots, table, max_blocks, sel_idx, sel_cnt,     \
-                             k_max, ctx_len, B, Hq, Hkv, G, sp, scale_log2, ws_o, ws_ml, out, lse, x, status)
+#define PULSE_ATTN(...)                                                                                              \
+    launch_attn_t<__VA_ARGS__>(grid, lds, st, splitk_stop, q, pool, n_slots, table, max_blocks, sel_idx, sel_cnt,   \
+                               k_max, ctx_len, B, Hq, Hkv, G, sp, scale_log2, ws_o, ws_ml, out, lse, x, status)
 #define PULSE_ATTN_W(DT, BS) \
     if (W == 8) PULSE_ATTN(DT, BS, 8); else PULSE_ATTN(DT, BS, 4)
-    if (s.dtype == PULSE_BF16) {
-        if (s.block_size == 16) PULSE_ATTN_W(PULSE_BF16, 16);
-        else if (s.block_size == 32) PULSE_ATTN_W(PULSE_BF16, 32);
-        else PULSE_ATTN_W(PULSE_BF16, 64);
-    } else {
-        if (s.block_size == 16) PULSE_ATTN_W(PULSE_F16, 16);
-        else if (s.block_size == 32) PULSE_ATTN_W(PULSE_F16, 32);
-        else PULSE_ATTN_W(PULSE_F16, 64);
-    }
+#define PULSE_ATTN_KV4(DT, BS)                \
+    if (G <= 4) PULSE_ATTN(DT, BS, 8, 4);     \
+    else if (G <= 8) PULSE_ATTN(DT, BS, 8, 8); \
+    else PULSE_ATTN(DT, BS, 4, 16)
+#define PULSE_ATTN_BS(WHICH, DT)                   \
+    if (s.block_size == 16) { WHICH(DT, 16); }      \
+    else if (s.block_size == 32) { WHICH(DT, 32); } \
+    else { WHICH(DT, 64); }
+    if (s.dtype == PULSE_BF16) { PULSE_ATTN_BS(PULSE_ATTN_W, PULSE_BF16) }
+    else if (s.dtype == PULSE_F16) { PULSE_ATTN_BS(PULSE_ATTN_W, PULSE_F16) }
+    else if (s.dtype == PULSE_BF16_KV4) { PULSE_ATTN_BS(PULSE_ATTN_KV4, PULSE_BF16_KV4) }
+    else { PULSE_ATTN_BS(PULSE_ATTN_KV4, PULSE_F16_KV4) }
+#undef PULSE_ATTN_BS
+#undef PULSE_ATTN_KV4
 #undef PULSE_ATTN_W
 #undef PULSE_ATTN
     hipError_t e = hipGetLastError();

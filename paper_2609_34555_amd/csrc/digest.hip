@@ -435,7 +435,7 @@ hipError_t launch_average_scores(const pulse_shape& s, const void* q, const void
         return hipGetLastError();
     }
     const int32_t H = s.num_kv_heads, G = s.num_q_heads / H;
-    if (s.dtype == PULSE_BF16)
+    if (elem_type(s.dtype) == PULSE_BF16)
         launch_average_dt<PULSE_BF16>(G, st, q, digests, blk_off, B, total_blocks, s.num_q_heads, H, n_sink, n_local,
                                       scores);
     else
@@ -454,7 +454,7 @@ hipError_t launch_score(const pulse_shape& s, const void* q, const void* digests
         return e;
     }
     const int G = s.num_q_heads / s.num_kv_heads;
-    if (s.dtype == PULSE_BF16)
+    if (elem_type(s.dtype) == PULSE_BF16)
         launch_score_dt<PULSE_BF16>(G, heads, st, start, stop, q, digests, blk_off, B, total_blocks, s.num_q_heads,
                                     solo, n_sink, n_local, scores, rel);
     else

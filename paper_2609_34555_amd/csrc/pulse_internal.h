@@ -25,6 +25,14 @@ constexpr int kMaxGroup = 16;   // G = Hq / Hkv padded to one 16-wide MFMA tile
 constexpr int kChunkTokens = 32;  // attention processes 32 tokens per MFMA step
 constexpr int kMaxBatch = 4096;   // requests per call: the recall and publish kernels scan their counts in LDS
 
+// ---- dtypes -----------------------------------------------------------------
+
+// 16-bit type of the queries and rows of a dtype, and whether its cache is held in 4 bits.
+__host__ __device__ constexpr int elem_type(int dtype) {
+    return dtype == PULSE_BF16 || dtype == PULSE_BF16_KV4 ? PULSE_BF16 : PULSE_F16;
+}
+__host__ __device__ constexpr bool is_kv4(int dtype) { return dtype == PULSE_F16_KV4 || dtype == PULSE_BF16_KV4; }
+
 // ---- timed launches ---------------------------------------------------------
 
 // Launch with optional timing events carried by the dispatch itself
@@ -163,7 +171,8 @@ inline int64_t attn_partial_units(const pulse_shape& s, int32_t B, int32_t k_max
     return (int64_t)B * s.num_kv_heads * ((p.n_split + W - 1) / W);
 }
 WsLayout ws_layout(const pulse_shape& s, int32_t B, int32_t k_max, int64_t total_blocks);
-bool shape_supported(const pulse_shape* s);
+bool shape_supported(const pulse_shape* s);      // a 16-bit cache
+bool kv_shape_supported(const pulse_shape* s);   // a 16-bit or a 4-bit cache
 
 // ---- launchers (each returns hipSuccess or the launch error) --------------
 
@@ -294,6 +303,27 @@ MamPlan mam_plan(int32_t B, int32_t Hkv, int32_t max_blocks, int32_t bs);
 hipError_t launch_mam(const pulse_shape& s, const void* q, const void* pool, int32_t n_slots, const int32_t* table,
                       int32_t max_blocks, const int32_t* ctx_len, int32_t B, int32_t n_sink, int32_t n_local,
                       float sm_scale, float* mam, float4* part, int32_t* status, hipStream_t st);
+
+// Block offsets, tables and slot maps from request lengths (tables.hip).
+size_t tables_ws_bytes(int32_t B, int32_t bs, int64_t max_tokens);
+hipError_t launch_tables(const int32_t* ctx, const int32_t* fresh, int32_t B, int32_t bs, int32_t* table,
+                         int32_t max_blocks, const int32_t* free_slots, int32_t* free_head, int32_t n_free,
+                         int32_t n_slots, int64_t* blk_off, int32_t* tok_off, int64_t* slot_map, int32_t* positions,
+                         int64_t max_tokens, int32_t* status, void* ws, hipStream_t st);
+
+// Head norms with the rotation (rope.hip).
+hipError_t launch_qk_norm_rope(const pulse_shape& s, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                               int32_t rows, const int32_t* positions, const void* qw, const void* kw, float eps,
+                               const double* inv_freq, int32_t rot, bool inter, void* q_out, int64_t q_out_stride,
+                               void* k_out, int64_t k_out_stride, hipStream_t st);
+
+// Rows into the cache and back (cache.hip).
+hipError_t launch_append_kv(const pulse_shape& s, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                            const int64_t* slot_map, int32_t rows, void* pool, int32_t n_slots, int32_t* status,
+                            hipStream_t st);
+hipError_t launch_load_kv(const pulse_shape& s, const void* pool, int32_t n_slots, const int64_t* slot_map,
+                          int32_t rows, void* k, int64_t k_stride, void* v, int64_t v_stride, int32_t* status,
+                          hipStream_t st);
 
 // Host-side argument check: return `code` from the calling entry point.
 #define PULSE_REQUIRE(cond, code)   \

@@ -136,7 +136,34 @@ __device__ inline void copy_chunk(const uint8_t* __restrict__ src, uint8_t* __re
     }
 }
 
+// The first `pieces` 16-byte pieces of a chunk that its threads do not fill.
+template <int LPT, bool NT>
+__device__ inline void copy_part(const uint8_t* __restrict__ src, uint8_t* __restrict__ dst, int tid, int pieces) {
+    u32x4 v[LPT];
+#pragma unroll
+    for (int k = 0; k < LPT; ++k)
+        if (tid + k * kCopyThreads < pieces)
+            v[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src) + tid + k * kCopyThreads);
+#pragma unroll
+    for (int k = 0; k < LPT; ++k)
+        if (tid + k * kCopyThreads < pieces) {
+            if constexpr (NT)
+                __builtin_nontemporal_store(v[k], reinterpret_cast<u32x4*>(dst) + tid + k * kCopyThreads);
+            else
+                reinterpret_cast<u32x4*>(dst)[tid + k * kCopyThreads] = v[k];
+        }
+}
+
+// Loads per thread of such a chunk: 20 KiB, which hold a 4-bit block of 8 KV heads and 16 tokens (17 KiB).
+constexpr int kPartLoads = 5;
+
+// Chunks of a block that is not a multiple of any LPT's 4 KiB * LPT (the 4-bit blocks): as few as hold it, of
+// equal length but for the last.
 template <int LPT>
+__host__ __device__ constexpr int64_t part_chunks(int64_t U) { return (U + 4096 * LPT - 1) / (4096 * LPT); }
+
+// PARTS: the block is cut into part_chunks.
+template <int LPT, bool PARTS>
 __global__ __launch_bounds__(kCopyThreads) void recall_copy_kernel(
     const uint8_t* __restrict__ host, const int64_t* __restrict__ blk_off, int32_t B, int32_t k_max,
     int32_t* __restrict__ table, int32_t max_blocks, const int32_t* __restrict__ free_slots,
@@ -214,8 +241,8 @@ __global__ __launch_bounds__(kCopyThreads) void recall_copy_kernel(
         if (go) *free_head = fh0 + (int32_t)total;
     }
     if (!go) return;
-    constexpr int64_t chunk = 4096 * LPT;
-    const int64_t cpb = U / chunk;
+    const int64_t cpb = PARTS ? part_chunks<LPT>(U) : U / (4096 * LPT);
+    const int64_t chunk = PARTS ? (U / 16 + cpb - 1) / cpb * 16 : 4096 * LPT;
     const int64_t n_chunks = total * cpb;
     const bool nt_store = total * U > kNtStoreBytes;
     // copying workgroups: those on the first copy_xcds XCDs when the grid spans whole
@@ -241,7 +268,10 @@ __global__ __launch_bounds__(kCopyThreads) void recall_copy_kernel(
             if (slot < 0 || slot >= n_slots) continue;  // checked above; guards the store all the same
             const uint8_t* src = host + (blk_off[r] + j) * U + part * chunk;
             uint8_t* dst = pool + (int64_t)slot * U + part * chunk;
-            copy_chunk<LPT, decltype(nt)::value>(src, dst, tid);
+            if constexpr (PARTS)
+                copy_part<LPT, decltype(nt)::value>(src, dst, tid, (int)(min(chunk, U - part * chunk) / 16));
+            else
+                copy_chunk<LPT, decltype(nt)::value>(src, dst, tid);
             if (part == 0 && tid == 0) table[(size_t)r * max_blocks + j] = slot;
         }
     };
@@ -305,18 +335,21 @@ hipError_t launch_recall_copy(const void* host_kv, const int64_t* blk_off, int32
     int lpt = 2;
     if (PULSE_RECALL_LPT >= 8 && unit_bytes % 32768 == 0) lpt = 8;
     else if (unit_bytes % 16384 == 0) lpt = 4;
+    const bool parts = unit_bytes % 8192 != 0;
     const int64_t chunk = 4096 * (int64_t)lpt;
-    const int64_t max_chunks = (int64_t)B * k_max * (int64_t)(unit_bytes / chunk);
+    const int64_t cpb = parts ? part_chunks<kPartLoads>((int64_t)unit_bytes) : (int64_t)(unit_bytes / chunk);
+    const int64_t max_chunks = (int64_t)B * k_max * cpb;
     const int64_t max_bytes = (int64_t)B * k_max * (int64_t)unit_bytes;
     const int64_t cap = (copy_xcds >= kXcds && max_bytes <= kSmallRecallBytes) ? kRecallGridSmall : kRecallGrid;
     const unsigned grid = (unsigned)(max_chunks < cap ? (max_chunks > 0 ? max_chunks : 1) : cap);
-#define PULSE_COPY(L)                                                                                              \
-    launch_timed(recall_copy_kernel<L>, dim3(grid), dim3(kCopyThreads), 0u, st, start, stop, (const uint8_t*)host_kv, \
+#define PULSE_COPY(...)                                                                                            \
+    launch_timed(recall_copy_kernel<__VA_ARGS__>, dim3(grid), dim3(kCopyThreads), 0u, st, start, stop, (const uint8_t*)host_kv, \
                  blk_off, B, k_max, table, max_blocks, free_slots, free_head, n_free, (uint8_t*)pool, n_slots,        \
                  (int64_t)unit_bytes, miss_list, miss_cnt, run_cnt, req_err, misc, stats, status, copy_xcds)
-    if (lpt == 8) PULSE_COPY(8);
-    else if (lpt == 4) PULSE_COPY(4);
-    else PULSE_COPY(2);
+    if (parts) PULSE_COPY(kPartLoads, true);
+    else if (lpt == 8) PULSE_COPY(8, false);
+    else if (lpt == 4) PULSE_COPY(4, false);
+    else PULSE_COPY(2, false);
 #undef PULSE_COPY
     return hipGetLastError();
 }

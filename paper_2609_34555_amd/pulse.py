@@ -27,6 +27,8 @@ PULSE_ERR_TIMEOUT = 8
 NOALLOC_SCRATCH_BYTES = 32 << 20  # PULSE_NOALLOC_SCRATCH_BYTES: static workspace of pulse_decode_layer_noalloc
 PULSE_F16 = 0
 PULSE_BF16 = 1
+PULSE_F16_KV4 = 2  # 16-bit queries and rows, KV blocks in 4 bits
+PULSE_BF16_KV4 = 3
 
 EXPORTED = (
     "pulse_status_string", "pulse_block_bytes", "pulse_workspace_bytes", "pulse_build_digests",
@@ -39,6 +41,7 @@ EXPORTED = (
     "pulse_ioaa_plan", "pulse_average_workspace_bytes", "pulse_select_average", "pulse_mam_workspace_bytes",
     "pulse_mam", "pulse_pick_solo_heads", "pulse_irq_create", "pulse_irq_destroy", "pulse_irq_step",
     "pulse_probe_hbm_read", "pulse_probe_hbm_sink_bytes", "pulse_release_recalled", "pulse_attention_workgroups",
+    "pulse_tables_workspace_bytes", "pulse_build_tables", "pulse_qk_norm_rope", "pulse_append_kv", "pulse_load_kv",
 )
 
 
@@ -184,6 +187,13 @@ def signatures():
         "pulse_ioaa_plan": (ctypes.c_int, [ctypes.POINTER(pulse_ioaa_params), _P, I32, _P,
                                            ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64),
                                            ctypes.POINTER(ctypes.c_int64)]),
+        "pulse_tables_workspace_bytes": (SZ, [SP, I32, I64]),
+        "pulse_build_tables": (ctypes.c_int, [SP, _P, _P, I32, _P, I32, _P, _P, I32, I32, _P, _P, _P, _P, I64, _P, _P,
+                                              SZ, _P]),
+        "pulse_qk_norm_rope": (ctypes.c_int, [SP, _P, I64, _P, I64, I32, _P, _P, _P, F, _P, I32, I32, _P, I64, _P, I64,
+                                              _P]),
+        "pulse_append_kv": (ctypes.c_int, [SP, _P, I64, _P, I64, _P, I32, _P, I32, _P, _P]),
+        "pulse_load_kv": (ctypes.c_int, [SP, _P, I32, _P, I32, _P, I64, _P, I64, _P, _P]),
         "pulse_events_create": (ctypes.c_int, [I32, _P]),
         "pulse_events_destroy": (ctypes.c_int, [I32, _P]),
         "pulse_event_elapsed_ms": (ctypes.c_int, [_P, _P, ctypes.POINTER(ctypes.c_float)]),
@@ -295,6 +305,43 @@ def pulse_mam(shape, q, slot_pool, n_slots, block_table, max_blocks, ctx_len, B,
                          _ptr(ctx_len), B, n_sink_blocks, n_local_blocks, float(sm_scale), _ptr(mam),
                          _ptr(dev_status), _ptr(ws), ws_bytes, _stream(stream))
     return _check(st, "pulse_mam", check)
+
+
+def pulse_tables_workspace_bytes(shape: pulse_shape, B: int, max_tokens: int) -> int:
+    return lib().pulse_tables_workspace_bytes(ctypes.byref(shape), B, max_tokens)
+
+
+def pulse_build_tables(shape, ctx_len, new_len, B, block_table, max_blocks, free_slots, free_head, n_free, n_slots,
+                       blk_off, tok_off, slot_map, positions, max_tokens, dev_status, ws, ws_bytes, stream=None,
+                       check=True):
+    st = lib().pulse_build_tables(ctypes.byref(shape), _ptr(ctx_len), _ptr(new_len), B, _ptr(block_table), max_blocks,
+                                  _ptr(free_slots), _ptr(free_head), n_free, n_slots, _ptr(blk_off), _ptr(tok_off),
+                                  _ptr(slot_map), _ptr(positions), max_tokens, _ptr(dev_status), _ptr(ws), ws_bytes,
+                                  _stream(stream))
+    return _check(st, "pulse_build_tables", check)
+
+
+def pulse_qk_norm_rope(shape, q, q_stride, k, k_stride, n_rows, positions, q_weight, k_weight, eps, inv_freq, rot_dim,
+                       interleaved, q_out, q_out_stride, k_out, k_out_stride, stream=None, check=True):
+    st = lib().pulse_qk_norm_rope(ctypes.byref(shape), _ptr(q), q_stride, _ptr(k), k_stride, n_rows, _ptr(positions),
+                                  _ptr(q_weight), _ptr(k_weight), float(eps), _ptr(inv_freq), rot_dim,
+                                  int(interleaved), _ptr(q_out), q_out_stride, _ptr(k_out), k_out_stride,
+                                  _stream(stream))
+    return _check(st, "pulse_qk_norm_rope", check)
+
+
+def pulse_append_kv(shape, k, k_stride, v, v_stride, slot_map, n_rows, slot_pool, n_slots, dev_status, stream=None,
+                    check=True):
+    st = lib().pulse_append_kv(ctypes.byref(shape), _ptr(k), k_stride, _ptr(v), v_stride, _ptr(slot_map), n_rows,
+                               _ptr(slot_pool), n_slots, _ptr(dev_status), _stream(stream))
+    return _check(st, "pulse_append_kv", check)
+
+
+def pulse_load_kv(shape, slot_pool, n_slots, slot_map, n_rows, k, k_stride, v, v_stride, dev_status, stream=None,
+                  check=True):
+    st = lib().pulse_load_kv(ctypes.byref(shape), _ptr(slot_pool), n_slots, _ptr(slot_map), n_rows, _ptr(k), k_stride,
+                             _ptr(v), v_stride, _ptr(dev_status), _stream(stream))
+    return _check(st, "pulse_load_kv", check)
 
 
 def pulse_pick_solo_heads(mam, check=True):

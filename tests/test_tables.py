@@ -1,0 +1,219 @@
+"""Block offsets, tables and slot maps of a step, against loops over requests, blocks and tokens."""
+import random
+
+import pytest
+import torch
+
+import plain64
+from paper_2609_34555_amd import pulse as P
+from parity import say
+
+DEV = "cuda"
+FAKE = 0x1000
+
+
+def shape(bs=16, **kw):
+    return P.make_shape(**{**dict(num_q_heads=8, num_kv_heads=2, head_dim=128, block_size=bs, dtype=P.PULSE_BF16), **kw})
+
+
+class Step:
+    """Device buffers of a call; every output starts as garbage."""
+
+    def __init__(self, ctx, new, bs, table, free, n_slots, max_tokens, head=0):
+        t = lambda x, d=torch.int32: torch.tensor(x, dtype=d, device=DEV)  # noqa: E731
+        self.B, self.bs, self.n_slots, self.cap = len(ctx), bs, n_slots, max_tokens
+        self.ctx, self.new = t(list(ctx)), t(list(new))
+        self.table = t(table).view(self.B, len(table[0]))
+        self.free, self.head = t(list(free)), t([head])
+        self.blk = t([77] * (self.B + 1), torch.int64)
+        self.tok, self.pos = t([77] * (self.B + 1)), t([77] * (max_tokens + 4))
+        self.place = t([77] * (max_tokens + 4), torch.int64)
+        self.status = t([0])
+        self.sh = shape(bs)
+        self.nb = P.pulse_tables_workspace_bytes(self.sh, self.B, max_tokens)
+        self.ws = torch.full((self.nb,), 255, dtype=torch.uint8, device=DEV)
+
+    def run(self, **kw):
+        P.pulse_build_tables(self.sh, self.ctx, self.new, self.B, self.table, max(1, self.table.shape[1]), self.free,
+                             self.head, self.free.numel(), self.n_slots, self.blk, self.tok, self.place, self.pos,
+                             self.cap, self.status, self.ws, self.nb, **kw)
+        return self
+
+    def got(self):
+        assert (self.pos[self.cap:] == 77).all() and (self.place[self.cap:] == 77).all()
+        return (self.blk.tolist(), self.tok.tolist(), self.place[: self.cap].tolist(), self.pos[: self.cap].tolist(),
+                self.table.tolist(), self.head.item())
+
+
+def start(ctx, new, bs, rng, spare=5, later=0.0):
+    """A table whose earlier blocks have slots of no order (and some of the later ones, as after a shortened
+    sequence), and the free list of the other slots."""
+    mb = max([1] + [-(-x // bs) for x in ctx]) + 2
+    n = [-(-x // bs) for x in ctx]
+    slots = list(range(sum(n) + spare))
+    rng.shuffle(slots)
+    table = [[-1] * mb for _ in ctx]
+    for r, (x, k) in enumerate(zip(ctx, new)):
+        for j in range(n[r]):
+            if j < -(-(x - k) // bs) or rng.random() < later:
+                table[r][j] = slots.pop()
+    return table, slots, sum(n) + spare
+
+
+CASES = [  # contexts, new tokens, bs, room behind the last token, share of later blocks that have a slot
+    ([1], [1], 16, 0, 0.0),
+    ([1], [0], 64, 3, 0.0),
+    ([0, 0, 5, 0], [0, 0, 5, 0], 16, 2, 0.0),
+    ([16, 17, 32, 33, 100], [1, 1, 1, 1, 1], 16, 0, 0.0),
+    ([16, 17, 32, 33, 100], [16, 2, 32, 0, 37], 16, 9, 0.0),
+    ([64, 65, 1, 128, 500], [64, 65, 1, 1, 436], 64, 0, 0.5),
+    ([31, 32, 33, 4000], [31, 1, 33, 3999], 32, 1, 0.3),
+    ([700 + 13 * r for r in range(70)], [1] * 70, 16, 26, 0.0),          # a decode step
+    ([20 * r + 1 for r in range(70)], [r % 7 for r in range(70)], 16, 0, 0.1),
+    ([3000] * 20, [2999] * 20, 16, 0, 0.05),                              # several rounds of one workgroup
+    ([16 * 4094 - 5], [16 * 4094 - 5], 16, 5, 0.2),                       # the largest step of one workgroup
+    ([16 * 4094 + 16], [16 * 4094 + 16], 16, 0, 0.2),                     # and the smallest of two launches
+    ([60000, 1, 0, 70001, 33, 16 * 2048], [59999, 1, 0, 70001, 2, 16 * 2048], 16, 700, 0.1),
+    ([300000, 5, 300001], [299990, 5, 300001], 64, 0, 0.02),
+    ([x % 50 for x in range(4096)], [min(1, x % 50) for x in range(4096)], 16, 0, 0.0),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ctx,new,bs,room,later", CASES)
+def test_tables(ctx, new, bs, room, later):
+    say(f"\n[gpu] tables B={len(ctx)} tokens={sum(new)} bs={bs}")
+    rng = random.Random(len(ctx) + sum(ctx))
+    table, free, n_slots = start(ctx, new, bs, rng, later=later)
+    cap = sum(new) + room
+    s = Step(ctx, new, bs, table, free, n_slots, cap).run()
+    want = plain64.tables(ctx, new, bs, table, free, 0, cap)
+    assert s.status.item() == 0
+    assert s.got() == tuple(want)
+    s.run()  # once more on its own result: every block has its slot
+    assert s.status.item() == 0 and s.got() == tuple(want)
+
+
+@pytest.mark.gpu
+def test_tables_of_no_request_clear_the_maps():
+    s = Step([], [], 16, [[]], [3, 4], 8, 5, head=1).run()
+    assert s.status.item() == 0
+    assert s.got()[:4] == ([0], [0], [-1] * 5, [-1] * 5) and s.head.item() == 1
+    s = Step([40], [0], 16, [[0, 1, 2]], [], 8, 0).run()  # no new token, no map at all
+    assert s.got() == ([0, 3], [0, 0], [], [], [[0, 1, 2]], 0)
+
+
+@pytest.mark.gpu
+def test_tables_step_by_step():
+    """A prompt, then tokens one at a time, the free list's head kept between the calls."""
+    rng = random.Random(5)
+    ctx, bs = [30, 1, 47], 16
+    table, free, n_slots = start(ctx, ctx, bs, rng, spare=20)
+    s = Step(ctx, ctx, bs, table, free, n_slots, 80).run()
+    want = plain64.tables(ctx, ctx, bs, table, free, 0, 80)
+    assert s.got() == tuple(want)
+    for _ in range(20):
+        ctx = [x + 1 for x in ctx]
+        s.ctx += 1
+        s.new.fill_(1)
+        s.run()
+        want = plain64.tables(ctx, [1] * 3, bs, want[4], free, want[5], 80)
+        assert s.got() == tuple(want) and s.status.item() == 0
+
+
+def _bad(what, ctx, new, table, free, n_slots, bs):
+    """(changes to a good step, status) of one fault."""
+    ctx, new, table, free = list(ctx), list(new), [list(r) for r in table], list(free)
+    cap, head, code = sum(new) + 3, 0, P.PULSE_ERR_BAD_INDEX
+    need = sum(1 for r, (x, k) in enumerate(zip(ctx, new)) if k
+               for j in range((x - k) // bs, -(-x // bs)) if table[r][j] == -1)
+    last = -(-ctx[-1] // bs) - 1
+    if what == "exhausted":
+        free, code = free[: need - 1], P.PULSE_ERR_POOL_EXHAUSTED
+    elif what == "exhausted_head":
+        head, code = len(free) - need + 1, P.PULSE_ERR_POOL_EXHAUSTED
+    elif what == "slot":
+        free[need - 1] = n_slots
+    elif what == "slot_negative":
+        free[0] = -1
+    elif what == "entry":
+        table[-1][last] = n_slots
+    elif what == "entry_negative":
+        table[-1][last] = -2
+    elif what == "partial":
+        r = next(r for r, (x, k) in enumerate(zip(ctx, new)) if k and (x - k) % bs)
+        table[r][(ctx[r] - new[r]) // bs] = -1
+    elif what == "head":
+        head = len(free) + 1
+    elif what == "head_negative":
+        head = -1
+    elif what == "ctx_negative":
+        ctx[1] = -1
+    elif what == "new_negative":
+        new[0] = -1
+    elif what == "new_above":
+        new[0] = ctx[0] + 1
+    elif what == "long":
+        ctx[0] = len(table[0]) * bs + 1
+    elif what == "tokens":
+        cap = sum(new) - 1
+    elif what == "huge":
+        ctx[0] = new[0] = 2**31 - 1
+    return ctx, new, table, free, cap, head, code
+
+
+FAULTS = ["exhausted", "exhausted_head", "slot", "slot_negative", "entry", "entry_negative", "partial", "head",
+          "head_negative", "ctx_negative", "new_negative", "new_above", "long", "tokens", "huge"]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("large", [False, True])
+@pytest.mark.parametrize("what", FAULTS)
+def test_tables_faults_change_nothing(what, large):
+    say(f"\n[gpu] tables fault {what} large={large}")
+    rng = random.Random(9)
+    bs = 16
+    ctx, new = ([100, 33, 0, 64], [37, 1, 0, 64]) if not large else ([100, 33, 0, 70000], [37, 1, 0, 69990])
+    table, free, n_slots = start(ctx, new, bs, rng)
+    good = Step(ctx, new, bs, table, free, n_slots, sum(new) + 3).run()
+    assert good.status.item() == 0
+    c2, n2, t2, f2, cap, head, code = _bad(what, ctx, new, table, free, n_slots, bs)
+    s = Step(c2, n2, bs, t2, f2, n_slots, cap, head).run()
+    assert s.status.item() == code
+    assert s.got() == ([0] * 5, [0] * 5, [-1] * cap, [-1] * cap, t2, head)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("large", [False, True])
+def test_tables_slots_behind_the_needed_ones_are_not_looked_at(large):
+    rng = random.Random(3)
+    ctx = [40, 70000] if large else [40, 70]
+    table, free, n_slots = start(ctx, ctx, 16, rng, spare=0)
+    s = Step(ctx, ctx, 16, table, free + [n_slots, -7], n_slots, sum(ctx)).run()
+    assert s.status.item() == 0
+    assert s.got() == tuple(plain64.tables(ctx, ctx, 16, table, free, 0, sum(ctx)))
+
+
+def test_tables_refusals():
+    sh = shape()
+    a = dict(ctx_len=FAKE, new_len=FAKE, B=2, block_table=FAKE, max_blocks=4, free_slots=FAKE, free_head=FAKE, n_free=3,
+             n_slots=9, blk_off=FAKE, tok_off=FAKE, slot_map=FAKE, positions=FAKE, max_tokens=10, dev_status=FAKE,
+             ws=FAKE, ws_bytes=1 << 20, stream=0, check=False)
+    call = lambda s=sh, **kw: P.pulse_build_tables(s, **{**a, **kw})  # noqa: E731
+    for name in ("ctx_len", "new_len", "block_table", "free_slots", "free_head", "blk_off", "tok_off", "slot_map",
+                 "positions", "dev_status"):
+        assert call(**{name: None}) == P.PULSE_ERR_INVALID_ARG, name
+    for kw in (dict(B=-1), dict(max_blocks=0), dict(n_free=-1), dict(n_slots=0), dict(max_tokens=-1)):
+        assert call(**kw) == P.PULSE_ERR_INVALID_ARG, kw
+    for kw in (dict(B=4097), dict(max_tokens=1 << 31)):
+        assert call(**kw) == P.PULSE_ERR_UNSUPPORTED, kw
+    assert call(shape(bs=8)) == P.PULSE_ERR_UNSUPPORTED
+    assert call(shape(dtype=7)) == P.PULSE_ERR_UNSUPPORTED
+    assert call(ws=None) == P.PULSE_ERR_WORKSPACE
+    nb = P.pulse_tables_workspace_bytes(sh, 4096, 1 << 30)
+    assert nb > 0 and call(B=4096, max_tokens=1 << 30, ws_bytes=nb - 1) == P.PULSE_ERR_WORKSPACE
+    assert P.pulse_tables_workspace_bytes(sh, -1, 5) == 0
+    assert P.pulse_tables_workspace_bytes(sh, 1, -5) == 0
+    assert P.pulse_tables_workspace_bytes(shape(bs=8), 1, 5) == 0
+    assert P.lib().pulse_build_tables(None, *[None] * 2, 0, None, 1, None, None, 0, 1, None, None, None, None, 0, None,
+                                      None, 0, None) == P.PULSE_ERR_INVALID_ARG
