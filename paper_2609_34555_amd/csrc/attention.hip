@@ -307,9 +307,18 @@ __device__ inline void attend_split(const uint16_t* __restrict__ q, const uint16
 // of the P operand hold GP = 4, 8 or 16 query heads for 4, 2 or 1 groups at once (row = g' * GP + q: the query
 // columns of S^T repeat), so P' costs a multiplication per row and token however many heads there are; the
 // product of channel tile t uses the rows of its group t / 2, the other rows of its result are left unused.
-// Codes are exact in bf16 and scales are powers of two, so P' is split into two bf16 parts for either 16-bit type
-// (fp16 would not hold the range of the scales).
+// Codes are exact in bf16 and scales are powers of two, so P' is split into bf16 parts for either 16-bit type (fp16
+// would not hold the range of the scales): three of them, all 24 bits of it.  With two (2^-17 of it) the results
+// were 1.4e-6 off, with three 4e-7, as a computation in fp32 is.
 // Row 4 * grp + v of acc[t] is query head (4 * grp + v) % GP of group (4 * grp + v) / GP of the tile's set.
+template <int GP>
+struct Kv4Step {
+    u32x4 k[2];            // codes of a key's 32 channels, tokens of both sub-tiles
+    uint32_t ks[2];        // their scale bytes
+    u32x4 v[2];            // codes of 8 tokens, channel tiles 0..3 and 4..7
+    u32x2 vs[GP / 4];      // scale bytes of 8 tokens
+};
+
 template <int DT, int BS, int GP>
 __device__ inline void attend_split_kv4(const uint16_t* __restrict__ q, const uint8_t* __restrict__ pool,
                                         int32_t n_slots, const int32_t* __restrict__ table, int32_t max_blocks,
@@ -329,91 +338,104 @@ __device__ inline void attend_split_kv4(const uint16_t* __restrict__ q, const ui
     m_run = -INFINITY;
     l_run = 0.f;
     if (ne <= 0) return;
+    // entry metadata, one entry per lane; an entry without a block reads slot 0 and counts no token
     const int32_t j = lane < ne ? j_lane : -1;
     const int32_t sl = (j >= 0 && j < max_blocks) ? table[(size_t)r * max_blocks + j] : -1;
     const int ctx = ctx_len[r];
     const int64_t n_r = ((int64_t)ctx + BS - 1) / BS;
-    int my_slot = -1, my_nv = 0;
+    int my_slot = 0, my_nv = 0;
     if (lane < ne) {
-        if (j < n_r && sl >= 0 && sl < n_slots) {
+        if (j >= 0 && j < n_r && sl >= 0 && sl < n_slots) {
             my_slot = sl;
             const int64_t v = (int64_t)ctx - (int64_t)j * BS;
             my_nv = v >= BS ? BS : (int)v;
+        } else {
+            report(status, PULSE_ERR_BAD_INDEX);
         }
-        if (my_slot < 0) report(status, PULSE_ERR_BAD_INDEX);
     }
+    const uint64_t whole = __ballot(my_nv == BS);
     // Q^T operand: channels 32 * grp + 8 * kc .. + 7 of the column's query head
     vec qb[4];
     {
         const uint16_t* qr = q + ((size_t)r * Hq + (size_t)h * G + qc) * kHeadDim + grp * kGroup;
 #pragma unroll
         for (int kc = 0; kc < 4; ++kc) qb[kc] = qc < G ? load_vec<ET>(qr + 8 * kc) : zero_vec<ET>();
+        // logits are scaled after their maximum is taken: the sign of the scale goes to Q, a zero becomes tiny
+        if (scale_log2 < 0.f) {
+#pragma unroll
+            for (int kc = 0; kc < 4; ++kc) qb[kc] = -qb[kc];
+        }
+        scale_log2 = fmaxf(fabsf(scale_log2), 1e-30f);
     }
-    const size_t E = (size_t)Hkv * kv4_head_bytes(BS);
+    const uint32_t E = (uint32_t)Hkv * kv4_head_bytes(BS);
     const uint8_t* head = pool + (size_t)h * kv4_head_bytes(BS);
     const int tokens = ne * BS;
 
-#pragma unroll 1
-    for (int t0 = 0; t0 < tokens; t0 += kChunkTokens) {
+    auto load = [&](int t0, Kv4Step<GP>& x) {
         // K: MFMA row m = col is token 8 * (col / 4) + 4 * sub + col % 4
-        u32x4 ka[2];
-        float ks[2];
-        {
-            const int seq = t0 + 8 * (col >> 2);
-            const int e = seq / BS;
-            const int slot = __shfl(my_slot, e < ne ? e : 0);
-            const bool ok = e < ne && slot >= 0;
-            const uint8_t* b = head + (size_t)(ok ? slot : 0) * E;
+        const int k_seq = t0 + 8 * (col >> 2);
+        const uint8_t* kb = head + (size_t)(uint32_t)__shfl(my_slot, k_seq / BS) * E;
+        const int k_row = k_seq % BS + (col & 3);
 #pragma unroll
-            for (int sub = 0; sub < 2; ++sub) {
-                const int row = seq % BS + 4 * sub + (col & 3);
-                ka[sub] = ok ? *reinterpret_cast<const u32x4*>(b + row * 64 + grp * 16) : u32x4{0, 0, 0, 0};
-                ks[sub] = ok ? kv4_scale(b[kv4_key_scales(BS) + row * kGroups + grp]) : 0.f;
-            }
+        for (int sub = 0; sub < 2; ++sub) {
+            x.k[sub] = *reinterpret_cast<const u32x4*>(kb + (k_row + 4 * sub) * 64 + grp * 16);
+            x.ks[sub] = kb[kv4_key_scales(BS) + (k_row + 4 * sub) * kGroups + grp];
         }
         // V: lane group grp holds tokens 8 * grp .. + 7, channels col + 16 * t in word t
-        const int pv_seq = t0 + 8 * grp;
-        const int pv_e = pv_seq / BS;
-        const int pv_slot = __shfl(my_slot, pv_e < ne ? pv_e : 0);
-        const int pv_nv = __shfl(my_nv, pv_e < ne ? pv_e : 0);
-        const int pv_row = pv_seq % BS;
-        const bool pv_ok = pv_e < ne && pv_slot >= 0;
-        const uint8_t* vb = head + (size_t)(pv_ok ? pv_slot : 0) * E;
-        u32x4 vw[2];
-        u32x2 vs[kSets];
+        const int v_seq = t0 + 8 * grp;
+        const uint8_t* vb = head + (size_t)(uint32_t)__shfl(my_slot, v_seq / BS) * E;
+        const int v_row = v_seq % BS;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-            vw[i] = pv_ok ? reinterpret_cast<const u32x4*>(vb + kv4_values(BS) + pv_row * 64 + col * 32)[i]
-                          : u32x4{0, 0, 0, 0};
+            x.v[i] = reinterpret_cast<const u32x4*>(vb + kv4_values(BS) + v_row * 64 + col * 32)[i];
 #pragma unroll
-        for (int k = 0; k < kSets; ++k) {
-            const int g = k * (16 / GP) + col / GP;
-            vs[k] = pv_ok ? *reinterpret_cast<const u32x2*>(vb + kv4_value_scales(BS) + g * BS + pv_row) : u32x2{0, 0};
-        }
+        for (int k = 0; k < kSets; ++k)
+            x.vs[k] = *reinterpret_cast<const u32x2*>(vb + kv4_value_scales(BS) + (k * (16 / GP) + col / GP) * BS + v_row);
+    };
+
+    Kv4Step<GP> next;
+    load(0, next);
+#pragma unroll 1
+    for (int t0 = 0; t0 < tokens; t0 += kChunkTokens) {
+        Kv4Step<GP> now = next;
+        if (t0 + kChunkTokens < tokens) load(t0 + kChunkTokens, next);
         // --- S^T = K . Q^T
         f32x4 s[2];
 #pragma unroll
         for (int sub = 0; sub < 2; ++sub) {
+            const float ks = kv4_scale(now.ks[sub]);
             s[sub] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int kc = 0; kc < 4; ++kc) s[sub] = MQ::mac(kv4_decode8<ET>(ka[sub][kc], ks[sub]), qb[kc], s[sub]);
+            for (int kc = 0; kc < 4; ++kc) s[sub] = MQ::mac(kv4_decode8<ET>(now.k[sub][kc], ks), qb[kc], s[sub]);
         }
         float x[8];
-        float cm = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            x[i] = s[i / 4][i % 4] * scale_log2;
-            if (!pv_ok || pv_row + i >= pv_nv) x[i] = -INFINITY;
-            cm = fmaxf(cm, x[i]);
+        for (int i = 0; i < 8; ++i) x[i] = s[i / 4][i % 4];
+        // blocks that are not whole (the last of the context, a missing one, none behind an odd count): their other
+        // tokens count nothing, whatever their scale bytes are
+        constexpr uint64_t kStepEntries = BS >= kChunkTokens ? 1 : (1 << (kChunkTokens / BS)) - 1;
+        if ((~whole >> (t0 / BS)) & kStepEntries) {
+            const int v_seq = t0 + 8 * grp;
+            const int left = __shfl(my_nv, v_seq / BS) - v_seq % BS;  // tokens of this lane's 8
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (i >= left) x[i] = -INFINITY;
+#pragma unroll
+                for (int k = 0; k < kSets; ++k)
+                    if (i >= left) now.vs[k][i / 4] &= ~(0xFFu << (8 * (i % 4)));
+            }
         }
+        float cm = x[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) cm = fmaxf(cm, x[i]);
         cm = across_groups(cm, [](float a, float b) { return fmaxf(a, b); });
-        const float m_new = fmaxf(m_run, cm);
+        const float m_new = fmaxf(m_run, cm * scale_log2);
         const float m_use = m_new == -INFINITY ? 0.f : m_new;
         const float alpha = exp2_fast(m_run - m_use);
         float psum = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            x[i] = exp2_fast(x[i] - m_use);
+            x[i] = exp2_fast(x[i] * scale_log2 - m_use);
             psum += x[i];
         }
         l_run = l_run * alpha + psum;
@@ -429,21 +451,24 @@ __device__ inline void attend_split_kv4(const uint16_t* __restrict__ q, const ui
         // --- O += P' . V
 #pragma unroll
         for (int k = 0; k < kSets; ++k) {
-            bf16x8 ph, pl;
+            u32x4 part[3];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                // what lies behind the last token is not read into a product, whatever its scale byte is
-                const float sc = pv_row + i < pv_nv ? kv4_scale(vs[k][i / 4] >> (8 * (i % 4)) & 0xFFu) : 0.f;
-                __bf16 hi, lo;
-                MP::split(x[i] * sc, hi, lo);
-                ph[i] = hi;
-                pl[i] = lo;
+            for (int i = 0; i < 4; ++i) {
+                float a = x[2 * i] * kv4_scale(now.vs[k][i / 2] >> (16 * (i % 2)) & 0xFFu);
+                float b = x[2 * i + 1] * kv4_scale(now.vs[k][i / 2] >> (16 * (i % 2) + 8) & 0xFFu);
+#pragma unroll
+                for (int n = 0; n < 3; ++n) {
+                    const bf16x2 two = {(__bf16)a, (__bf16)b};
+                    part[n][i] = __builtin_bit_cast(uint32_t, two);
+                    a -= __uint_as_float(part[n][i] << 16);
+                    b -= __uint_as_float(part[n][i] & 0xFFFF0000u);
+                }
             }
 #pragma unroll
             for (int t = 8 / kSets * k; t < 8 / kSets * (k + 1); ++t) {
-                const bf16x8 v = kv4_decode8<PULSE_BF16>(vw[t / 4][t % 4], 1.0f);
-                acc[t] = MP::mac(ph, v, acc[t]);
-                acc[t] = MP::mac(pl, v, acc[t]);
+                const bf16x8 v = kv4_decode8<PULSE_BF16>(now.v[t / 4][t % 4], 1.0f);
+#pragma unroll
+                for (int n = 0; n < 3; ++n) acc[t] = MP::mac(__builtin_bit_cast(bf16x8, part[n]), v, acc[t]);
             }
         }
     }

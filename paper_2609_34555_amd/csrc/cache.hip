@@ -1,22 +1,26 @@
 // cache.hip -- rows of keys and values into the blocks of a slot pool, and back, by the slot map of a step.
 // Row i belongs at token slot_map[i] % bs of slot slot_map[i] / bs (-1: nowhere).
 //
-// Bound: HBM; a row's head is 512 bytes of 16-bit keys and values against 136 in the 4-bit cache.  A wave owns
-// one head of a run of rows: a lane is channels 2 * lane and 2 * lane + 1, so a row's head is one 256-byte load
-// and a group of 32 channels (one scale) is 16 lanes, a register reduction.
+// Bound: HBM; a row's head is 512 bytes of 16-bit keys and values against 136 in the 4-bit cache.
 //
-// Values lie 8 tokens to a word (or to 16 bytes of the 16-bit cache), so a run is the rows, at most 8, that
-// follow one another inside one octet of tokens: the wave of its first row writes it, whole octets with plain
-// stores.  A shorter run shares words with other tokens, which other rows of the call may be writing: it clears
-// and sets its own bits with atomics, whose order does not matter.
+// Values lie 8 tokens to a word (or to 16 bytes of the 16-bit cache), so the unit of work is a run: the rows, at
+// most 8, that follow one another inside one octet of tokens.  A wave takes one head of a run.  Its lane group g
+// holds tokens 2g and 2g + 1 of the octet and lane l of a group channels 8l .. 8l + 7, so that a head of a row is
+// one 16-byte load per lane, a scale's 32 channels are four neighbouring lanes (two register exchanges) and a
+// row's key codes one 4-byte store per lane.  Values change between "8 channels of 2 tokens" and "8 tokens of 2
+// channels" by exchanges of lane groups in registers.
+// A run shorter than an octet shares words with other tokens, which other rows of the call may be writing: it
+// clears and sets its own bits with atomics, whose order does not matter.
 #include "kv4.h"
 
 namespace pulse {
 
 constexpr int kCacheThreads = 256;
 constexpr int kCacheWaves = kCacheThreads / kWave;
-constexpr int64_t kCacheGrid = 1 << 20;
 constexpr int kOct = 8;
+constexpr int64_t kCacheGrid = 65535;
+// Rows times heads up to which a wave looks at one row (each may begin a run), above at an octet's.
+constexpr int64_t kRunRows = 8192;
 
 struct CacheArgs {
     const uint16_t *k_in, *v_in;  // append
@@ -29,189 +33,297 @@ struct CacheArgs {
     int32_t* status;
 };
 
-// The run that row i begins: its first place and length; n = 0 if i begins none (a row inside a run, a row
-// without a place).  Every lane of the wave takes part and gets the same answer.
+// One head of a run: its rows are `first` .. first + n - 1, their places `at` .. at + n - 1.
 struct Run {
-    int64_t at;
-    int n;
+    int64_t first, at;
+    int n, h;
 };
-__device__ inline Run find_run(const CacheArgs& a, int64_t i, int lane, bool check) {
-    const int64_t row = i - 1 + lane;  // lane 0: the row before
-    int64_t m = -1;
-    if (lane <= kOct && row >= 0 && row < a.rows) m = a.slot_map[row];
-    const int64_t before = __shfl(m, 0);
-    Run r;
-    r.at = __shfl(m, 1);
-    r.n = 0;
-    if (r.at < 0 || r.at >= a.places) {
-        if (check && r.at != -1 && lane == 0) report(a.status, PULSE_ERR_BAD_INDEX);
-        return r;
+
+// Exchange of lane groups: rows 0..3 of a and b become {a0, b0, a2, b2} and {a1, b1, a3, b3} (cross16), or
+// {a0, a1, b0, b1} and {a2, a3, b2, b3} (cross32).
+__device__ inline void cross16(uint32_t& a, uint32_t& b) {
+    const u32x2 r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    a = r[0];
+    b = r[1];
+}
+__device__ inline void cross32(uint32_t& a, uint32_t& b) {
+    const u32x2 r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+    a = r[0];
+    b = r[1];
+}
+
+// Group g holds words 0 .. 7 of its own; afterwards it holds words 2g and 2g + 1 of every group: w[j] is word
+// 2g + j / 4 of group j % 4.
+__device__ inline void transpose_groups(uint32_t (&w)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) cross32(w[i], w[i + 4]);
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+        cross16(w[i], w[i + 2]);
+        cross16(w[i + 1], w[i + 3]);
     }
-    if (r.at % kOct != 0 && before == r.at - 1) return r;
-    // lane 1 + k continues the run if it holds the k-th next place of the octet
-    const bool on = lane >= 1 && lane <= kOct && m == r.at + (lane - 1) && r.at % kOct + (lane - 1) < kOct;
-    r.n = __builtin_ctzll(~(__ballot(on) >> 1));
-    return r;
+    // now w[4 * (group / 2) + 2 * (group % 2) + (word % 2)] of the words 2g, 2g + 1
+    const uint32_t t[8] = {w[0], w[2], w[4], w[6], w[1], w[3], w[5], w[7]};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = t[i];
 }
 
-// Largest of x >= 0 over the 16 lanes of a group; NaN counts as more than anything.
-__device__ inline float group_top(float x) {
-    uint32_t u = __float_as_uint(x);
-    auto top = [&](int y) { u = max(u, (uint32_t)y); };
-    top(__builtin_amdgcn_mov_dpp((int)u, 0xB1, 0xF, 0xF, true));
-    top(__builtin_amdgcn_mov_dpp((int)u, 0x4E, 0xF, 0xF, true));
-    top(__builtin_amdgcn_mov_dpp((int)u, 0x141, 0xF, 0xF, true));
-    top(__builtin_amdgcn_mov_dpp((int)u, 0x140, 0xF, 0xF, true));
-    return __uint_as_float(u);
+// The same back: w[j] holds word 2g + j / 4 of group j % 4; afterwards w[i] is word i of the lane's own group.
+__device__ inline void untranspose_groups(uint32_t (&w)[8]) {
+    uint32_t t[8] = {w[0], w[4], w[1], w[5], w[2], w[6], w[3], w[7]};
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+        cross16(t[i], t[i + 2]);
+        cross16(t[i + 1], t[i + 3]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) cross32(t[i], t[i + 4]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = t[i];
 }
 
-// Two channels of a row as codes (0 .. 255), with the byte of their group's scale.
+// Largest magnitude of 8 16-bit values and of those of the other three lanes of a scale; infinities and NaN
+// are more than anything.
 template <int DT>
-__device__ inline uint32_t encode_pair(uint32_t two, uint32_t& scale_byte) {
-    const float x = elem_to_float<DT>((uint16_t)(two & 0xFFFF)), y = elem_to_float<DT>((uint16_t)(two >> 16));
-    const uint32_t ux = __float_as_uint(x) & 0x7FFFFFFFu, uy = __float_as_uint(y) & 0x7FFFFFFFu;
-    scale_byte = kv4_scale_byte<DT>(group_top(__uint_as_float(max(ux, uy))));
-    return scale_byte == kKv4Nan ? 0u : kv4_encode(x, y, kv4_scale(scale_byte));
+__device__ inline float scale_top(u32x4 v) {
+    uint32_t u = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u = max(max(u, v[i] & 0x7FFFu), (v[i] >> 16) & 0x7FFFu);
+    u = max(u, (uint32_t)__builtin_amdgcn_mov_dpp((int)u, 0xB1, 0xF, 0xF, true));  // lane ^ 1
+    u = max(u, (uint32_t)__builtin_amdgcn_mov_dpp((int)u, 0x4E, 0xF, 0xF, true));  // lane ^ 2
+    return elem_to_float<DT>((uint16_t)u);
+}
+
+// 8 values as 8 codes, channel 8l + i in bits 4i .. 4i + 3, and the byte of their scale.
+template <int DT>
+__device__ inline uint32_t encode8(u32x4 v, uint32_t& scale_byte) {
+    scale_byte = kv4_scale_byte<DT>(scale_top<DT>(v));
+    if (scale_byte == kKv4Nan) return 0;
+    const float s = kv4_scale(scale_byte);
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        w |= kv4_encode(elem_to_float<DT>((uint16_t)(v[i] & 0xFFFF)), elem_to_float<DT>((uint16_t)(v[i] >> 16)), s)
+             << (8 * i);
+    return w;
+}
+
+// x of the four scales of a row (lanes 0-3, 4-7, ..) as the bytes of a word, in every lane of the row.
+__device__ inline uint32_t row_bytes(uint32_t x, int l) {
+    uint32_t u = x << (8 * (l >> 2));
+    u |= (uint32_t)__builtin_amdgcn_mov_dpp((int)u, 0x141, 0xF, 0xF, true);  // mirrored half row
+    u |= (uint32_t)__builtin_amdgcn_mov_dpp((int)u, 0x140, 0xF, 0xF, true);  // mirrored row
+    return u;
 }
 
 template <int DT, int BS, bool KV4>
-__device__ inline void append_run(const CacheArgs& a, int64_t unit, int lane) {
-    const int64_t i = unit / a.Hkv;
-    const int h = (int)(unit % a.Hkv);
-    const Run run = find_run(a, i, lane, h == 0);
-    if (run.n == 0) return;
-    uint32_t k[kOct], v[kOct];
-#pragma unroll
-    for (int t = 0; t < kOct; ++t) {
-        k[t] = v[t] = 0;
-        if (t < run.n) {
-            k[t] = reinterpret_cast<const uint32_t*>(a.k_in + (i + t) * a.k_stride + (size_t)h * kHeadDim)[lane];
-            v[t] = reinterpret_cast<const uint32_t*>(a.v_in + (i + t) * a.v_stride + (size_t)h * kHeadDim)[lane];
-        }
-    }
+__device__ inline void append_run(const CacheArgs& a, const Run& run, int lane) {
+    const int l = lane & 15, grp = lane >> 4;
     const int64_t slot = run.at / BS;
-    const int row = (int)(run.at % BS), t0 = row % kOct;
-    if constexpr (KV4) {
-        uint8_t* base = a.pool + ((size_t)slot * a.Hkv + h) * kv4_head_bytes(BS);
-        uint32_t w0 = 0, w1 = 0;  // words of the lane's two channels
+    const int o0 = (int)(run.at % BS) / kOct * kOct, t0 = (int)(run.at % kOct);  // the octet, the run's place in it
+    u32x4 k[2], v[2];
+    bool on[2];
 #pragma unroll
-        for (int t = 0; t < kOct; ++t) {
-            if (t < run.n) {
-                uint32_t ks, vs;
-                const uint32_t kc = encode_pair<DT>(k[t], ks), vc = encode_pair<DT>(v[t], vs);
-                base[(row + t) * 64 + lane] = (uint8_t)kc;
-                if ((lane & 15) == 0) {
-                    base[kv4_key_scales(BS) + (row + t) * kGroups + (lane >> 4)] = (uint8_t)ks;
-                    base[kv4_value_scales(BS) + (lane >> 4) * BS + row + t] = (uint8_t)vs;
-                }
-                w0 |= (vc & 15u) << (4 * (t0 + t));
-                w1 |= (vc >> 4) << (4 * (t0 + t));
+    for (int i = 0; i < 2; ++i) {
+        const int t = 2 * grp + i - t0;  // row of the run that is this token
+        on[i] = t >= 0 && t < run.n;
+        const int64_t row = run.first + (on[i] ? t : 0);
+        const size_t c = (size_t)run.h * kHeadDim + 8 * l;
+        k[i] = on[i] ? *reinterpret_cast<const u32x4*>(a.k_in + row * a.k_stride + c) : u32x4{0, 0, 0, 0};
+        v[i] = on[i] ? *reinterpret_cast<const u32x4*>(a.v_in + row * a.v_stride + c) : u32x4{0, 0, 0, 0};
+    }
+    const bool full = run.n == kOct;
+    if constexpr (KV4) {
+        uint8_t* base = a.pool + ((size_t)slot * a.Hkv + run.h) * kv4_head_bytes(BS);
+        uint32_t vc[2], vs[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int row = o0 + 2 * grp + i;
+            uint32_t ks;
+            const uint32_t kc = encode8<DT>(k[i], ks);
+            vc[i] = encode8<DT>(v[i], vs[i]);
+            const uint32_t ks4 = row_bytes(ks, l);
+            if (on[i]) {
+                *reinterpret_cast<uint32_t*>(base + row * 64 + 4 * l) = kc;
+                if (l == 0) *reinterpret_cast<uint32_t*>(base + kv4_key_scales(BS) + row * kGroups) = ks4;
             }
         }
-        // channel c = 2 * lane is word [o][c % 16][c / 16]; channel c + 1 the word 8 further on
-        uint32_t* words = reinterpret_cast<uint32_t*>(base + kv4_values(BS)) + (row / kOct) * 128 +
-                          (2 * lane % 16) * 8 + lane / 8;
-        if (run.n == kOct) {
-            words[0] = w0;
-            words[8] = w1;
-        } else {
-            const uint32_t mine = ((1u << (4 * run.n)) - 1) << (4 * t0);
-            atomicAnd(&words[0], ~mine);
-            atomicAnd(&words[8], ~mine);
-            atomicOr(&words[0], w0);
-            atomicOr(&words[8], w1);
+        // value scales of a group: a byte per token
+        uint8_t* vsd = base + kv4_value_scales(BS) + (l >> 2) * BS + o0 + 2 * grp;
+        if ((l & 3) == 0) {
+            if (full) {
+                *reinterpret_cast<uint16_t*>(vsd) = (uint16_t)(vs[0] | vs[1] << 8);
+            } else {
+                if (on[0]) vsd[0] = (uint8_t)vs[0];
+                if (on[1]) vsd[1] = (uint8_t)vs[1];
+            }
+        }
+        // words of 8 tokens: this lane's two tokens of channels 8l + i, then the groups' words or-ed together,
+        // each group keeping two channels
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = ((vc[0] >> (4 * i) & 15u) | (vc[1] >> (4 * i) & 15u) << 4) << (8 * grp);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            cross32(w[i], w[i + 4]);
+            w[i] |= w[i + 4];
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            cross16(w[i], w[i + 2]);
+            w[i] |= w[i + 2];
+        }
+        const uint32_t mine = full ? ~0u : ((1u << (4 * run.n)) - 1) << (4 * t0);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int c = 8 * l + 2 * grp + i;
+            uint32_t* word = reinterpret_cast<uint32_t*>(base + kv4_values(BS)) + (o0 / kOct * 16 + c % 16) * 8 + c / 16;
+            if (full) {
+                *word = w[i];
+            } else {
+                atomicAnd(word, ~mine);
+                atomicOr(word, w[i]);
+            }
         }
     } else {
         uint16_t* base = reinterpret_cast<uint16_t*>(a.pool) + (size_t)slot * 2 * a.Hkv * BS * kHeadDim;
-        uint16_t* kd = base + (size_t)h * BS * kHeadDim;
-        uint16_t* vd = base + (size_t)a.Hkv * BS * kHeadDim + ((size_t)h * kHeadDim + 2 * lane) * BS;
+        uint16_t* kd = base + (size_t)run.h * BS * kHeadDim + 8 * l;
+        uint16_t* vd = base + (size_t)(a.Hkv + run.h) * BS * kHeadDim + o0;
 #pragma unroll
-        for (int t = 0; t < kOct; ++t)
-            if (t < run.n) reinterpret_cast<uint32_t*>(kd + (size_t)(row + t) * kHeadDim)[lane] = k[t];
-        if (run.n == kOct) {
-            u32x4 lo, hi;
+        for (int i = 0; i < 2; ++i)
+            if (on[i]) *reinterpret_cast<u32x4*>(kd + (size_t)(o0 + 2 * grp + i) * kHeadDim) = k[i];
+        uint32_t w[8];  // two tokens of channel 8l + i
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                lo[t] = (v[2 * t] & 0xFFFFu) | (v[2 * t + 1] << 16);
-                hi[t] = (v[2 * t] >> 16) | (v[2 * t + 1] & 0xFFFF0000u);
-            }
-            *reinterpret_cast<u32x4*>(vd + row) = lo;
-            *reinterpret_cast<u32x4*>(vd + BS + row) = hi;
+        for (int i = 0; i < 8; ++i)
+            w[i] = (v[0][i / 2] >> (16 * (i % 2)) & 0xFFFFu) | (v[1][i / 2] >> (16 * (i % 2)) << 16);
+        if (full) {
+            transpose_groups(w);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                *reinterpret_cast<u32x4*>(vd + (size_t)(8 * l + 2 * grp + i) * BS) =
+                    u32x4{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]};
         } else {
 #pragma unroll
-            for (int t = 0; t < kOct; ++t)
-                if (t < run.n) {
-                    vd[row + t] = (uint16_t)(v[t] & 0xFFFF);
-                    vd[BS + row + t] = (uint16_t)(v[t] >> 16);
-                }
+            for (int i = 0; i < 8; ++i) {
+                if (on[0]) vd[(size_t)(8 * l + i) * BS + 2 * grp] = (uint16_t)(w[i] & 0xFFFF);
+                if (on[1]) vd[(size_t)(8 * l + i) * BS + 2 * grp + 1] = (uint16_t)(w[i] >> 16);
+            }
         }
     }
 }
 
 template <int DT, int BS, bool KV4>
-__device__ inline void load_run(const CacheArgs& a, int64_t unit, int lane) {
-    const int64_t i = unit / a.Hkv;
-    const int h = (int)(unit % a.Hkv);
-    const Run run = find_run(a, i, lane, h == 0);
-    if (run.n == 0) return;
+__device__ inline void load_run(const CacheArgs& a, const Run& run, int lane) {
+    const int l = lane & 15, grp = lane >> 4;
     const int64_t slot = run.at / BS;
-    const int row = (int)(run.at % BS), t0 = row % kOct;
-    uint32_t k[kOct], v[kOct];
-    if constexpr (KV4) {
-        const uint8_t* base = a.pool + ((size_t)slot * a.Hkv + h) * kv4_head_bytes(BS);
-        const uint32_t* words = reinterpret_cast<const uint32_t*>(base + kv4_values(BS)) + (row / kOct) * 128 +
-                                (2 * lane % 16) * 8 + lane / 8;
-        const uint32_t w0 = words[0], w1 = words[8];
+    const int o0 = (int)(run.at % BS) / kOct * kOct, t0 = (int)(run.at % kOct);
+    bool on[2];
 #pragma unroll
-        for (int t = 0; t < kOct; ++t) {
-            k[t] = v[t] = 0;
-            if (t < run.n) {
-                const uint32_t kc = base[(row + t) * 64 + lane];
-                const float ks = kv4_scale(base[kv4_key_scales(BS) + (row + t) * kGroups + (lane >> 4)]);
-                const float vs = kv4_scale(base[kv4_value_scales(BS) + (lane >> 4) * BS + row + t]);
-                const uint32_t vc = (w0 >> (4 * (t0 + t)) & 15u) | (w1 >> (4 * (t0 + t)) & 15u) << 4;
-                k[t] = kv4_decode<DT, 0>(kc, ks);
-                v[t] = kv4_decode<DT, 0>(vc, vs);
+    for (int i = 0; i < 2; ++i) on[i] = 2 * grp + i >= t0 && 2 * grp + i < t0 + run.n;
+    u32x4 k[2] = {}, v[2];
+    uint32_t w[8];
+    if constexpr (KV4) {
+        const uint8_t* base = a.pool + ((size_t)slot * a.Hkv + run.h) * kv4_head_bytes(BS);
+        uint32_t kc[2] = {}, ks[2] = {}, vs = 0, mine[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int row = o0 + 2 * grp + i, c = 8 * l + 2 * grp + i;
+            if (on[i]) {
+                kc[i] = *reinterpret_cast<const uint32_t*>(base + row * 64 + 4 * l);
+                ks[i] = base[kv4_key_scales(BS) + row * kGroups + (l >> 2)];
             }
+            mine[i] = reinterpret_cast<const uint32_t*>(base + kv4_values(BS))[(o0 / kOct * 16 + c % 16) * 8 + c / 16];
+        }
+        vs = *reinterpret_cast<const uint16_t*>(base + kv4_value_scales(BS) + (l >> 2) * BS + o0 + 2 * grp);
+        // each group's two words to all groups: word 2g + i of the group's own channels
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            uint32_t e = mine[i], o = mine[i];
+            cross16(e, o);  // e: groups 0 and 2, o: groups 1 and 3
+            uint32_t e2 = e, o2 = o;
+            cross32(e, e2);
+            cross32(o, o2);
+            w[i] = e;
+            w[2 + i] = o;
+            w[4 + i] = e2;
+            w[6 + i] = o2;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            k[i] = __builtin_bit_cast(u32x4, kv4_decode8<DT>(kc[i], kv4_scale(ks[i])));
+            uint32_t c = 0;
+#pragma unroll
+            for (int n = 0; n < 8; ++n) c |= (w[n] >> (8 * grp + 4 * i) & 15u) << (4 * n);
+            v[i] = __builtin_bit_cast(u32x4, kv4_decode8<DT>(c, kv4_scale(vs >> (8 * i) & 0xFFu)));
         }
     } else {
         const uint16_t* base = reinterpret_cast<const uint16_t*>(a.pool) + (size_t)slot * 2 * a.Hkv * BS * kHeadDim;
-        const uint16_t* kd = base + (size_t)h * BS * kHeadDim;
-        const uint16_t* vd = base + (size_t)a.Hkv * BS * kHeadDim + ((size_t)h * kHeadDim + 2 * lane) * BS;
+        const uint16_t* kd = base + (size_t)run.h * BS * kHeadDim + 8 * l;
+        const uint16_t* vd = base + (size_t)(a.Hkv + run.h) * BS * kHeadDim + o0;
 #pragma unroll
-        for (int t = 0; t < kOct; ++t) {
-            k[t] = v[t] = 0;
-            if (t < run.n) {
-                k[t] = reinterpret_cast<const uint32_t*>(kd + (size_t)(row + t) * kHeadDim)[lane];
-                v[t] = (uint32_t)vd[row + t] | (uint32_t)vd[BS + row + t] << 16;
-            }
+        for (int i = 0; i < 2; ++i) {
+            if (on[i]) k[i] = *reinterpret_cast<const u32x4*>(kd + (size_t)(o0 + 2 * grp + i) * kHeadDim);
+            const u32x4 x = *reinterpret_cast<const u32x4*>(vd + (size_t)(8 * l + 2 * grp + i) * BS);
+#pragma unroll
+            for (int n = 0; n < 4; ++n) w[4 * i + n] = x[n];
+        }
+        untranspose_groups(w);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            v[0][n] = (w[2 * n] & 0xFFFFu) | w[2 * n + 1] << 16;
+            v[1][n] = w[2 * n] >> 16 | (w[2 * n + 1] & 0xFFFF0000u);
         }
     }
 #pragma unroll
-    for (int t = 0; t < kOct; ++t)
-        if (t < run.n) {
-            reinterpret_cast<uint32_t*>(a.k_out + (i + t) * a.k_stride + (size_t)h * kHeadDim)[lane] = k[t];
-            reinterpret_cast<uint32_t*>(a.v_out + (i + t) * a.v_stride + (size_t)h * kHeadDim)[lane] = v[t];
+    for (int i = 0; i < 2; ++i)
+        if (on[i]) {
+            const int64_t row = run.first + (2 * grp + i - t0);
+            const size_t c = (size_t)run.h * kHeadDim + 8 * l;
+            *reinterpret_cast<u32x4*>(a.k_out + row * a.k_stride + c) = k[i];
+            *reinterpret_cast<u32x4*>(a.v_out + row * a.v_stride + c) = v[i];
         }
 }
 
-// A wave takes (row, head) pairs a grid apart.
+// grid = (Hkv, groups of kCacheWaves * per rows): a wave takes one head of the runs that begin in its `per` rows (1 or
+// kOct); neighbouring workgroups take neighbouring heads, which lie together in rows and blocks.
 template <int DT, int BS, bool KV4, bool APPEND>
-__global__ __launch_bounds__(kCacheThreads) void cache_kernel(CacheArgs a) {
-    const int64_t units = (int64_t)a.rows * a.Hkv, stride = (int64_t)gridDim.x * kCacheWaves;
-    const int lane = threadIdx.x & 63;
-    for (int64_t u = (int64_t)blockIdx.x * kCacheWaves + (threadIdx.x >> 6); u < units; u += stride) {
-        if constexpr (APPEND) append_run<DT, BS, KV4>(a, u, lane);
-        else load_run<DT, BS, KV4>(a, u, lane);
+__global__ __launch_bounds__(kCacheThreads) void cache_kernel(CacheArgs a, int32_t per) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t step = (int64_t)kCacheWaves * per;
+    for (int64_t r0 = blockIdx.y * step + wave * per; r0 < a.rows; r0 += gridDim.y * step) {
+        // places of the row before, of this wave's rows and of those that its last run may go on to
+        const int64_t row = r0 - 1 + lane;
+        int64_t m = -1;
+        if (lane < per + kOct && row >= 0 && row < a.rows) m = a.slot_map[row];
+        const bool ok = m >= 0 && m < a.places;
+        if (blockIdx.x == 0 && m != -1 && !ok && lane >= 1 && lane <= per) report(a.status, PULSE_ERR_BAD_INDEX);
+        const int64_t prev = __shfl_up(m, 1);
+        const bool goes_on = lane > 0 && ok && prev == m - 1 && m % kOct != 0;
+        const uint64_t on = __ballot(goes_on);
+        uint64_t begin = __ballot(ok && !goes_on) & (((1ull << per) - 1) << 1);
+        while (begin) {
+            const int at = __builtin_ctzll(begin);
+            begin &= begin - 1;
+            Run run;
+            run.first = r0 - 1 + at;
+            const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)m, at);
+            const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(m >> 32), at);
+            run.at = (int64_t)((uint64_t)hi << 32 | lo);
+            run.n = 1 + __builtin_ctzll(~(on >> (at + 1)));
+            run.h = blockIdx.x;
+            if constexpr (APPEND) append_run<DT, BS, KV4>(a, run, lane);
+            else load_run<DT, BS, KV4>(a, run, lane);
+        }
     }
 }
 
 template <int DT, int BS, bool KV4>
 static void launch_cache_t(const CacheArgs& a, bool append, hipStream_t st) {
-    const int64_t groups = ((int64_t)a.rows * a.Hkv + kCacheWaves - 1) / kCacheWaves;
-    const dim3 grid((unsigned)(groups < kCacheGrid ? groups : kCacheGrid));
-    if (append) hipLaunchKernelGGL((cache_kernel<DT, BS, KV4, true>), grid, dim3(kCacheThreads), 0, st, a);
-    else hipLaunchKernelGGL((cache_kernel<DT, BS, KV4, false>), grid, dim3(kCacheThreads), 0, st, a);
+    const int32_t per = (int64_t)a.rows * a.Hkv > kRunRows ? kOct : 1;
+    const int64_t groups = ((int64_t)a.rows + kCacheWaves * per - 1) / (kCacheWaves * per);
+    const dim3 grid((unsigned)a.Hkv, (unsigned)(groups < kCacheGrid ? groups : kCacheGrid));
+    if (append) hipLaunchKernelGGL((cache_kernel<DT, BS, KV4, true>), grid, dim3(kCacheThreads), 0, st, a, per);
+    else hipLaunchKernelGGL((cache_kernel<DT, BS, KV4, false>), grid, dim3(kCacheThreads), 0, st, a, per);
 }
 
 template <int DT, bool KV4>

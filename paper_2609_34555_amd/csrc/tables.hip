@@ -5,25 +5,22 @@
 // (ctx - new) / bs .. ceil(ctx / bs) - 1.  Cells of all requests are numbered in order; those without a slot
 // take the free list front to back, so a cell's slot is free_slots[head + cells without a slot before it].
 //
-// Bound: two memory round trips (lengths, table entries) and the launches; beyond some ten thousand tokens the
-// 12 bytes written per token.  Nothing may be written before every length, entry and slot has been checked.
-// Small steps run in one workgroup, which counts, checks and writes.  Larger ones take two launches over tiles
-// of cells: the first counts and checks each tile, the second adds the tiles' counts up (each workgroup for
-// itself) and writes.
+// Bound: memory round trips (lengths; then table entries and free slots, which do not wait for one another; then the
+// writes) and launches; beyond some ten thousand tokens the 12 bytes written per token.  Nothing may be written before
+// every length, entry and slot has been checked.  Small steps run in one workgroup, whose threads keep their cells in
+// registers.  Larger ones take two launches over tiles of cells: the first counts and checks each tile, the second adds
+// the tiles' counts up (each workgroup for itself) and writes.
 #include "pulse_internal.h"
 
 namespace pulse {
 
-constexpr int kTabThreads = 1024;
-constexpr int kTabWaves = kTabThreads / kWave;
-constexpr int kTabPer = kMaxBatch / kTabThreads;  // requests of a thread
-constexpr int kTileCells = 2048;                  // cells of a workgroup of the larger form
-constexpr int kTilePer = kTileCells / kTabThreads;
-constexpr int64_t kOneGroupCells = 4096;          // bound on the cells up to which one workgroup does it all
+constexpr int kCellsPer = 4;            // cells of a thread of the one-workgroup form
+constexpr int kTileThreads = 256;       // a tile is a multiple of that many cells
+constexpr int64_t kMaxTiles = 1024;     // every workgroup of the larger form reads every tile's count
 
 struct TabArgs {
     const int32_t *ctx, *fresh;
-    int32_t B, bs;
+    int32_t B, shift;  // blocks of 1 << shift tokens
     int32_t* table;
     int32_t max_blocks;
     const int32_t* free_slots;
@@ -42,14 +39,16 @@ struct TabArgs {
 struct TabScratch {
     int32_t* head;
     int32_t *count, *bad_place;
+    int32_t tile;  // cells of a tile
 };
 
-struct TabShared {
-    int32_t first[kMaxBatch];     // position of the first new token
-    int32_t tok[kMaxBatch + 1];   // new tokens before request r
-    int32_t cell[kMaxBatch + 1];  // cells before request r
-    uint64_t wave[3][kTabWaves];
-    uint32_t misses[kTabWaves];
+// Sums over the requests, for up to B of them.
+template <int B>
+struct TabRequests {
+    int32_t first[B];     // position of the first new token
+    int32_t tok[B + 1];   // new tokens before request r
+    int32_t cell[B + 1];  // cells before request r
+    uint64_t wave[3][16];
 };
 
 // Exclusive sum of x over the lanes of a wave and its total.  x < 2^46.
@@ -60,87 +59,81 @@ __device__ inline uint64_t wave_sum_before(uint64_t x, uint64_t& total) {
     return ((uint64_t)(shi - hi) << 20) + (slo - lo);
 }
 
-// Checks the lengths and fills the shared sums; false (in every thread) if a length is out of range.  With `write`
-// the block and token offsets go to memory, all zero where the lengths are bad.  tokens / cells: totals.
-__device__ inline bool scan_requests(const TabArgs& a, TabShared& s, int64_t& tokens, int64_t& cells, int64_t* off) {
+// Checks the lengths and fills the sums; false (in every thread) if a length is out of range.  A thread takes a
+// contiguous part of the requests.  off0: blocks before its first one; tokens / cells / blocks: totals.
+struct TabTotals {
+    int64_t blocks, tokens, cells;
+};
+template <int T, int B>
+__device__ inline bool scan_requests(const TabArgs& a, TabRequests<B>& s, TabTotals& all, int64_t& off0) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    uint64_t nb[kTabPer], nt[kTabPer], nc[kTabPer], sum[3] = {0, 0, 0};
+    const int per = B <= T ? 1 : (a.B + T - 1) / T, r0 = tid * per, r1 = min(a.B, r0 + per);
+    uint64_t sum[3] = {0, 0, 0}, before[3];
     int bad = 0;
-#pragma unroll
-    for (int i = 0; i < kTabPer; ++i) {
-        const int r = tid * kTabPer + i;
-        nb[i] = nt[i] = nc[i] = 0;
-        if (r < a.B) {
-            const int32_t ctx = a.ctx[r], n = a.fresh[r];
-            const int64_t blocks = ((int64_t)ctx + a.bs - 1) / a.bs;
-            if (ctx < 0 || n < 0 || n > ctx || blocks > a.max_blocks) {
-                bad = 1;
-            } else {
-                nb[i] = (uint64_t)blocks;
-                nt[i] = (uint64_t)n;
-                nc[i] = n > 0 ? (uint64_t)(blocks - (ctx - n) / a.bs) : 0;
-                s.first[r] = ctx - n;
-            }
-        }
-        sum[0] += nb[i];
-        sum[1] += nt[i];
-        sum[2] += nc[i];
+    for (int r = r0; r < r1; ++r) {
+        const int32_t ctx = a.ctx[r], n = a.fresh[r];
+        const int64_t blocks = ((int64_t)ctx + (1 << a.shift) - 1) >> a.shift;
+        const bool no = ctx < 0 || n < 0 || n > ctx || blocks > a.max_blocks;
+        const int32_t cells = no || n == 0 ? 0 : (int32_t)(blocks - ((ctx - n) >> a.shift));
+        bad |= no;
+        s.first[r] = ctx - n;
+        s.tok[r] = no ? 0 : n;
+        s.cell[r] = cells;
+        sum[0] += no ? 0 : (uint64_t)blocks;
+        sum[1] += no ? 0 : (uint64_t)n;
+        sum[2] += (uint64_t)cells;
     }
-    uint64_t before[3];
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
-        uint64_t all;
-        before[k] = wave_sum_before(sum[k], all);
-        if (lane == 0) s.wave[k][wave] = all;
+        uint64_t w;
+        before[k] = wave_sum_before(sum[k], w);
+        if (lane == 0) s.wave[k][wave] = w;
     }
     bad = __syncthreads_or(bad);
     uint64_t total[3] = {0, 0, 0};
 #pragma unroll
     for (int k = 0; k < 3; ++k)
-        for (int w = 0; w < kTabWaves; ++w) {
+#pragma unroll
+        for (int w = 0; w < T / kWave; ++w) {
             if (w == wave) before[k] += total[k];
             total[k] += s.wave[k][w];
         }
-    if ((int64_t)total[1] > a.max_tokens) bad = 1;  // the same in every thread
-    tokens = (int64_t)total[1];
-    cells = (int64_t)total[2];
-    if (!bad) {
-#pragma unroll
-        for (int i = 0; i < kTabPer; ++i) {
-            const int r = tid * kTabPer + i;
-            if (off) off[i] = (int64_t)before[0];
-            if (r < a.B) {
-                s.tok[r] = (int32_t)before[1];
-                s.cell[r] = (int32_t)before[2];
-            }
-            before[0] += nb[i];
-            before[1] += nt[i];
-            before[2] += nc[i];
+    all.blocks = (int64_t)total[0];
+    all.tokens = (int64_t)total[1];
+    all.cells = (int64_t)total[2];
+    off0 = (int64_t)before[0];
+    if (all.tokens > a.max_tokens) bad = 1;  // the same in every thread
+    if (!bad) {  // counts to sums
+        for (int r = r0; r < r1; ++r) {
+            const int32_t n = s.tok[r], c = s.cell[r];
+            s.tok[r] = (int32_t)before[1];
+            s.cell[r] = (int32_t)before[2];
+            before[1] += (uint64_t)n;
+            before[2] += (uint64_t)c;
         }
         if (tid == 0) {
-            s.tok[a.B] = (int32_t)tokens;
-            s.cell[a.B] = (int32_t)cells;
+            s.tok[a.B] = (int32_t)all.tokens;
+            s.cell[a.B] = (int32_t)all.cells;
         }
     }
-    if (off) off[kTabPer] = (int64_t)total[0];
     __syncthreads();
     return !bad;
 }
 
 // Writes the block and token offsets (all zero unless ok).
-__device__ inline void write_offsets(const TabArgs& a, const TabShared& s, const int64_t* off, bool ok) {
+template <int T, int B>
+__device__ inline void write_offsets(const TabArgs& a, const TabRequests<B>& s, const TabTotals& all, int64_t off0,
+                                     bool ok) {
     const int tid = threadIdx.x;
-#pragma unroll
-    for (int i = 0; i < kTabPer; ++i) {
-        const int r = tid * kTabPer + i;
-        if (r < a.B) {
-            a.blk_off[r] = ok ? off[i] : 0;
-            a.tok_off[r] = ok ? s.tok[r] : 0;
-        }
+    const int per = B <= T ? 1 : (a.B + T - 1) / T, r0 = tid * per, r1 = min(a.B, r0 + per);
+    for (int r = r0; r < r1; ++r) {
+        a.blk_off[r] = ok ? off0 : 0;
+        a.tok_off[r] = ok ? s.tok[r] : 0;
+        if (ok) off0 += ((int64_t)s.first[r] + (s.tok[r + 1] - s.tok[r]) + (1 << a.shift) - 1) >> a.shift;
     }
     if (tid == 0) {
-        a.blk_off[a.B] = ok ? off[kTabPer] : 0;
-        a.tok_off[a.B] = ok ? s.tok[a.B] : 0;
+        a.blk_off[a.B] = ok ? all.blocks : 0;
+        a.tok_off[a.B] = ok ? (int32_t)all.tokens : 0;
     }
 }
 
@@ -157,25 +150,28 @@ __device__ inline int request_of(const int32_t* at, int B, int32_t i) {
     return lo;
 }
 
-// Cell c: its request, block and table entry; bad: the entry is none, or a block whose first tokens are in no slot.
+// Cell c: its place in the table and its entry there; bad: the entry is none, or a block whose first tokens are in
+// no slot.  Its tokens: the t-th of the block is new token g + t for t in lo .. hi - 1.
 struct Cell {
-    int r;
-    int32_t j, entry;
+    size_t at;
+    int32_t entry, g, p;
+    int16_t lo, hi;
     bool bad;
 };
-__device__ inline Cell load_cell(const TabArgs& a, const TabShared& s, int32_t c) {
+template <int B>
+__device__ inline Cell load_cell(const TabArgs& a, const TabRequests<B>& s, int32_t c) {
     Cell x;
-    x.r = request_of(s.cell, a.B, c);
-    const int32_t j0 = s.first[x.r] / a.bs;
-    x.j = j0 + (c - s.cell[x.r]);
-    x.entry = a.table[(size_t)x.r * a.max_blocks + x.j];
-    x.bad = x.entry < -1 || x.entry >= a.n_slots || (x.entry < 0 && x.j == j0 && s.first[x.r] % a.bs != 0);
+    const int r = request_of(s.cell, a.B, c);
+    const int32_t first = s.first[r], n = s.tok[r + 1] - s.tok[r], mask = (1 << a.shift) - 1;
+    const int32_t j = (first >> a.shift) + (c - s.cell[r]);
+    x.at = (size_t)r * a.max_blocks + j;
+    x.entry = a.table[x.at];
+    x.p = j << a.shift;  // below the context length, which fits
+    x.g = s.tok[r] + (x.p - first);
+    x.lo = (int16_t)max(0, first - x.p);
+    x.hi = (int16_t)min((int64_t)mask + 1, (int64_t)first + n - x.p);
+    x.bad = x.entry < -1 || x.entry >= a.n_slots || (x.entry < 0 && x.lo > 0);
     return x;
-}
-
-__device__ inline void fill_token(const TabArgs& a, int64_t i, int32_t slot, int32_t p) {
-    a.slot_map[i] = (int64_t)slot * a.bs + p % a.bs;
-    a.positions[i] = p;
 }
 
 __device__ inline void fill_rest(const TabArgs& a, int64_t from, int64_t at, int64_t stride) {
@@ -185,140 +181,172 @@ __device__ inline void fill_rest(const TabArgs& a, int64_t from, int64_t at, int
     }
 }
 
-// Rank of this thread's cell among the workgroup's cells without a slot, and their number.
-__device__ inline uint32_t rank_misses(TabShared& s, bool miss, uint32_t& all) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint64_t m = __ballot(miss);
-    if (lane == 0) s.misses[wave] = (uint32_t)__popcll(m);
-    __syncthreads();
-    uint32_t before = (uint32_t)__popcll(m & ((1ull << lane) - 1));
-    all = 0;
-    for (int w = 0; w < kTabWaves; ++w) {
-        if (w == wave) before += all;
-        all += s.misses[w];
+// What the tokens of a cell need, in LDS.
+template <int N>
+struct CellTokens {
+    int32_t slot[N], g[N], p[N];
+    int32_t range[N];  // lo | hi << 16
+};
+template <int N>
+__device__ inline void keep_cell(CellTokens<N>& s, int i, const Cell& x, int32_t slot) {
+    s.slot[i] = slot;
+    s.g[i] = x.g;
+    s.p[i] = x.p;
+    s.range[i] = (int32_t)x.lo | (int32_t)x.hi << 16;
+}
+// Maps of the tokens of n cells, neighbouring threads on neighbouring tokens.
+template <int T, int N>
+__device__ inline void fill_tokens(const TabArgs& a, const CellTokens<N>& s, int n) {
+    for (int i = threadIdx.x; i < n << a.shift; i += T) {
+        const int c = i >> a.shift, t = i & ((1 << a.shift) - 1);
+        const int32_t range = s.range[c];
+        if (t < (range & 0xFFFF) || t >= range >> 16) continue;
+        a.slot_map[s.g[c] + t] = ((int64_t)s.slot[c] << a.shift) + t;
+        a.positions[s.g[c] + t] = s.p[c] + t;
     }
-    __syncthreads();
-    return before;
 }
 
-__global__ __launch_bounds__(kTabThreads) void tables_small_kernel(TabArgs a) {
-    __shared__ TabShared s;
-    const int tid = threadIdx.x;
+// One workgroup of T threads: up to T * kCellsPer cells, B requests.
+template <int T, int B>
+__global__ __launch_bounds__(T) void tables_one_kernel(TabArgs a) {
+    constexpr int kWaves = T / kWave;
+    __shared__ TabRequests<B> s;
+    __shared__ CellTokens<T * kCellsPer> tokens;
+    __shared__ int32_t free_list[T * kCellsPer];
+    __shared__ uint32_t miss_of[kWave];  // [kCellsPer][kWaves] counts of cells without a slot
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int32_t head = *a.free_head;
-    int64_t tokens, cells, off[kTabPer + 1];
-    bool ok = scan_requests(a, s, tokens, cells, off);
-    int32_t code = ok ? PULSE_OK : PULSE_ERR_BAD_INDEX;
-    if (ok) {
-        int64_t total = 0;
-        int bad = 0;
-        for (int64_t c0 = 0; c0 < cells; c0 += kTabThreads) {
-            bool miss = false;
-            if (c0 + tid < cells) {
-                const Cell x = load_cell(a, s, (int32_t)(c0 + tid));
-                bad |= x.bad;
-                miss = x.entry < 0;
-            }
-            total += __syncthreads_count(miss);
-        }
-        const bool head_ok = head >= 0 && head <= a.n_free;
-        const bool fits = head_ok && total <= (int64_t)a.n_free - head;
-        if (fits)
-            for (int64_t g = tid; g < total; g += kTabThreads)
-                bad |= (uint32_t)a.free_slots[head + g] >= (uint32_t)a.n_slots;
-        bad = __syncthreads_or(bad);
-        if (bad || !head_ok) code = PULSE_ERR_BAD_INDEX;
-        else if (!fits) code = PULSE_ERR_POOL_EXHAUSTED;
-        ok = code == PULSE_OK;
-        if (ok) {
-            int32_t g0 = head;
-            for (int64_t c0 = 0; c0 < cells; c0 += kTabThreads) {
-                Cell x;
-                x.entry = 0;
-                if (c0 + tid < cells) x = load_cell(a, s, (int32_t)(c0 + tid));
-                uint32_t all;
-                const uint32_t rank = rank_misses(s, x.entry < 0, all);
-                if (x.entry < 0) a.table[(size_t)x.r * a.max_blocks + x.j] = a.free_slots[g0 + (int32_t)rank];
-                g0 += (int32_t)all;
-            }
-            if (tid == 0) *a.free_head = g0;
-        }
-    }
-    if (tid == 0 && code != PULSE_OK) report(a.status, code);
-    write_offsets(a, s, off, ok);
-    if (!ok) tokens = 0;
-    __syncthreads();  // the table entries above
-    for (int64_t i = tid; i < tokens; i += kTabThreads) {
-        const int r = request_of(s.tok, a.B, (int32_t)i);
-        const int32_t p = s.first[r] + (int32_t)(i - s.tok[r]);
-        fill_token(a, i, a.table[(size_t)r * a.max_blocks + p / a.bs], p);
-    }
-    fill_rest(a, tokens, tid, kTabThreads);
-}
-
-__global__ __launch_bounds__(kTabThreads) void tables_count_kernel(TabArgs a, TabScratch w) {
-    __shared__ TabShared s;
-    const int tid = threadIdx.x, tile = blockIdx.x;
-    const int32_t head = *a.free_head;
-    int64_t tokens, cells;
-    const bool ok = scan_requests(a, s, tokens, cells, nullptr);
-    if (tile == 0 && tid == 0) *w.head = head;
-    int n = 0, bad = 0;
-    int32_t place = INT32_MAX;
-    if (ok) {
+    const bool head_ok = head >= 0 && head <= a.n_free;
+    // the slots that the step could take; they do not wait for the lengths
+    const int64_t left = head_ok ? (int64_t)a.n_free - head : 0;
 #pragma unroll
-        for (int k = 0; k < kTilePer; ++k) {
-            const int64_t c = (int64_t)tile * kTileCells + k * kTabThreads + tid;
-            bool miss = false;
-            if (c < cells) {
-                const Cell x = load_cell(a, s, (int32_t)c);
-                bad |= x.bad;
-                miss = x.entry < 0;
-                if (head >= 0 && c < (int64_t)a.n_free - head &&
-                    (uint32_t)a.free_slots[head + c] >= (uint32_t)a.n_slots && place == INT32_MAX)
-                    place = (int32_t)c;
-            }
-            n += __syncthreads_count(miss);
+    for (int k = 0; k < kCellsPer; ++k) {
+        const int g = k * T + tid;
+        free_list[g] = g < left ? a.free_slots[head + g] : -1;
+    }
+    if (tid < kWave) miss_of[tid] = 0;
+    TabTotals all;
+    int64_t off0;
+    bool ok = scan_requests<T, B>(a, s, all, off0);
+    const int cells = ok ? (int)all.cells : 0;
+    Cell x[kCellsPer];
+    uint64_t misses[kCellsPer];
+    int bad = 0;
+#pragma unroll
+    for (int k = 0; k < kCellsPer; ++k) {
+        const int c = k * T + tid;
+        x[k].entry = 0;
+        if (c < cells) {
+            x[k] = load_cell(a, s, c);
+            bad |= x[k].bad;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kCellsPer; ++k) {
+        misses[k] = __ballot(x[k].entry < 0);
+        if (lane == 0) miss_of[k * kWaves + wave] = (uint32_t)__popcll(misses[k]);
+    }
+    bad = __syncthreads_or(bad);
+    const uint32_t sums = wave_scan(miss_of[lane], 0u, OpAdd());
+    const int total = (int)last_lane(sums);
+    const bool fits = total <= left;
+    int32_t slot[kCellsPer];
+#pragma unroll
+    for (int k = 0; k < kCellsPer; ++k) {
+        const int i = k * kWaves + wave;
+        const uint32_t before = i > 0 ? (uint32_t)__builtin_amdgcn_readlane((int)sums, max(0, i - 1)) : 0u;
+        slot[k] = x[k].entry;
+        if (slot[k] < 0) {
+            slot[k] = free_list[before + (uint32_t)__popcll(misses[k] & ((1ull << lane) - 1))];
+            if (fits && (uint32_t)slot[k] >= (uint32_t)a.n_slots) bad = 1;
         }
     }
     bad = __syncthreads_or(bad);
-    // the least place over the workgroup
-    const uint32_t m = last_lane(wave_scan((uint32_t)place, 0xFFFFFFFFu, OpMin()));
-    if ((tid & 63) == 0) s.misses[tid >> 6] = m;
+    int32_t code = PULSE_OK;
+    if (!ok || !head_ok || bad) code = PULSE_ERR_BAD_INDEX;
+    else if (!fits) code = PULSE_ERR_POOL_EXHAUSTED;
+    ok = code == PULSE_OK;
+    write_offsets<T, B>(a, s, all, off0, ok);
+    fill_rest(a, ok ? all.tokens : 0, tid, T);
+    if (!ok) {
+        if (tid == 0) report(a.status, code);
+        return;
+    }
+    if (tid == 0 && total > 0) *a.free_head = head + total;
+#pragma unroll
+    for (int k = 0; k < kCellsPer; ++k) {
+        const int c = k * T + tid;
+        if (c >= cells) continue;
+        if (x[k].entry < 0) a.table[x[k].at] = slot[k];
+        keep_cell(tokens, c, x[k], slot[k]);
+    }
+    __syncthreads();
+    fill_tokens<T>(a, tokens, cells);
+}
+
+__global__ __launch_bounds__(kTileThreads) void tables_count_kernel(TabArgs a, TabScratch w) {
+    __shared__ TabRequests<kMaxBatch> s;
+    __shared__ int32_t s_count, s_bad, s_place;
+    const int tid = threadIdx.x, tile = blockIdx.x;
+    const int32_t head = *a.free_head;
+    if (tid == 0) {
+        s_count = s_bad = 0;
+        s_place = INT32_MAX;
+        if (tile == 0) *w.head = head;
+    }
+    TabTotals all;
+    int64_t off0;
+    int n = 0, bad = 0;
+    int32_t place = INT32_MAX;
+    if (scan_requests<kTileThreads, kMaxBatch>(a, s, all, off0)) {
+        const int64_t c1 = min(all.cells, (int64_t)(tile + 1) * w.tile);
+        for (int64_t c = (int64_t)tile * w.tile + tid; c < c1; c += kTileThreads) {
+            // the c-th place of the free list may be taken if there are c cells without a slot before it
+            const int32_t f = head >= 0 && c < (int64_t)a.n_free - head ? a.free_slots[head + c] : 0;
+            const Cell x = load_cell(a, s, (int32_t)c);
+            bad |= x.bad;
+            n += x.entry < 0;
+            if ((uint32_t)f >= (uint32_t)a.n_slots) place = min(place, (int32_t)c);
+        }
+    }
+    if (n) atomicAdd(&s_count, n);
+    if (bad) atomicOr(&s_bad, 1);
+    if (place != INT32_MAX) atomicMin(&s_place, place);
     __syncthreads();
     if (tid == 0) {
-        uint32_t least = s.misses[0];
-        for (int i = 1; i < kTabWaves; ++i) least = min(least, s.misses[i]);
-        w.count[tile] = bad ? -1 : n;
-        w.bad_place[tile] = (int32_t)least;
+        w.count[tile] = s_bad ? -1 : s_count;
+        w.bad_place[tile] = s_place;
     }
 }
 
-__global__ __launch_bounds__(kTabThreads) void tables_fill_kernel(TabArgs a, TabScratch w) {
-    __shared__ TabShared s;
-    __shared__ int32_t slot[kTileCells];
+__global__ __launch_bounds__(kTileThreads) void tables_fill_kernel(TabArgs a, TabScratch w) {
+    constexpr int kWaves = kTileThreads / kWave;
+    __shared__ TabRequests<kMaxBatch> s;
+    __shared__ CellTokens<kTileThreads> tokens;
+    __shared__ uint32_t miss_of[kWaves];
     __shared__ int32_t s_before, s_total, s_place, s_bad;
-    const int tid = threadIdx.x, tile = blockIdx.x, tiles = gridDim.x;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, tile = blockIdx.x, tiles = gridDim.x;
     const int32_t head = *w.head;
     if (tid == 0) {
         s_before = s_total = s_bad = 0;
         s_place = INT32_MAX;
     }
-    int64_t tokens, cells, off[kTabPer + 1];
-    bool ok = scan_requests(a, s, tokens, cells, off);
     int32_t before = 0, total = 0, place = INT32_MAX, bad = 0;
-    for (int t = tid; t < tiles; t += kTabThreads) {
+    for (int t = tid; t < tiles; t += kTileThreads) {
         const int32_t n = w.count[t];
         bad |= n < 0;
         total += n;
         before += t < tile ? n : 0;
         place = min(place, w.bad_place[t]);
     }
+    TabTotals all;
+    int64_t off0;
+    bool ok = scan_requests<kTileThreads, kMaxBatch>(a, s, all, off0);
     if (total) atomicAdd(&s_total, total);
     if (before) atomicAdd(&s_before, before);
     if (place != INT32_MAX) atomicMin(&s_place, place);
     if (bad) atomicOr(&s_bad, 1);
     __syncthreads();
-    before = s_before;
     total = s_total;
     int32_t code = PULSE_OK;
     if (!ok || s_bad || head < 0 || head > a.n_free) code = PULSE_ERR_BAD_INDEX;
@@ -326,70 +354,73 @@ __global__ __launch_bounds__(kTabThreads) void tables_fill_kernel(TabArgs a, Tab
     else if (s_place < total) code = PULSE_ERR_BAD_INDEX;
     ok = code == PULSE_OK;
     if (tile == 0) {
-        write_offsets(a, s, off, ok);
+        write_offsets<kTileThreads, kMaxBatch>(a, s, all, off0, ok);
         if (tid == 0) {
             if (ok) *a.free_head = head + total;
             else report(a.status, code);
         }
     }
-    const int64_t at = (int64_t)tile * kTabThreads + tid, stride = (int64_t)tiles * kTabThreads;
-    fill_rest(a, ok ? tokens : 0, at, stride);
+    fill_rest(a, ok ? all.tokens : 0, (int64_t)tile * kTileThreads + tid, (int64_t)tiles * kTileThreads);
     if (!ok) return;
-    int32_t g0 = head + before;
-    const int64_t c0 = (int64_t)tile * kTileCells;
-    const int n = (int)max((int64_t)0, min((int64_t)kTileCells, cells - c0));
-#pragma unroll
-    for (int k = 0; k < kTilePer; ++k) {
-        const int c = k * kTabThreads + tid;
+    int32_t g0 = head + s_before;
+    const int64_t c1 = min(all.cells, (int64_t)(tile + 1) * w.tile);
+    for (int64_t c0 = (int64_t)tile * w.tile; c0 < c1; c0 += kTileThreads) {
+        const int64_t c = c0 + tid;
         Cell x;
         x.entry = 0;
-        if (c < n) x = load_cell(a, s, (int32_t)(c0 + c));
-        uint32_t all;
-        const uint32_t rank = rank_misses(s, x.entry < 0, all);
-        if (x.entry < 0) {
-            x.entry = a.free_slots[g0 + (int32_t)rank];
-            a.table[(size_t)x.r * a.max_blocks + x.j] = x.entry;
+        if (c < c1) x = load_cell(a, s, (int32_t)c);
+        const uint64_t m = __ballot(x.entry < 0);
+        if (lane == 0) miss_of[wave] = (uint32_t)__popcll(m);
+        __syncthreads();
+        int32_t g = g0 + __popcll(m & ((1ull << lane) - 1));
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+            g += i < wave ? (int32_t)miss_of[i] : 0;
+            g0 += (int32_t)miss_of[i];
         }
-        if (c < n) slot[c] = x.entry;
-        g0 += (int32_t)all;
-    }
-    __syncthreads();
-    // the tile's tokens, neighbouring threads on neighbouring tokens
-    for (int i = tid; i < n * a.bs; i += kTabThreads) {
-        const int c = i / a.bs;
-        const int r = request_of(s.cell, a.B, (int32_t)(c0 + c));
-        const int32_t first = s.first[r];
-        const int64_t p = ((int64_t)first / a.bs + (c0 + c - s.cell[r])) * a.bs + i % a.bs;
-        const int32_t k = s.tok[r + 1] - s.tok[r];
-        if (p >= first && p < (int64_t)first + k) fill_token(a, s.tok[r] + (p - first), slot[c], (int32_t)p);
+        if (c < c1) {
+            int32_t slot = x.entry;
+            if (slot < 0) a.table[x.at] = slot = a.free_slots[g];
+            keep_cell(tokens, tid, x, slot);
+        }
+        __syncthreads();
+        fill_tokens<kTileThreads>(a, tokens, (int)min((int64_t)kTileThreads, c1 - c0));
+        __syncthreads();
     }
 }
 
 // Bound on the cells of a step: a request's new tokens lie in at most two blocks more than they fill.
 static int64_t cell_bound(int32_t B, int32_t bs, int64_t max_tokens) { return max_tokens / bs + 2 * (int64_t)B; }
-static int64_t tile_count(int32_t B, int32_t bs, int64_t max_tokens) {
-    return (cell_bound(B, bs, max_tokens) + kTileCells - 1) / kTileCells;
+// Cells of a tile: kTileThreads, or the multiple of them that keeps the tiles few.
+static int64_t tile_cells(int64_t cells) {
+    return kTileThreads * ((cells + kTileThreads * kMaxTiles - 1) / (kTileThreads * kMaxTiles));
 }
 
 size_t tables_ws_bytes(int32_t B, int32_t bs, int64_t max_tokens) {
-    return (sizeof(int32_t) * (size_t)(1 + 2 * tile_count(B, bs, max_tokens)) + 255) & ~(size_t)255;
+    const int64_t cells = cell_bound(B, bs, max_tokens);
+    const int64_t tiles = cells > 0 ? (cells + tile_cells(cells) - 1) / tile_cells(cells) : 0;
+    return (sizeof(int32_t) * (size_t)(1 + 2 * tiles) + 255) & ~(size_t)255;
 }
 
 hipError_t launch_tables(const int32_t* ctx, const int32_t* fresh, int32_t B, int32_t bs, int32_t* table,
                          int32_t max_blocks, const int32_t* free_slots, int32_t* free_head, int32_t n_free,
                          int32_t n_slots, int64_t* blk_off, int32_t* tok_off, int64_t* slot_map, int32_t* positions,
                          int64_t max_tokens, int32_t* status, void* ws, hipStream_t st) {
-    const TabArgs a{ctx,     fresh,   B,       bs,       table,     max_blocks, free_slots, free_head,
+    const int32_t shift = bs == 16 ? 4 : bs == 32 ? 5 : 6;
+    const TabArgs a{ctx,     fresh,   B,       shift,    table,     max_blocks, free_slots, free_head,
                     n_free,  n_slots, blk_off, tok_off,  slot_map,  positions,  max_tokens, status};
-    if (cell_bound(B, bs, max_tokens) <= kOneGroupCells) {
-        hipLaunchKernelGGL(tables_small_kernel, dim3(1), dim3(kTabThreads), 0, st, a);
-        return hipGetLastError();
+    const int64_t cells = cell_bound(B, bs, max_tokens);
+    if (B <= 256 && cells <= 256 * kCellsPer) {
+        hipLaunchKernelGGL((tables_one_kernel<256, 256>), dim3(1), dim3(256), 0, st, a);
+    } else if (cells <= 1024 * kCellsPer) {
+        hipLaunchKernelGGL((tables_one_kernel<1024, kMaxBatch>), dim3(1), dim3(1024), 0, st, a);
+    } else {
+        const int64_t tile = tile_cells(cells), tiles = (cells + tile - 1) / tile;
+        int32_t* w = static_cast<int32_t*>(ws);
+        const TabScratch sc{w, w + 1, w + 1 + tiles, (int32_t)tile};
+        hipLaunchKernelGGL(tables_count_kernel, dim3((unsigned)tiles), dim3(kTileThreads), 0, st, a, sc);
+        hipLaunchKernelGGL(tables_fill_kernel, dim3((unsigned)tiles), dim3(kTileThreads), 0, st, a, sc);
     }
-    const int64_t tiles = tile_count(B, bs, max_tokens);
-    int32_t* w = static_cast<int32_t*>(ws);
-    const TabScratch sc{w, w + 1, w + 1 + tiles};
-    hipLaunchKernelGGL(tables_count_kernel, dim3((unsigned)tiles), dim3(kTabThreads), 0, st, a, sc);
-    hipLaunchKernelGGL(tables_fill_kernel, dim3((unsigned)tiles), dim3(kTabThreads), 0, st, a, sc);
     return hipGetLastError();
 }
 

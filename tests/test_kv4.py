@@ -367,3 +367,25 @@ def test_plain_form_packs_what_it_unpacks():
         top = kv.double().unflatten(-1, (4, 32)).abs().amax(-1, keepdim=True)
         err = (torch.stack([k, v]) - kv.double()).unflatten(-1, (4, 32)).abs()
         assert (err <= top / 3.5).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale", [0.0, -0.1, 3.0])
+def test_any_scale(scale):
+    ctx, cnt = [200, 77], [13, 5]
+    gen = torch.Generator().manual_seed(8)
+    sh, q, pool, table, sel = case_state(ctx, cnt, 4, 2, 16, "bf16", gen)
+    d = [x.to(DEV) for x in (q, pool, table, sel)]
+    out, lse = torch.zeros((2, 4, D), device=DEV), torch.zeros((2, 4), device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    nb = P.pulse_workspace_bytes(sh, 2, 13, 0)
+    ws = torch.zeros(nb, dtype=torch.uint8, device=DEV)
+    P.pulse_sparse_decode_attn(sh, d[0], d[1], pool.shape[0], d[2], table.shape[1], d[3], dev(cnt), 13, dev(ctx), 2, scale,
+                               out, lse, status, ws, nb)
+    assert status.item() == 0
+    for r in range(2):
+        j = sel[r, : cnt[r]].long()
+        k, v = (x.transpose(0, 1).reshape(2, -1, D) for x in plain64.unpack(pool[table[r, j].long()], 2, 16))
+        n = (j[:, None] * 16 + torch.arange(16)).view(-1) < ctx[r]
+        check_attention(out[r], lse[r], *plain64.attention(q[r] * (-1 if scale < 0 else 1), k[:, n], v[:, n], abs(scale)),
+                        int(n.sum()))
