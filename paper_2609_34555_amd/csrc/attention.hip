@@ -36,6 +36,10 @@ namespace pulse {
 #ifndef PULSE_ATTN_TARGET_WAVES
 #define PULSE_ATTN_TARGET_WAVES 2048
 #endif
+// Steps of a wave up to which one workgroup takes a whole request and head of a 4-bit cache, so that no merge
+// launch follows.  In us, split as far as 2048 waves go and kept together: 272 tokens 9.9 and 7.6, 400 9.9 and 8.7,
+// 600 9.9 and 9.9 (16 requests of them 12.7 and 11.0), 1040 (five steps) 10.0 and 12.2.
+constexpr int kKv4OneSteps = 4;
 constexpr int kCombineThreads = kHeadDim;
 
 // Waves per workgroup (attn_waves): 8 while the LDS merge buffer (waves x G x
@@ -44,7 +48,13 @@ constexpr int kCombineThreads = kHeadDim;
 
 // Entries of one 32-token step, and of the shortest split.
 static int32_t split_step(int32_t bs) { return bs >= kChunkTokens ? 1 : kChunkTokens / bs; }
-static int32_t split_least(int32_t bs) { return bs >= 2 * kChunkTokens ? 1 : 2 * kChunkTokens / bs; }
+// Two steps, one of a 4-bit cache (a quarter of the bytes, and twice the shortest split's work to share out: 64
+// requests of 80 tokens 10.1 and 9.0 us with two and one).
+static int32_t split_least(const pulse_shape& s) {
+    const int t = (is_kv4(s.dtype) ? 1 : 2) * kChunkTokens;
+    return s.block_size >= t ? 1 : t / s.block_size;
+}
+int attn_waves(const pulse_shape& s) { return s.num_q_heads / s.num_kv_heads <= 8 ? 8 : 4; }
 
 struct SplitArgs {
     int32_t eps, n_wg;    // host plan: entries per wave, workgroups per (request, KV head)
@@ -312,12 +322,21 @@ __device__ inline void attend_split(const uint16_t* __restrict__ q, const uint16
 // were 1.4e-6 off, with three 4e-7, as a computation in fp32 is.
 // Row 4 * grp + v of acc[t] is query head (4 * grp + v) % GP of group (4 * grp + v) / GP of the tile's set.
 template <int GP>
-struct Kv4Step {
-    u32x4 k[2];            // codes of a key's 32 channels, tokens of both sub-tiles
-    uint32_t ks[2];        // their scale bytes
-    u32x4 v[2];            // codes of 8 tokens, channel tiles 0..3 and 4..7
-    u32x2 vs[GP / 4];      // scale bytes of 8 tokens
+struct Kv4Values {
+    u32x4 v[2];        // codes of 8 tokens, channel tiles 0..3 and 4..7
+    u32x2 vs[GP / 4];  // scale bytes of 8 tokens
 };
+
+// 2^e of byte N of a word of scale bytes.
+template <int N>
+__device__ inline float kv4_scale_of(uint32_t w) {
+    uint32_t u;
+    if constexpr (N == 0) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_0" : "=v"(u) : "v"(23), "v"(w));
+    if constexpr (N == 1) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_1" : "=v"(u) : "v"(23), "v"(w));
+    if constexpr (N == 2) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_2" : "=v"(u) : "v"(23), "v"(w));
+    if constexpr (N == 3) u = (w >> 1) & 0x7F800000u;
+    return __uint_as_float(u);
+}
 
 template <int DT, int BS, int GP>
 __device__ inline void attend_split_kv4(const uint16_t* __restrict__ q, const uint8_t* __restrict__ pool,
@@ -367,80 +386,91 @@ __device__ inline void attend_split_kv4(const uint16_t* __restrict__ q, const ui
         }
         scale_log2 = fmaxf(fabsf(scale_log2), 1e-30f);
     }
+    // Step i covers tokens 32 i ..: entry and row of a lane's tokens.  K: MFMA row m = col is token
+    // 8 * (col / 4) + 4 * sub + col % 4; V: lane group grp holds tokens 8 * grp .. + 7, channels col + 16 * t in word t.
+    constexpr int kPer = BS >= kChunkTokens ? 1 : kChunkTokens / BS;  // entries of a step
+    constexpr int kHalves = BS > kChunkTokens ? BS / kChunkTokens : 1;  // steps of an entry
     const uint32_t E = (uint32_t)Hkv * kv4_head_bytes(BS);
     const uint8_t* head = pool + (size_t)h * kv4_head_bytes(BS);
-    const int tokens = ne * BS;
+    const int k_tok = 8 * (col >> 2), v_tok = 8 * grp;
+    const uint8_t* k_at = head + (k_tok % BS + (col & 3)) * 64 + grp * 16;
+    const uint8_t* ks_at = head + kv4_key_scales(BS) + (k_tok % BS + (col & 3)) * kGroups + grp;
+    const uint8_t* v_at = head + kv4_values(BS) + v_tok % BS * 64 + col * 32;
+    const uint8_t* vs_at = head + kv4_value_scales(BS) + col / GP * BS + v_tok % BS;
+    const int steps = (ne * BS + kChunkTokens - 1) / kChunkTokens;
 
-    auto load = [&](int t0, Kv4Step<GP>& x) {
-        // K: MFMA row m = col is token 8 * (col / 4) + 4 * sub + col % 4
-        const int k_seq = t0 + 8 * (col >> 2);
-        const uint8_t* kb = head + (size_t)(uint32_t)__shfl(my_slot, k_seq / BS) * E;
-        const int k_row = k_seq % BS + (col & 3);
+    u32x4 kw[2];
+    uint32_t ksb[2];
+    Kv4Values<GP> vnext;
+    auto load_k = [&](int i) {
+        const uint32_t slot = (uint32_t)__shfl(my_slot, i / kHalves * kPer + k_tok / BS);
+        const int half = i % kHalves * kChunkTokens;
+        const uint8_t* kb = k_at + (uint64_t)slot * E + half * 64;
+        const uint8_t* sb = ks_at + (uint64_t)slot * E + half * kGroups;
 #pragma unroll
         for (int sub = 0; sub < 2; ++sub) {
-            x.k[sub] = *reinterpret_cast<const u32x4*>(kb + (k_row + 4 * sub) * 64 + grp * 16);
-            x.ks[sub] = kb[kv4_key_scales(BS) + (k_row + 4 * sub) * kGroups + grp];
+            kw[sub] = *reinterpret_cast<const u32x4*>(kb + 4 * sub * 64);
+            ksb[sub] = sb[4 * sub * kGroups];
         }
-        // V: lane group grp holds tokens 8 * grp .. + 7, channels col + 16 * t in word t
-        const int v_seq = t0 + 8 * grp;
-        const uint8_t* vb = head + (size_t)(uint32_t)__shfl(my_slot, v_seq / BS) * E;
-        const int v_row = v_seq % BS;
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            x.v[i] = reinterpret_cast<const u32x4*>(vb + kv4_values(BS) + v_row * 64 + col * 32)[i];
-#pragma unroll
-        for (int k = 0; k < kSets; ++k)
-            x.vs[k] = *reinterpret_cast<const u32x2*>(vb + kv4_value_scales(BS) + (k * (16 / GP) + col / GP) * BS + v_row);
     };
-
-    Kv4Step<GP> next;
-    load(0, next);
+    auto load_v = [&](int i) {
+        const uint32_t slot = (uint32_t)__shfl(my_slot, i / kHalves * kPer + v_tok / BS);
+        const int half = i % kHalves * kChunkTokens;
+        const uint8_t* vb = v_at + (uint64_t)slot * E + half * 64;
+        const uint8_t* sb = vs_at + (uint64_t)slot * E + half;
+#pragma unroll
+        for (int n = 0; n < 2; ++n) vnext.v[n] = reinterpret_cast<const u32x4*>(vb)[n];
+#pragma unroll
+        for (int k = 0; k < kSets; ++k) vnext.vs[k] = *reinterpret_cast<const u32x2*>(sb + k * (16 / GP) * BS);
+    };
+    load_k(0);
+    load_v(0);
 #pragma unroll 1
-    for (int t0 = 0; t0 < tokens; t0 += kChunkTokens) {
-        Kv4Step<GP> now = next;
-        if (t0 + kChunkTokens < tokens) load(t0 + kChunkTokens, next);
+    for (int i = 0; i < steps; ++i) {
+        Kv4Values<GP> now = vnext;
         // --- S^T = K . Q^T
-        f32x4 s[2];
+        f32x4 s[2] = {};
+        const float ks[2] = {kv4_scale(ksb[0]), kv4_scale(ksb[1])};
 #pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-            const float ks = kv4_scale(now.ks[sub]);
-            s[sub] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int kc = 0; kc < 4; ++kc)
 #pragma unroll
-            for (int kc = 0; kc < 4; ++kc) s[sub] = MQ::mac(kv4_decode8<ET>(now.k[sub][kc], ks), qb[kc], s[sub]);
+            for (int sub = 0; sub < 2; ++sub) s[sub] = MQ::mac(kv4_decode8<ET>(kw[sub][kc], ks[sub]), qb[kc], s[sub]);
+        if (i + 1 < steps) {
+            load_k(i + 1);
+            load_v(i + 1);
         }
         float x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = s[i / 4][i % 4];
+        for (int n = 0; n < 8; ++n) x[n] = s[n / 4][n % 4];
         // blocks that are not whole (the last of the context, a missing one, none behind an odd count): their other
         // tokens count nothing, whatever their scale bytes are
-        constexpr uint64_t kStepEntries = BS >= kChunkTokens ? 1 : (1 << (kChunkTokens / BS)) - 1;
-        if ((~whole >> (t0 / BS)) & kStepEntries) {
-            const int v_seq = t0 + 8 * grp;
-            const int left = __shfl(my_nv, v_seq / BS) - v_seq % BS;  // tokens of this lane's 8
+        if ((~whole >> (i / kHalves * kPer)) & ((1u << kPer) - 1)) {
+            // tokens of this lane's 8
+            const int left = __shfl(my_nv, i / kHalves * kPer + v_tok / BS) - v_tok % BS - i % kHalves * kChunkTokens;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (i >= left) x[i] = -INFINITY;
+            for (int n = 0; n < 8; ++n) {
+                if (n >= left) x[n] = -INFINITY;
 #pragma unroll
                 for (int k = 0; k < kSets; ++k)
-                    if (i >= left) now.vs[k][i / 4] &= ~(0xFFu << (8 * (i % 4)));
+                    if (n >= left) now.vs[k][n / 4] &= ~(0xFFu << (8 * (n % 4)));
             }
         }
         float cm = x[0];
 #pragma unroll
-        for (int i = 1; i < 8; ++i) cm = fmaxf(cm, x[i]);
+        for (int n = 1; n < 8; ++n) cm = fmaxf(cm, x[n]);
         cm = across_groups(cm, [](float a, float b) { return fmaxf(a, b); });
         const float m_new = fmaxf(m_run, cm * scale_log2);
         const float m_use = m_new == -INFINITY ? 0.f : m_new;
         const float alpha = exp2_fast(m_run - m_use);
         float psum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            x[i] = exp2_fast(x[i] * scale_log2 - m_use);
-            psum += x[i];
+        for (int n = 0; n < 8; ++n) {
+            x[n] = exp2_fast(x[n] * scale_log2 - m_use);
+            psum += x[n];
         }
         l_run = l_run * alpha + psum;
         m_run = m_new;
-        if (t0 > 0 && __ballot(alpha != 1.f)) {
+        if (i > 0 && __ballot(alpha != 1.f)) {
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 const float av = __shfl(alpha, 4 * grp + v);
@@ -451,24 +481,31 @@ __device__ inline void attend_split_kv4(const uint16_t* __restrict__ q, const ui
         // --- O += P' . V
 #pragma unroll
         for (int k = 0; k < kSets; ++k) {
+            float y[8];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                y[4 * n] = x[4 * n] * kv4_scale_of<0>(now.vs[k][n]);
+                y[4 * n + 1] = x[4 * n + 1] * kv4_scale_of<1>(now.vs[k][n]);
+                y[4 * n + 2] = x[4 * n + 2] * kv4_scale_of<2>(now.vs[k][n]);
+                y[4 * n + 3] = x[4 * n + 3] * kv4_scale_of<3>(now.vs[k][n]);
+            }
             u32x4 part[3];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float a = x[2 * i] * kv4_scale(now.vs[k][i / 2] >> (16 * (i % 2)) & 0xFFu);
-                float b = x[2 * i + 1] * kv4_scale(now.vs[k][i / 2] >> (16 * (i % 2) + 8) & 0xFFu);
+            for (int n = 0; n < 4; ++n) {
+                float a = y[2 * n], b = y[2 * n + 1];
 #pragma unroll
-                for (int n = 0; n < 3; ++n) {
+                for (int m = 0; m < 3; ++m) {
                     const bf16x2 two = {(__bf16)a, (__bf16)b};
-                    part[n][i] = __builtin_bit_cast(uint32_t, two);
-                    a -= __uint_as_float(part[n][i] << 16);
-                    b -= __uint_as_float(part[n][i] & 0xFFFF0000u);
+                    part[m][n] = __builtin_bit_cast(uint32_t, two);
+                    a -= __uint_as_float(part[m][n] << 16);
+                    b -= __uint_as_float(part[m][n] & 0xFFFF0000u);
                 }
             }
 #pragma unroll
             for (int t = 8 / kSets * k; t < 8 / kSets * (k + 1); ++t) {
                 const bf16x8 v = kv4_decode8<PULSE_BF16>(now.v[t / 4][t % 4], 1.0f);
 #pragma unroll
-                for (int n = 0; n < 3; ++n) acc[t] = MP::mac(__builtin_bit_cast(bf16x8, part[n]), v, acc[t]);
+                for (int m = 0; m < 3; ++m) acc[t] = MP::mac(__builtin_bit_cast(bf16x8, part[m]), v, acc[t]);
             }
         }
     }
@@ -674,16 +711,20 @@ __global__ __launch_bounds__(kCombineThreads) void attn_combine_kernel(
             m_run == -INFINITY ? -INFINITY : (m_run + log2f(L)) * 0.69314718055994531f;
 }
 
-AttnPlan attn_plan(int32_t B, int32_t Hkv, int32_t k_max, int32_t bs) {
+AttnPlan attn_plan(const pulse_shape& s, int32_t B, int32_t k_max) {
     // a split covers whole 32-token steps, at least two, and at most 64 entries
-    const int32_t step = split_step(bs);
-    const int64_t units = (int64_t)B * Hkv;
+    const int32_t step = split_step(s.block_size);
+    const int64_t units = (int64_t)B * s.num_kv_heads;
     const int64_t target_waves = PULSE_ATTN_TARGET_WAVES;  // one round at 2 resident waves per SIMD on 256 CUs
     int64_t want = units > 0 ? (target_waves + units - 1) / units : 1;
-    const int64_t min_entries = split_least(bs);
+    const int64_t min_entries = split_least(s);
     int64_t max_split = (k_max + min_entries - 1) / min_entries;
     if (want > max_split) want = max_split;
     if (want < 1) want = 1;
+    if (is_kv4(s.dtype)) {
+        const int64_t W = attn_waves(s);
+        if (want > W && k_max <= W * kKv4OneSteps * kChunkTokens / s.block_size) want = W;
+    }
     int64_t eps = (k_max + want - 1) / want;
     eps = ((eps + step - 1) / step) * step;
     if (eps > 64) eps = 64;
@@ -713,14 +754,14 @@ hipError_t launch_attention(const pulse_shape& s, const void* q, const void* poo
                             hipEvent_t done, __bf16* x) {
     if (B == 0) return hipSuccess;
     const int32_t Hkv = s.num_kv_heads, Hq = s.num_q_heads, G = Hq / Hkv;
-    const AttnPlan p = attn_plan(B, Hkv, k_max, s.block_size);
-    const int W = attn_waves(G);
+    const AttnPlan p = attn_plan(s, B, k_max);
+    const int W = attn_waves(s);
     const int32_t n_wg = (p.n_split + W - 1) / W;
     SplitArgs sp;
     sp.eps = p.entries_per_split;
     sp.n_wg = n_wg;
     sp.step = split_step(s.block_size);
-    sp.least = split_least(s.block_size);
+    sp.least = split_least(s);
     const int64_t all = (int64_t)B * n_wg;
     const int32_t round = PULSE_ATTN_TARGET_WAVES / (W * Hkv);  // pieces of one round
     sp.fit = (int32_t)(4 * (int64_t)round >= 5 * (int64_t)B && round < all ? round : all);
@@ -738,7 +779,7 @@ hipError_t launch_attention(const pulse_shape& s, const void* q, const void* poo
 #define PULSE_ATTN_W(DT, BS) \
     if (W == 8) PULSE_ATTN(DT, BS, 8); else PULSE_ATTN(DT, BS, 4)
 #define PULSE_ATTN_KV4(DT, BS)                \
-    if (G <= 4) PULSE_ATTN(DT, BS, 8, 4);     \
+    if (G <= 4) PULSE_ATTN(DT, BS, 8, 4);      \
     else if (G <= 8) PULSE_ATTN(DT, BS, 8, 8); \
     else PULSE_ATTN(DT, BS, 4, 16)
 #define PULSE_ATTN_BS(WHICH, DT)                   \

@@ -160,14 +160,13 @@ struct WsLayout {
     size_t total;
 };
 
-AttnPlan attn_plan(int32_t B, int32_t Hkv, int32_t k_max, int32_t bs);
-// Waves per attention workgroup for a GQA group of G query heads.
-inline int attn_waves(int G) { return G <= 8 ? 8 : 4; }
+AttnPlan attn_plan(const pulse_shape& s, int32_t B, int32_t k_max);
+// Waves per attention workgroup; and of all of them, those that a plan aims at.
+int attn_waves(const pulse_shape& s);
 // Attention partials a call with these arguments writes: one per workgroup.
 inline int64_t attn_partial_units(const pulse_shape& s, int32_t B, int32_t k_max) {
-    const int G = s.num_q_heads / s.num_kv_heads;
-    const AttnPlan p = attn_plan(B, s.num_kv_heads, k_max, s.block_size);
-    const int W = attn_waves(G);
+    const AttnPlan p = attn_plan(s, B, k_max);
+    const int W = attn_waves(s);
     return (int64_t)B * s.num_kv_heads * ((p.n_split + W - 1) / W);
 }
 WsLayout ws_layout(const pulse_shape& s, int32_t B, int32_t k_max, int64_t total_blocks);

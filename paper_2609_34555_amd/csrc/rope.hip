@@ -13,6 +13,7 @@ namespace pulse {
 constexpr int kRopeThreads = 256;
 constexpr int kRopeGroups = kRopeThreads / 16;
 constexpr int32_t kRopeGrid = 1 << 20;
+constexpr int kRopeAhead = 3;  // heads of a group whose loads are in flight together
 constexpr int kMaxPairs = kHeadDim / 2;
 
 struct RopeArgs {
@@ -56,63 +57,95 @@ __device__ inline float group_sum(float x) {
     return x;
 }
 
+// The rotation of a head's channels 8l .. 8l + 7.
+template <bool INTER>
+__device__ inline void rotate(int rot, const float* s_cos, const float* s_sin, float (&x)[8], int l, int tid) {
+    const int c8 = 8 * l, half = rot / 2;
+    if constexpr (INTER) {
+        if (c8 < rot) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float c = s_cos[4 * l + i], s = s_sin[4 * l + i];
+                const float u = x[2 * i], v = x[2 * i + 1];
+                x[2 * i] = u * c - v * s;
+                x[2 * i + 1] = u * s + v * c;
+            }
+        }
+    } else {
+        // a channel's partner is rot / 2 channels, a whole number of lanes, away
+        const bool low = c8 < half;
+        const int partner = (tid & 48) | (low ? l + half / 8 : l - half / 8);
+        const int pair = low ? c8 : c8 - half;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float o = __shfl(x[i], partner & 63);
+            if (c8 < rot) {
+                const float c = s_cos[pair + i], s = s_sin[pair + i];
+                x[i] = low ? x[i] * c - o * s : o * s + x[i] * c;
+            }
+        }
+    }
+}
+
 template <int DT, bool INTER>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeArgs a) {
     __shared__ float s_cos[kMaxPairs], s_sin[kMaxPairs];
     const int tid = threadIdx.x, l = tid & 15, group = tid >> 4;
     const int c8 = 8 * l, half = a.rot / 2;
+    const int heads = a.Hq + a.Hkv;
+    auto at = [&](const uint16_t* q, int64_t q_stride, const uint16_t* k, int64_t k_stride, int64_t row, int h) {
+        return (h < a.Hq ? q + row * q_stride + (size_t)h * kHeadDim
+                         : k + row * k_stride + (size_t)(h - a.Hq) * kHeadDim) + c8;
+    };
+    // this lane's weights, and the row's first heads, do not wait for its angles
+    float qw[8], kw[8];
+    if (a.qw) to_floats<DT>(*reinterpret_cast<const u32x4*>(a.qw + c8), qw);
+    if (a.kw) to_floats<DT>(*reinterpret_cast<const u32x4*>(a.kw + c8), kw);
+    const double freq = tid < half ? a.inv_freq[tid] : 0.0;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        u32x4 raw[kRopeAhead];
+#pragma unroll
+        for (int i = 0; i < kRopeAhead; ++i) {
+            const int h = group + i * kRopeGroups;
+            if (h < heads) raw[i] = *reinterpret_cast<const u32x4*>(at(a.q, a.q_stride, a.k, a.k_stride, row, h));
+        }
         const int32_t pos = a.positions[row];
         if (pos < 0) continue;  // the same in every thread of the workgroup
         if (tid < half) {
             // less whole turns, 2 pi in two parts, then as a fraction of half a turn
-            const double t = (double)pos * a.inv_freq[tid], n = rint(t * 0.15915494309189533577);
+            const double t = (double)pos * freq, n = rint(t * 0.15915494309189533577);
             const double rest = fma(-n, 2.4492935982947064e-16, fma(-n, 6.28318530717958647693, t));
             sincospif((float)(rest * 0.31830988618379067154), &s_sin[tid], &s_cos[tid]);
         }
         __syncthreads();
-        for (int h = group; h < a.Hq + a.Hkv; h += kRopeGroups) {
-            const bool is_q = h < a.Hq;
-            const int hh = is_q ? h : h - a.Hq;
-            const uint16_t* src = is_q ? a.q + row * a.q_stride : a.k + row * a.k_stride;
-            const uint16_t* w = is_q ? a.qw : a.kw;
-            float x[8];
-            to_floats<DT>(*reinterpret_cast<const u32x4*>(src + (size_t)hh * kHeadDim + c8), x);
-            if (w) {
-                float ss = 0.f, wf[8];
+        for (int h0 = group; h0 < heads; h0 += kRopeAhead * kRopeGroups) {
+            if (h0 != group) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) ss += x[i] * x[i];
-                const float inv = 1.0f / sqrtf(group_sum(ss) * (1.0f / kHeadDim) + a.eps);
-                to_floats<DT>(*reinterpret_cast<const u32x4*>(w + c8), wf);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = x[i] * inv * wf[i];
-            }
-            if constexpr (INTER) {
-                if (c8 < a.rot) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float c = s_cos[4 * l + i], s = s_sin[4 * l + i];
-                        const float u = x[2 * i], v = x[2 * i + 1];
-                        x[2 * i] = u * c - v * s;
-                        x[2 * i + 1] = u * s + v * c;
-                    }
-                }
-            } else {
-                // a channel's partner is rot / 2 channels, a whole number of lanes, away
-                const bool low = c8 < half;
-                const int partner = (tid & 48) | (low ? l + half / 8 : l - half / 8);
-                const int pair = low ? c8 : c8 - half;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float o = __shfl(x[i], partner & 63);
-                    if (c8 < a.rot) {
-                        const float c = s_cos[pair + i], s = s_sin[pair + i];
-                        x[i] = low ? x[i] * c - o * s : o * s + x[i] * c;
-                    }
+                for (int i = 0; i < kRopeAhead; ++i) {
+                    const int h = h0 + i * kRopeGroups;
+                    if (h < heads) raw[i] = *reinterpret_cast<const u32x4*>(at(a.q, a.q_stride, a.k, a.k_stride, row, h));
                 }
             }
-            uint16_t* dst = is_q ? a.q_out + row * a.q_out_stride : a.k_out + row * a.k_out_stride;
-            *reinterpret_cast<u32x4*>(dst + (size_t)hh * kHeadDim + c8) = from_floats<DT>(x);
+#pragma unroll
+            for (int i = 0; i < kRopeAhead; ++i) {
+                const int h = h0 + i * kRopeGroups;
+                if (h >= heads) break;
+                const bool is_q = h < a.Hq;
+                float x[8];
+                to_floats<DT>(raw[i], x);
+                if (is_q ? a.qw != nullptr : a.kw != nullptr) {
+                    float ss = 0.f;
+#pragma unroll
+                    for (int n = 0; n < 8; ++n) ss += x[n] * x[n];
+                    const float inv = 1.0f / sqrtf(group_sum(ss) * (1.0f / kHeadDim) + a.eps);
+#pragma unroll
+                    for (int n = 0; n < 8; ++n) x[n] = x[n] * inv * (is_q ? qw[n] : kw[n]);
+                }
+                rotate<INTER>(a.rot, s_cos, s_sin, x, l, tid);
+                *reinterpret_cast<u32x4*>(
+                    const_cast<uint16_t*>(at(a.q_out, a.q_out_stride, a.k_out, a.k_out_stride, row, h))) =
+                    from_floats<DT>(x);
+            }
         }
         __syncthreads();
     }
