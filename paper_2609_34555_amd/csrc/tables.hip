@@ -324,6 +324,7 @@ __global__ __launch_bounds__(kTileThreads) void tables_fill_kernel(TabArgs a, Ta
     __shared__ TabRequests<kMaxBatch> s;
     __shared__ CellTokens<kTileThreads> tokens;
     __shared__ uint32_t miss_of[kWaves];
+    __shared__ int32_t free_list[kTileThreads];
     __shared__ int32_t s_before, s_total, s_place, s_bad;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, tile = blockIdx.x, tiles = gridDim.x;
     const int32_t head = *w.head;
@@ -366,13 +367,16 @@ __global__ __launch_bounds__(kTileThreads) void tables_fill_kernel(TabArgs a, Ta
     const int64_t c1 = min(all.cells, (int64_t)(tile + 1) * w.tile);
     for (int64_t c0 = (int64_t)tile * w.tile; c0 < c1; c0 += kTileThreads) {
         const int64_t c = c0 + tid;
+        // the slots that these cells could take do not wait for the entries
+        const int32_t f = tid < head + total - g0 ? a.free_slots[g0 + tid] : 0;
         Cell x;
         x.entry = 0;
         if (c < c1) x = load_cell(a, s, (int32_t)c);
         const uint64_t m = __ballot(x.entry < 0);
+        free_list[tid] = f;
         if (lane == 0) miss_of[wave] = (uint32_t)__popcll(m);
         __syncthreads();
-        int32_t g = g0 + __popcll(m & ((1ull << lane) - 1));
+        int32_t g = __popcll(m & ((1ull << lane) - 1));
 #pragma unroll
         for (int i = 0; i < kWaves; ++i) {
             g += i < wave ? (int32_t)miss_of[i] : 0;
@@ -380,7 +384,7 @@ __global__ __launch_bounds__(kTileThreads) void tables_fill_kernel(TabArgs a, Ta
         }
         if (c < c1) {
             int32_t slot = x.entry;
-            if (slot < 0) a.table[x.at] = slot = a.free_slots[g];
+            if (slot < 0) a.table[x.at] = slot = free_list[g];
             keep_cell(tokens, tid, x, slot);
         }
         __syncthreads();
