@@ -57,7 +57,8 @@
  * Exponents lie in -23 .. 13 (fp16) or -100 .. 125 (bf16), so that every value
  * is one of the 16-bit type; the scale byte 255 makes a group NaN.  Pools and
  * stores of 4-bit blocks are 16-byte aligned.  The entry points that take
- * these types: pulse_block_bytes, pulse_workspace_bytes, the selections,
+ * these types: pulse_block_bytes, pulse_workspace_bytes,
+ * pulse_build_digests, the selections,
  * pulse_recall_gather, pulse_release_recalled, pulse_sparse_decode_attn,
  * pulse_attention_workgroups, pulse_decode_layer(_noalloc), the offload layers
  * of pulse_irq_step (without an engine), pulse_build_tables,
@@ -138,7 +139,8 @@ PULSE_API size_t pulse_workspace_bytes(const pulse_shape* shape, int32_t B, int3
  *   digests[b][1][c] = max over valid tokens t of K(kv_head, t, c)
  * exactly, in the KV dtype (-0 orders below +0).
  *   kv           [total_blocks][block] elements; device memory or pinned,
- *                host-mapped memory (the kernel reads it directly)
+ *                host-mapped memory (the kernel reads it directly); of 4-bit
+ *                blocks the values that the codes stand for are taken
  *   blk_off      device int64 [B+1];   ctx_len  device int32 [B]
  *   total_blocks = blk_off[B] (host copy of the value, sizes the grid)
  *   digests      device, [total_blocks][2][head_dim] elements, written
@@ -372,8 +374,8 @@ PULSE_API pulse_status pulse_gs_last_timing(pulse_gs_engine* engine, float* ms3)
  *   out[r][hq] = sum_t softmax(logit)_t V(h, t)      (fp32)
  *   lse[r][hq] = log sum_t exp(logit_t)              (fp32, optional)
  * An empty selection gives out = 0 and lse = -inf.  Products and sums are
- * accumulated in fp32.  The order of a request's sums depends on B, Hkv, k_max
- * and bs and, for 2 to 64 requests whose counts are not all k_max, may depend on
+ * accumulated in fp32.  The order of a request's sums depends on B, the shape
+ * and k_max and, for 2 to 64 requests whose counts are not all k_max, may depend on
  * every request's sel_cnt: the last bits of a request's results may change with its
  * neighbours' counts.  The same call repeats its bits.
  *   out          device float [B][Hq][d];  lse optional device float [B][Hq]
@@ -389,7 +391,7 @@ PULSE_API pulse_status pulse_sparse_decode_attn(const pulse_shape* shape, const 
 /*
  * Split-K workgroups per (request, KV head) that pulse_sparse_decode_attn,
  * and the attention of pulse_decode_layer, launch for a batch of B requests
- * with at most k_max selected blocks each (it depends on B, Hkv, k_max and bs
+ * with at most k_max selected blocks each (it depends on B, the shape and k_max
  * only; up to 64 requests whose counts differ may share these workgroups out
  * by their counts).  Above 1, a kernel that merges the workgroups' partials
  * follows the split-K kernel, and pulse_layer_args.attn_split_event marks the

@@ -91,7 +91,7 @@ pulse_status pulse_build_digests(const pulse_shape* shape, const void* kv, const
                                  const int32_t* ctx_len, int32_t B, int64_t total_blocks, int32_t kv_head,
                                  void* digests, int32_t* dev_status, pulse_stream_t stream) {
     PULSE_REQUIRE(shape, PULSE_ERR_INVALID_ARG);
-    PULSE_REQUIRE(shape_supported(shape), PULSE_ERR_UNSUPPORTED);
+    PULSE_REQUIRE(kv_shape_supported(shape), PULSE_ERR_UNSUPPORTED);
     PULSE_REQUIRE(B >= 0 && total_blocks >= 0, PULSE_ERR_INVALID_ARG);
     PULSE_REQUIRE(kv_head >= 0 && kv_head < shape->num_kv_heads, PULSE_ERR_INVALID_ARG);
     if (B == 0 || total_blocks == 0) return PULSE_OK;

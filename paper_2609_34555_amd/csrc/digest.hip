@@ -12,7 +12,7 @@
 // channel costs one bit-select and half of a packed dot product.  Both
 // kernels are HBM-bound streams over the digests (512 B per block); one
 // 16-lane group owns one block, each lane 8 channels (one 16-byte load).
-#include "pulse_internal.h"
+#include "kv4.h"
 
 namespace pulse {
 
@@ -39,7 +39,8 @@ __device__ inline s16x2 order16(s16x2 x) { return x ^ ((x >> 15) & (int16_t)0x7F
 // vector instructions bound the kernel.  8 x 32K tokens, 8 KV heads (73 MB), six batches in
 // turn: 24.2 us with both the look-up first and single values, 17.6 now (4.2 TB/s).  One batch
 // over and over, whose keys stay in the 256 MB Infinity Cache: 18.0 and 14.7.
-template <int BS>
+// DT: a 4-bit cache's keys are decoded as they are loaded; 16-bit ones are taken as patterns, whatever their type.
+template <int BS, int DT>
 __global__ __launch_bounds__(256) void build_digests_kernel(const uint16_t* __restrict__ kv,
                                                             const int64_t* __restrict__ blk_off,
                                                             const int32_t* __restrict__ ctx_len, int32_t B,
@@ -51,11 +52,22 @@ __global__ __launch_bounds__(256) void build_digests_kernel(const uint16_t* __re
     if (b >= total_blocks) return;
     const int c8 = (lane & 15) * 8;
     const int tg = lane >> 4;
-    const size_t E = (size_t)2 * Hkv * BS * kHeadDim;
-    const uint16_t* K = kv + (size_t)b * E + (size_t)kv_head * BS * kHeadDim + tg * kHeadDim + c8;
     u32x4 v[R];
+    if constexpr (is_kv4(DT)) {
+        const uint8_t* K = reinterpret_cast<const uint8_t*>(kv) + ((size_t)b * Hkv + kv_head) * kv4_head_bytes(BS);
 #pragma unroll
-    for (int i = 0; i < R; ++i) v[i] = *reinterpret_cast<const u32x4*>(K + (size_t)4 * i * kHeadDim);
+        for (int i = 0; i < R; ++i) {
+            const int row = 4 * i + tg;
+            const uint32_t code = *reinterpret_cast<const uint32_t*>(K + row * 64 + c8 / 2);
+            const uint32_t scale = K[kv4_key_scales(BS) + row * kGroups + c8 / kGroup];
+            v[i] = __builtin_bit_cast(u32x4, kv4_decode8<elem_type(DT)>(code, kv4_scale(scale)));
+        }
+    } else {
+        const size_t E = (size_t)2 * Hkv * BS * kHeadDim;
+        const uint16_t* K = kv + (size_t)b * E + (size_t)kv_head * BS * kHeadDim + tg * kHeadDim + c8;
+#pragma unroll
+        for (int i = 0; i < R; ++i) v[i] = *reinterpret_cast<const u32x4*>(K + (size_t)4 * i * kHeadDim);
+    }
     const int r = find_request(blk_off, B, b);
     const int64_t j = b - blk_off[r];
     const int64_t nv64 = (int64_t)ctx_len[r] - j * BS;
@@ -337,13 +349,18 @@ hipError_t launch_build_digests(const pulse_shape& s, const void* kv, const int6
                                 const int32_t* ctx_len, int32_t B, int64_t total_blocks, int32_t kv_head,
                                 void* digests, int32_t* status, hipStream_t st) {
     if (total_blocks == 0) return hipSuccess;
-#define PULSE_DIGEST(BS)                                                                                          \
-    hipLaunchKernelGGL(build_digests_kernel<BS>, dim3((unsigned)((total_blocks + 3) / 4)), dim3(256), 0, st,     \
+#define PULSE_DIGEST(BS, DT)                                                                                      \
+    hipLaunchKernelGGL((build_digests_kernel<BS, DT>), dim3((unsigned)((total_blocks + 3) / 4)), dim3(256), 0, st, \
                        (const uint16_t*)kv, blk_off, ctx_len, B, total_blocks, s.num_kv_heads, kv_head,          \
                        (uint16_t*)digests, status)
-    if (s.block_size == 16) PULSE_DIGEST(16);
-    else if (s.block_size == 32) PULSE_DIGEST(32);
-    else PULSE_DIGEST(64);
+#define PULSE_DIGEST_BS(DT)                             \
+    if (s.block_size == 16) PULSE_DIGEST(16, DT);       \
+    else if (s.block_size == 32) PULSE_DIGEST(32, DT);  \
+    else PULSE_DIGEST(64, DT)
+    if (s.dtype == PULSE_F16_KV4) { PULSE_DIGEST_BS(PULSE_F16_KV4); }
+    else if (s.dtype == PULSE_BF16_KV4) { PULSE_DIGEST_BS(PULSE_BF16_KV4); }
+    else { PULSE_DIGEST_BS(PULSE_BF16); }
+#undef PULSE_DIGEST_BS
 #undef PULSE_DIGEST
     return hipGetLastError();
 }

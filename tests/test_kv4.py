@@ -205,7 +205,7 @@ def attend(sh, q, pool, table, sel, cnt, ctx, lse=True, ws_fill=255, status_want
 def check_attention(out, lse, want, want_lse, mass, reach, n):
     """A logit is a sum of 128 fp32 products of exact factors (132 * 2^-24 of the sum of their sizes covers it and the
     scaling), the exponential adds 2^-23 of its value and 2^-24 of its argument, which no larger than twice `reach` is;
-    the probability is two bf16 parts (2^-16), summed over n tokens in fp32 (as is the denominator)."""
+    the probability is a sum of bf16 parts (2^-16 at most), summed over n tokens in fp32 (as is the denominator)."""
     logit = reach * 134 * 2.0**-24 + 2.0**-23
     rel = (2 * logit + 2.0**-16 + (n + 16) * 2.0**-23)[:, None]
     over = ((out.double().cpu() - want).abs() / (mass * rel + 1e-30)).max().item()
