@@ -56,7 +56,8 @@
  *   key scales    [bs][4] bytes        value scales  [4][bs] bytes
  * Exponents lie in -23 .. 13 (fp16) or -100 .. 125 (bf16), so that every value
  * is one of the 16-bit type; the scale byte 255 makes a group NaN.  Pools and
- * stores of 4-bit blocks are 16-byte aligned.  The entry points that take
+ * stores of 4-bit blocks are 16-byte aligned (else PULSE_ERR_INVALID_ARG from
+ * the recall, the attention and the layer-step).  The entry points that take
  * these types: pulse_block_bytes, pulse_workspace_bytes,
  * pulse_build_digests, the selections,
  * pulse_recall_gather, pulse_release_recalled, pulse_sparse_decode_attn,

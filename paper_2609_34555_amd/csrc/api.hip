@@ -253,6 +253,11 @@ pulse_status pulse_pick_solo_heads(const float* mam, int32_t rows, int32_t num_k
     return PULSE_OK;
 }
 
+// Pools and stores of 4-bit blocks begin on a 16-byte piece.
+static bool kv4_aligned(const pulse_shape& s, const void* p) {
+    return !is_kv4(s.dtype) || reinterpret_cast<uintptr_t>(p) % 16 == 0;
+}
+
 static pulse_status check_recall_args(const pulse_shape* shape, const void* host_kv, const int64_t* blk_off,
                                       int32_t B, const int32_t* sel_idx, const int32_t* sel_cnt, int32_t k_max,
                                       int32_t* block_table, int32_t max_blocks, const int32_t* free_slots,
@@ -268,6 +273,7 @@ static pulse_status check_recall_args(const pulse_shape* shape, const void* host
                       dev_status,
                   PULSE_ERR_INVALID_ARG);
     PULSE_REQUIRE(free_slots || n_free == 0, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(kv4_aligned(*shape, host_kv) && kv4_aligned(*shape, slot_pool), PULSE_ERR_INVALID_ARG);
     return PULSE_OK;
 }
 
@@ -323,6 +329,7 @@ pulse_status pulse_sparse_decode_attn(const pulse_shape* shape, const void* q, c
     if (B == 0) return PULSE_OK;
     PULSE_REQUIRE(q && slot_pool && block_table && sel_idx && sel_cnt && ctx_len && out && dev_status,
                   PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(kv4_aligned(*shape, slot_pool), PULSE_ERR_INVALID_ARG);
     const WsLayout w = ws_layout(*shape, B, k_max, 0);
     PULSE_REQUIRE(ws && ws_bytes >= w.total, PULSE_ERR_WORKSPACE);
     return hip_status(launch_attention(*shape, q, slot_pool, n_slots, block_table, max_blocks, sel_idx, sel_cnt,

@@ -8,13 +8,17 @@
 // Bound: memory round trips (lengths; then table entries and free slots, which do not wait for one another; then the
 // writes) and launches; beyond some ten thousand tokens the 12 bytes written per token.  Nothing may be written before
 // every length, entry and slot has been checked.  Small steps run in one workgroup, whose threads keep their cells in
-// registers.  Larger ones take two launches over tiles of cells: the first counts and checks each tile, the second adds
+// registers; larger ones take two launches over tiles of cells: the first counts and checks each tile, the second adds
 // the tiles' counts up (each workgroup for itself) and writes.
 #include "pulse_internal.h"
 
 namespace pulse {
 
-constexpr int kCellsPer = 4;            // cells of a thread of the one-workgroup form
+constexpr int kCellsPer = 4;            // cells of a thread of the one-workgroup forms
+// Room for tokens up to which one workgroup of 256 threads, and one of 1024, is fastest: in us, 256 threads, 1024
+// and two launches: 32 requests of one token 5.0, 6.8, 7.1; one request of 1000 tokens 5.2, 6.9, 7.3; of 8000 9.2, 8.0,
+// 9.3; of 15000 13.5, 9.1, 9.5; of 30000 -, 12.0, 9.8; 4 of 15000 -, 18.1, 10.2.
+constexpr int64_t kOneTokens = 4096, kOneWideTokens = 16384;
 constexpr int kTileThreads = 256;       // a tile is a multiple of that many cells
 constexpr int64_t kMaxTiles = 1024;     // every workgroup of the larger form reads every tile's count
 
@@ -70,6 +74,7 @@ __device__ inline bool scan_requests(const TabArgs& a, TabRequests<B>& s, TabTot
     const int per = B <= T ? 1 : (a.B + T - 1) / T, r0 = tid * per, r1 = min(a.B, r0 + per);
     uint64_t sum[3] = {0, 0, 0}, before[3];
     int bad = 0;
+#pragma unroll 4
     for (int r = r0; r < r1; ++r) {
         const int32_t ctx = a.ctx[r], n = a.fresh[r];
         const int64_t blocks = ((int64_t)ctx + (1 << a.shift) - 1) >> a.shift;
@@ -393,8 +398,11 @@ __global__ __launch_bounds__(kTileThreads) void tables_fill_kernel(TabArgs a, Ta
     }
 }
 
-// Bound on the cells of a step: a request's new tokens lie in at most two blocks more than they fill.
-static int64_t cell_bound(int32_t B, int32_t bs, int64_t max_tokens) { return max_tokens / bs + 2 * (int64_t)B; }
+// Bound on the cells of a step: each holds a new token, and a request's lie in at most two blocks more than they fill.
+static int64_t cell_bound(int32_t B, int32_t bs, int64_t max_tokens) {
+    const int64_t n = max_tokens / bs + 2 * (int64_t)B;
+    return n < max_tokens ? n : max_tokens;
+}
 // Cells of a tile: kTileThreads, or the multiple of them that keeps the tiles few.
 static int64_t tile_cells(int64_t cells) {
     return kTileThreads * ((cells + kTileThreads * kMaxTiles - 1) / (kTileThreads * kMaxTiles));
@@ -414,9 +422,9 @@ hipError_t launch_tables(const int32_t* ctx, const int32_t* fresh, int32_t B, in
     const TabArgs a{ctx,     fresh,   B,       shift,    table,     max_blocks, free_slots, free_head,
                     n_free,  n_slots, blk_off, tok_off,  slot_map,  positions,  max_tokens, status};
     const int64_t cells = cell_bound(B, bs, max_tokens);
-    if (B <= 256 && cells <= 256 * kCellsPer) {
+    if (B <= 256 && cells <= 256 * kCellsPer && max_tokens <= kOneTokens) {
         hipLaunchKernelGGL((tables_one_kernel<256, 256>), dim3(1), dim3(256), 0, st, a);
-    } else if (cells <= 1024 * kCellsPer) {
+    } else if (cells <= 1024 * kCellsPer && max_tokens <= kOneWideTokens) {
         hipLaunchKernelGGL((tables_one_kernel<1024, kMaxBatch>), dim3(1), dim3(1024), 0, st, a);
     } else {
         const int64_t tile = tile_cells(cells), tiles = (cells + tile - 1) / tile;

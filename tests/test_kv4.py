@@ -343,6 +343,17 @@ def test_kv4_sizes_and_refusals():
     with pytest.raises(P.PulseError) as e:
         P.GatherScatterEngine(sh, 1, 8, 8)
     assert e.value.status == P.PULSE_ERR_UNSUPPORTED
+    r = dict(host_kv=FAKE, blk_off=FAKE, B=2, sel_idx=FAKE, sel_cnt=FAKE, k_max=16, block_table=FAKE, max_blocks=100,
+             free_slots=FAKE, free_head=FAKE, n_free=10, slot_pool=FAKE, n_slots=50, stats=FAKE, dev_status=FAKE, ws=FAKE,
+             ws_bytes=1, stream=0, check=False)
+    t = dict(q=FAKE, slot_pool=FAKE, n_slots=50, block_table=FAKE, max_blocks=100, sel_idx=FAKE, sel_cnt=FAKE, k_max=16,
+             ctx_len=FAKE, B=2, sm_scale=0.1, out=FAKE, lse=None, dev_status=FAKE, ws=FAKE, ws_bytes=1, stream=0,
+             check=False)
+    assert P.pulse_recall_gather(sh, **r) == P.PULSE_ERR_WORKSPACE
+    assert P.pulse_recall_gather(sh, **{**r, "host_kv": FAKE + 8}) == P.PULSE_ERR_INVALID_ARG
+    assert P.pulse_recall_gather(sh, **{**r, "slot_pool": FAKE + 8}) == P.PULSE_ERR_INVALID_ARG
+    assert P.pulse_sparse_decode_attn(sh, **t) == P.PULSE_ERR_WORKSPACE
+    assert P.pulse_sparse_decode_attn(sh, **{**t, "slot_pool": FAKE + 8}) == P.PULSE_ERR_INVALID_ARG
     a = dict(k=FAKE, k_stride=1024, v=FAKE, v_stride=1024, slot_map=FAKE, n_rows=3, slot_pool=FAKE, n_slots=9,
              dev_status=FAKE, stream=0, check=False)
     for fn in (P.pulse_append_kv, P.pulse_load_kv):

@@ -81,6 +81,23 @@ def test_norm_rope(T, hq, hkv, rot, inter, weights, far, gap, dt):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("which", ["q", "k"])
+def test_one_weight_alone(which):
+    """Only the side that has a weight is normed."""
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    q, k = (torch.randn((3, h, D), generator=gen, device=DEV).mul_(3).bfloat16() for h in (4, 2))
+    w = torch.randn(D, generator=gen, device=DEV).bfloat16()
+    pos = torch.tensor([0, 17, 4000], dtype=torch.int32, device=DEV)
+    qo, ko = torch.zeros_like(q), torch.zeros_like(k)
+    qw, kw = (w, None) if which == "q" else (None, w)
+    P.pulse_qk_norm_rope(P.make_shape(4, 2, D, 16, P.PULSE_BF16), q, 4 * D, k, 2 * D, 3, pos, qw, kw, 1e-6, inv_freq(D),
+                         D, 0, qo, 4 * D, ko, 2 * D)
+    for x, y, wt in ((q, qo, qw), (k, ko, kw)):
+        want, size = plain64.norm_rope(x, wt, 1e-6, pos, inv_freq(D), D, 0)
+        assert ((y.double().cpu() - want).abs() <= bound(want, size, torch.bfloat16)).all()
+
+
+@pytest.mark.gpu
 def test_norm_rope_non_finite_stays_in_its_head():
     q = torch.randn((2, 4, D), device=DEV).bfloat16()
     k = torch.randn((2, 2, D), device=DEV).bfloat16()

@@ -70,9 +70,17 @@ CASES = [  # contexts, new tokens, bs, room behind the last token, share of late
     ([31, 32, 33, 4000], [31, 1, 33, 3999], 32, 1, 0.3),
     ([700 + 13 * r for r in range(70)], [1] * 70, 16, 26, 0.0),          # a decode step
     ([20 * r + 1 for r in range(70)], [r % 7 for r in range(70)], 16, 0, 0.1),
-    ([3000] * 20, [2999] * 20, 16, 0, 0.05),                              # several rounds of one workgroup
-    ([16 * 4094 - 5], [16 * 4094 - 5], 16, 5, 0.2),                       # the largest step of one workgroup
-    ([16 * 4094 + 16], [16 * 4094 + 16], 16, 0, 0.2),                     # and the smallest of two launches
+    ([3000] * 20, [2999] * 20, 16, 0, 0.05),                              # many blocks of 20 requests
+    # on either side of the rules: room for 4096 and for 16384 tokens, 256 requests, 4096 blocks
+    ([4000, 91], [4000, 91], 16, 5, 0.2),
+    ([4000, 91], [4000, 91], 16, 6, 0.2),
+    ([9000, 7384], [9000, 7384], 16, 0, 0.2),
+    ([9000, 7385], [9000, 7385], 16, 0, 0.2),
+    ([33 + r for r in range(256)], [1] * 256, 16, 0, 0.0),
+    ([33 + r for r in range(257)], [1] * 257, 16, 0, 0.0),
+    ([9] * 1792, [4] * 1792, 16, 0, 0.2),
+    ([9] * 2040, [4] * 2040, 16, 0, 0.2),
+    ([16 * 4094 + 16], [16 * 4094 + 16], 16, 0, 0.2),
     ([60000, 1, 0, 70001, 33, 16 * 2048], [59999, 1, 0, 70001, 2, 16 * 2048], 16, 700, 0.1),
     ([300000, 5, 300001], [299990, 5, 300001], 64, 0, 0.02),
     ([x % 50 for x in range(4096)], [min(1, x % 50) for x in range(4096)], 16, 0, 0.0),
