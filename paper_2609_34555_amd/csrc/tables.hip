@@ -14,13 +14,15 @@
 
 namespace pulse {
 
-constexpr int kCellsPer = 4;            // cells of a thread of the one-workgroup forms
+constexpr int kCellsPer = 4;  // cells of a thread of the one-workgroup forms
 // Room for tokens up to which one workgroup of 256 threads, and one of 1024, is fastest: in us, 256 threads, 1024
 // and two launches: 32 requests of one token 5.0, 6.8, 7.1; one request of 1000 tokens 5.2, 6.9, 7.3; of 8000 9.2, 8.0,
 // 9.3; of 15000 13.5, 9.1, 9.5; of 30000 -, 12.0, 9.8; 4 of 15000 -, 18.1, 10.2.
 constexpr int64_t kOneTokens = 4096, kOneWideTokens = 16384;
-constexpr int kTileThreads = 256;       // a tile is a multiple of that many cells
-constexpr int64_t kMaxTiles = 1024;     // every workgroup of the larger form reads every tile's count
+// A tile is a multiple of that many cells, a thread each.  In us (with two small launches beside), 256, 512 and 1024: 590K
+// tokens 22.1, 22.2, 25.0; 3.2M tokens 39.0, 28.8, 30.5 (a workgroup's look-ups before its first token weigh less).
+constexpr int kTileThreads = 512;
+constexpr int64_t kMaxTiles = 1024;  // every workgroup of the larger form reads every tile's count
 
 struct TabArgs {
     const int32_t *ctx, *fresh;
@@ -202,6 +204,7 @@ __device__ inline void keep_cell(CellTokens<N>& s, int i, const Cell& x, int32_t
 // Maps of the tokens of n cells, neighbouring threads on neighbouring tokens.
 template <int T, int N>
 __device__ inline void fill_tokens(const TabArgs& a, const CellTokens<N>& s, int n) {
+#pragma unroll 4
     for (int i = threadIdx.x; i < n << a.shift; i += T) {
         const int c = i >> a.shift, t = i & ((1 << a.shift) - 1);
         const int32_t range = s.range[c];
