@@ -317,10 +317,20 @@ __device__ inline void attend_split(const uint16_t* __restrict__ q, const uint16
 // of the P operand hold GP = 4, 8 or 16 query heads for 4, 2 or 1 groups at once (row = g' * GP + q: the query
 // columns of S^T repeat), so P' costs a multiplication per row and token however many heads there are; the
 // product of channel tile t uses the rows of its group t / 2, the other rows of its result are left unused.
-// Codes are exact in bf16 and scales are powers of two, so P' is split into bf16 parts for either 16-bit type (fp16
+// Codes are exact in bf16 and scales are powers of two, so P' is cut into bf16 parts for either 16-bit type (fp16
 // would not hold the range of the scales): three of them, all 24 bits of it.  With two (2^-17 of it) the results
-// were 1.4e-6 off, with three 4e-7, as a computation in fp32 is.
+// were 1.4e-6 off, with three 2e-7, below what a computation in fp32 is off (4e-7), for 0.2 to 1 us a call.
 // Row 4 * grp + v of acc[t] is query head (4 * grp + v) % GP of group (4 * grp + v) / GP of the tile's set.
+//
+// Bound: 136 bytes per token and KV head.  32 requests of 4K tokens, 8 heads (141 MB): 29 us (4.9 TB/s; 24 at what
+// streaming reads reach), of which 8 are the launch, the look-ups ahead of the first key and the waves' merge; short
+// calls are those 8 and 0.6 to 1.4 us a step.  A step is about 230 vector instructions (64 of them decode), which the
+// eight waves of a CU issue in about 1 us, so they count beside the bytes: scale bytes by shift and mask cost 2 to 3%
+// on 16 ragged requests, rounded instead of cut parts as much.  Loads: the next step's are issued once the keys are
+// decoded.  Measured slower or equal: two, three and four steps ahead (2 to 6% slower), codes loaded with
+// neighbouring lanes on neighbouring pieces and passed through LDS (2% slower), the next step's softmax under the
+// products of this one (equal), products interleaved over accumulators (equal), 16 waves per workgroup (5 to 10%
+// slower), two workgroups per CU (20% slower).
 template <int GP>
 struct Kv4Values {
     u32x4 v[2];        // codes of 8 tokens, channel tiles 0..3 and 4..7
@@ -330,12 +340,7 @@ struct Kv4Values {
 // 2^e of byte N of a word of scale bytes.
 template <int N>
 __device__ inline float kv4_scale_of(uint32_t w) {
-    uint32_t u;
-    if constexpr (N == 0) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_0" : "=v"(u) : "v"(23), "v"(w));
-    if constexpr (N == 1) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_1" : "=v"(u) : "v"(23), "v"(w));
-    if constexpr (N == 2) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_2" : "=v"(u) : "v"(23), "v"(w));
-    if constexpr (N == 3) u = (w >> 1) & 0x7F800000u;
-    return __uint_as_float(u);
+    return kv4_scale(__builtin_amdgcn_ubfe(w, 8 * N, 8));
 }
 
 template <int DT, int BS, int GP>
@@ -425,7 +430,8 @@ __device__ inline void attend_split_kv4(const uint16_t* __restrict__ q, const ui
     };
     load_k(0);
     load_v(0);
-#pragma unroll 1
+    // (in twos, so that the values need not be moved from `vnext`)
+#pragma unroll 2
     for (int i = 0; i < steps; ++i) {
         Kv4Values<GP> now = vnext;
         // --- S^T = K . Q^T
@@ -455,9 +461,10 @@ __device__ inline void attend_split_kv4(const uint16_t* __restrict__ q, const ui
                     if (n >= left) now.vs[k][n / 4] &= ~(0xFFu << (8 * (n % 4)));
             }
         }
+        // (the median of two values and infinity: fmaxf would first make each of them a number of its own)
         float cm = x[0];
 #pragma unroll
-        for (int n = 1; n < 8; ++n) cm = fmaxf(cm, x[n]);
+        for (int n = 1; n < 8; ++n) cm = __builtin_amdgcn_fmed3f(cm, x[n], INFINITY);
         cm = across_groups(cm, [](float a, float b) { return fmaxf(a, b); });
         const float m_new = fmaxf(m_run, cm * scale_log2);
         const float m_use = m_new == -INFINITY ? 0.f : m_new;
@@ -495,10 +502,9 @@ __device__ inline void attend_split_kv4(const uint16_t* __restrict__ q, const ui
                 float a = y[2 * n], b = y[2 * n + 1];
 #pragma unroll
                 for (int m = 0; m < 3; ++m) {
-                    const bf16x2 two = {(__bf16)a, (__bf16)b};
-                    part[m][n] = __builtin_bit_cast(uint32_t, two);
-                    a -= __uint_as_float(part[m][n] << 16);
-                    b -= __uint_as_float(part[m][n] & 0xFFFF0000u);
+                    part[m][n] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+                    a -= __uint_as_float(__float_as_uint(a) & 0xFFFF0000u);
+                    b -= __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
                 }
             }
 #pragma unroll

@@ -11,7 +11,7 @@
 // channels" by exchanges of lane groups in registers.
 // A run shorter than an octet shares words with other tokens, which other rows of the call may be writing: it
 // clears and sets its own bits with atomics, whose order does not matter.
-// 16K rows of 8 heads into 4 bits: 24 us for 85 MB (17.8 at the rate of a large copy), back 15; with a lane per two
+// 16K rows of 8 heads into 4 bits: 19 us for 85 MB (17.8 at the rate of a large copy), back 15; with a lane per two
 // channels and a wave per row, byte stores and all, 97 and 69.
 #include "kv4.h"
 
@@ -134,8 +134,8 @@ __device__ inline void append_run(const CacheArgs& a, const Run& run, int lane) 
         on[i] = t >= 0 && t < run.n;
         const int64_t row = run.first + (on[i] ? t : 0);
         const size_t c = (size_t)run.h * kHeadDim + 8 * l;
-        // streamed: rows that stay in the caches push the half-written lines of the blocks out (16K rows of 8 heads 24 us
-        // with ordinary loads, 17 with these)
+        // streamed: rows that stay in the caches push the half-written lines of the blocks out (16K rows of 8 heads 27 us
+        // with ordinary loads, 19 with these)
         k[i] = v[i] = u32x4{0, 0, 0, 0};
         if (on[i]) {
             k[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(a.k_in + row * a.k_stride + c));
