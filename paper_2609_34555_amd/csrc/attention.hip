@@ -430,8 +430,7 @@ __device__ inline void attend_split_kv4(const uint16_t* __restrict__ q, const ui
     };
     load_k(0);
     load_v(0);
-    // (in twos, so that the values need not be moved from `vnext`)
-#pragma unroll 2
+#pragma unroll 1
     for (int i = 0; i < steps; ++i) {
         Kv4Values<GP> now = vnext;
         // --- S^T = K . Q^T
