@@ -400,3 +400,15 @@ def test_any_scale(scale):
         n = (j[:, None] * 16 + torch.arange(16)).view(-1) < ctx[r]
         check_attention(out[r], lse[r], *plain64.attention(q[r] * (-1 if scale < 0 else 1), k[:, n], v[:, n], abs(scale)),
                         int(n.sum()))
+
+
+def test_kv4_attention_workgroups():
+    """One workgroup, hence no merge launch, up to four 32-token steps of each of its waves (8, or 4 beyond eight query
+    heads per KV head); splits over several beyond."""
+    def groups(hq, hkv, bs, B, k):
+        return P.pulse_attention_workgroups(P.make_shape(hq, hkv, D, bs, P.PULSE_BF16_KV4), B, k)
+
+    for hq, hkv, bs, k in ((32, 8, 16, 64), (64, 8, 32, 32), (64, 4, 64, 8), (8, 8, 64, 16)):
+        assert groups(hq, hkv, bs, 2, k) == 1
+        assert groups(hq, hkv, bs, 2, k + 1) > 1
+    assert groups(32, 8, 16, 32, 256) == 1  # 256 requests and heads take a round of workgroups between them

@@ -225,3 +225,48 @@ def test_tables_refusals():
     assert P.pulse_tables_workspace_bytes(shape(bs=8), 1, 5) == 0
     assert P.lib().pulse_build_tables(None, *[None] * 2, 0, None, 1, None, None, 0, 1, None, None, None, None, 0, None,
                                       None, 0, None) == P.PULSE_ERR_INVALID_ARG
+
+
+@pytest.mark.gpu
+def test_two_launch_step_captured_and_replayed():
+    """The larger form in a graph: replays with the program's own eager calls and table resets between, the scratch full
+    of what the last call left; a fault in one replay leaves the next as it was."""
+    rng = random.Random(12)
+    ctx, new = [70000, 40, 30000], [69990, 40, 1]
+    table, free, n_slots = start(ctx, new, 16, rng, later=0.1)
+    cap = sum(new) + 9
+    want = tuple(plain64.tables(ctx, new, 16, table, free, 0, cap))
+    s = Step(ctx, new, 16, table, free, n_slots, cap)
+    t0 = s.table.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    s.run(stream=side)
+    side.synchronize()
+    assert s.got() == want
+
+    def reset():
+        s.table.copy_(t0)
+        s.head.zero_()
+        s.status.zero_()
+        for t in (s.blk, s.tok, s.place[:cap], s.pos[:cap]):
+            t.fill_(5)
+
+    reset()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        s.run()
+    for i in range(4):
+        reset()
+        if i == 2:
+            s.ctx[1] = -1
+        g.replay()
+        torch.cuda.synchronize()
+        if i == 2:
+            assert s.status.item() == P.PULSE_ERR_BAD_INDEX and s.got()[:2] == ([0] * 4, [0] * 4)
+            assert torch.equal(s.table, t0) and s.head.item() == 0
+            s.ctx[1] = ctx[1]
+        else:
+            assert s.status.item() == 0 and s.got() == want
+            s.run()  # eager, on its own result
+            assert s.got() == want
