@@ -330,7 +330,9 @@ __device__ inline void attend_split(const uint16_t* __restrict__ q, const uint16
 // decoded.  Measured slower or equal: two, three and four steps ahead (2 to 6% slower), codes loaded with
 // neighbouring lanes on neighbouring pieces and passed through LDS (2% slower), the next step's softmax under the
 // products of this one (equal), products interleaved over accumulators (equal), 16 waves per workgroup (5 to 10%
-// slower), two workgroups per CU (20% slower).
+// slower), two workgroups per CU (20% slower), keys multiplied as codes by the scaled 4-bit matrix instruction (Q cut
+// into two or three e4m3 parts; 34 vector instructions fewer a step: 1% faster on 16 ragged requests, 2 to 10% slower
+// on the others for the cutting, and its sums are some hundred times less exact).
 template <int GP>
 struct Kv4Values {
     u32x4 v[2];        // codes of 8 tokens, channel tiles 0..3 and 4..7
