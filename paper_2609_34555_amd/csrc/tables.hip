@@ -292,16 +292,39 @@ __global__ __launch_bounds__(T) void tables_one_kernel(TabArgs a) {
     fill_tokens<T>(a, tokens, cells);
 }
 
+// Counts of the larger form's threads, added up wave by wave in registers (with LDS atomics of every thread the two
+// launches took 5 us more).
+struct Counts {
+    int32_t total, before, place, bad;
+};
+struct WaveCounts {
+    Counts of[kTileThreads / kWave];
+    __device__ inline void put(int32_t total, int32_t before, int32_t place, int32_t bad) {
+        const int32_t t = (int32_t)last_lane(wave_scan((uint32_t)total, 0u, OpAdd()));
+        const int32_t b = (int32_t)last_lane(wave_scan((uint32_t)before, 0u, OpAdd()));
+        const int32_t p = (int32_t)last_lane(wave_scan((uint32_t)place, 0x7FFFFFFFu, OpMin()));
+        const int32_t any = __ballot(bad) != 0;
+        if ((threadIdx.x & 63) == 0) of[threadIdx.x >> 6] = Counts{t, b, p, any};
+    }
+    __device__ inline Counts sum() const {
+        Counts c = of[0];
+#pragma unroll
+        for (int i = 1; i < kTileThreads / kWave; ++i) {
+            c.total += of[i].total;
+            c.before += of[i].before;
+            c.place = min(c.place, of[i].place);
+            c.bad |= of[i].bad;
+        }
+        return c;
+    }
+};
+
 __global__ __launch_bounds__(kTileThreads) void tables_count_kernel(TabArgs a, TabScratch w) {
     __shared__ TabRequests<kMaxBatch> s;
-    __shared__ int32_t s_count, s_bad, s_place;
+    __shared__ WaveCounts s_wave;
     const int tid = threadIdx.x, tile = blockIdx.x;
     const int32_t head = *a.free_head;
-    if (tid == 0) {
-        s_count = s_bad = 0;
-        s_place = INT32_MAX;
-        if (tile == 0) *w.head = head;
-    }
+    if (tid == 0 && tile == 0) *w.head = head;
     TabTotals all;
     int64_t off0;
     int n = 0, bad = 0;
@@ -317,13 +340,12 @@ __global__ __launch_bounds__(kTileThreads) void tables_count_kernel(TabArgs a, T
             if ((uint32_t)f >= (uint32_t)a.n_slots) place = min(place, (int32_t)c);
         }
     }
-    if (n) atomicAdd(&s_count, n);
-    if (bad) atomicOr(&s_bad, 1);
-    if (place != INT32_MAX) atomicMin(&s_place, place);
+    s_wave.put(n, 0, place, bad);
     __syncthreads();
     if (tid == 0) {
-        w.count[tile] = s_bad ? -1 : s_count;
-        w.bad_place[tile] = s_place;
+        const Counts c = s_wave.sum();
+        w.count[tile] = c.bad ? -1 : c.total;
+        w.bad_place[tile] = c.place;
     }
 }
 
@@ -333,13 +355,9 @@ __global__ __launch_bounds__(kTileThreads) void tables_fill_kernel(TabArgs a, Ta
     __shared__ CellTokens<kTileThreads> tokens;
     __shared__ uint32_t miss_of[kWaves];
     __shared__ int32_t free_list[kTileThreads];
-    __shared__ int32_t s_before, s_total, s_place, s_bad;
+    __shared__ WaveCounts s_wave;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, tile = blockIdx.x, tiles = gridDim.x;
     const int32_t head = *w.head;
-    if (tid == 0) {
-        s_before = s_total = s_bad = 0;
-        s_place = INT32_MAX;
-    }
     int32_t before = 0, total = 0, place = INT32_MAX, bad = 0;
     for (int t = tid; t < tiles; t += kTileThreads) {
         const int32_t n = w.count[t];
@@ -348,19 +366,16 @@ __global__ __launch_bounds__(kTileThreads) void tables_fill_kernel(TabArgs a, Ta
         before += t < tile ? n : 0;
         place = min(place, w.bad_place[t]);
     }
+    s_wave.put(total, before, place, bad);  // (read behind the barriers of the scan)
     TabTotals all;
     int64_t off0;
     bool ok = scan_requests<kTileThreads, kMaxBatch>(a, s, all, off0);
-    if (total) atomicAdd(&s_total, total);
-    if (before) atomicAdd(&s_before, before);
-    if (place != INT32_MAX) atomicMin(&s_place, place);
-    if (bad) atomicOr(&s_bad, 1);
-    __syncthreads();
-    total = s_total;
+    const Counts sums = s_wave.sum();
+    total = sums.total;
     int32_t code = PULSE_OK;
-    if (!ok || s_bad || head < 0 || head > a.n_free) code = PULSE_ERR_BAD_INDEX;
+    if (!ok || sums.bad || head < 0 || head > a.n_free) code = PULSE_ERR_BAD_INDEX;
     else if (total > a.n_free - head) code = PULSE_ERR_POOL_EXHAUSTED;
-    else if (s_place < total) code = PULSE_ERR_BAD_INDEX;
+    else if (sums.place < total) code = PULSE_ERR_BAD_INDEX;
     ok = code == PULSE_OK;
     if (tile == 0) {
         write_offsets<kTileThreads, kMaxBatch>(a, s, all, off0, ok);
@@ -371,7 +386,7 @@ __global__ __launch_bounds__(kTileThreads) void tables_fill_kernel(TabArgs a, Ta
     }
     fill_rest(a, ok ? all.tokens : 0, (int64_t)tile * kTileThreads + tid, (int64_t)tiles * kTileThreads);
     if (!ok) return;
-    int32_t g0 = head + s_before;
+    int32_t g0 = head + sums.before;
     const int64_t c1 = min(all.cells, (int64_t)(tile + 1) * w.tile);
     for (int64_t c0 = (int64_t)tile * w.tile; c0 < c1; c0 += kTileThreads) {
         const int64_t c = c0 + tid;
