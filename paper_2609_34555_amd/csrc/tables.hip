@@ -19,8 +19,9 @@ constexpr int kCellsPer = 4;  // cells of a thread of the one-workgroup forms
 // and two launches: 32 requests of one token 5.0, 6.8, 7.1; one request of 1000 tokens 5.2, 6.9, 7.3; of 8000 9.2, 8.0,
 // 9.3; of 15000 13.5, 9.1, 9.5; of 30000 -, 12.0, 9.8; 4 of 15000 -, 18.1, 10.2.
 constexpr int64_t kOneTokens = 4096, kOneWideTokens = 16384;
-// A tile is a multiple of that many cells, a thread each.  In us (with two small launches beside), 256, 512 and 1024: 590K
-// tokens 22.1, 22.2, 25.0; 3.2M tokens 39.0, 28.8, 30.5 (a workgroup's look-ups before its first token weigh less).
+// Threads of a tile's workgroup, which takes that many cells of 16 tokens.  In us (with two small launches beside), 256,
+// 512 and 1024: 590K tokens 22.1, 22.2, 25.0; 3.2M tokens 39.0, 28.8, 30.5 (a workgroup's look-ups before its first token
+// weigh less).
 constexpr int kTileThreads = 512;
 constexpr int64_t kMaxTiles = 1024;  // every workgroup of the larger form reads every tile's count
 
@@ -421,14 +422,15 @@ static int64_t cell_bound(int32_t B, int32_t bs, int64_t max_tokens) {
     const int64_t n = max_tokens / bs + 2 * (int64_t)B;
     return n < max_tokens ? n : max_tokens;
 }
-// Cells of a tile: kTileThreads, or the multiple of them that keeps the tiles few.
-static int64_t tile_cells(int64_t cells) {
-    return kTileThreads * ((cells + kTileThreads * kMaxTiles - 1) / (kTileThreads * kMaxTiles));
+// Cells of a tile: those of 16 * kTileThreads tokens, or the multiple of them that keeps the tiles few.
+static int64_t tile_cells(int64_t cells, int32_t bs) {
+    const int64_t least = kTileThreads * 16 / bs;
+    return least * ((cells + least * kMaxTiles - 1) / (least * kMaxTiles));
 }
 
 size_t tables_ws_bytes(int32_t B, int32_t bs, int64_t max_tokens) {
     const int64_t cells = cell_bound(B, bs, max_tokens);
-    const int64_t tiles = cells > 0 ? (cells + tile_cells(cells) - 1) / tile_cells(cells) : 0;
+    const int64_t tiles = cells > 0 ? (cells + tile_cells(cells, bs) - 1) / tile_cells(cells, bs) : 0;
     return (sizeof(int32_t) * (size_t)(1 + 2 * tiles) + 255) & ~(size_t)255;
 }
 
@@ -445,7 +447,7 @@ hipError_t launch_tables(const int32_t* ctx, const int32_t* fresh, int32_t B, in
     } else if (cells <= 1024 * kCellsPer && max_tokens <= kOneWideTokens) {
         hipLaunchKernelGGL((tables_one_kernel<1024, kMaxBatch>), dim3(1), dim3(1024), 0, st, a);
     } else {
-        const int64_t tile = tile_cells(cells), tiles = (cells + tile - 1) / tile;
+        const int64_t tile = tile_cells(cells, bs), tiles = (cells + tile - 1) / tile;
         int32_t* w = static_cast<int32_t*>(ws);
         const TabScratch sc{w, w + 1, w + 1 + tiles, (int32_t)tile};
         hipLaunchKernelGGL(tables_count_kernel, dim3((unsigned)tiles), dim3(kTileThreads), 0, st, a, sc);
