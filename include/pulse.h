@@ -57,14 +57,14 @@
  * Exponents lie in -23 .. 13 (fp16) or -100 .. 125 (bf16), so that every value
  * is one of the 16-bit type; the scale byte 255 makes a group NaN.  Pools and
  * stores of 4-bit blocks are 16-byte aligned (else PULSE_ERR_INVALID_ARG from
- * the recall, the attention and the layer-step).  The entry points that take
- * these types: pulse_block_bytes, pulse_workspace_bytes,
- * pulse_build_digests, the selections,
+ * the recall, the attention, the layer-step and the scheduler).
+ * The entry points that take these types: pulse_block_bytes,
+ * pulse_workspace_bytes, pulse_build_digests, the selections,
  * pulse_recall_gather, pulse_release_recalled, pulse_sparse_decode_attn,
  * pulse_attention_workgroups, pulse_decode_layer(_noalloc), the offload layers
- * of pulse_irq_step (without an engine), pulse_build_tables,
- * pulse_qk_norm_rope, pulse_append_kv and pulse_load_kv.  The others return
- * what they return for a dtype that they do not know.
+ * (without an engine) and the normal layers of pulse_irq_step,
+ * pulse_build_tables, pulse_qk_norm_rope, pulse_append_kv and pulse_load_kv.
+ * The others return what they return for a dtype that they do not know.
  */
 #ifndef PULSE_H
 #define PULSE_H

@@ -319,12 +319,13 @@ struct pulse_irq {
 };
 
 static pulse_status check_normal(const pulse_normal_layer* n) {
-    PULSE_REQUIRE(n && shape_supported(&n->shape), PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(n && kv_shape_supported(&n->shape), PULSE_ERR_INVALID_ARG);
     PULSE_REQUIRE(n->B >= 1 && n->k_max >= 1 && n->max_blocks >= 1 && n->n_slots >= 1 && n->d_ff >= 1,
                   PULSE_ERR_INVALID_ARG);
     PULSE_REQUIRE(n->q && n->slot_pool && n->block_table && n->sel_idx && n->sel_cnt && n->ctx_len && n->out &&
                       n->w_gate_up && n->w_down && n->x && n->gu && n->h && n->y && n->dev_status,
                   PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(!is_kv4(n->shape.dtype) || ((uintptr_t)n->slot_pool & 15) == 0, PULSE_ERR_INVALID_ARG);
     PULSE_REQUIRE(n->ws && n->ws_bytes >= ws_layout(n->shape, n->B, n->k_max, 0).total, PULSE_ERR_WORKSPACE);
     // the FFN GEMMs load 16-byte pieces of rows of length D and d_ff
     PULSE_REQUIRE(n->d_ff % 8 == 0, PULSE_ERR_UNSUPPORTED);

@@ -377,3 +377,72 @@ def test_captured_decode_step_replays_as_eager():
         for n, (a, b) in enumerate(zip(eager.snapshot(), st.snapshot())):
             assert torch.equal(a, b), (i, n)
     assert eager.status.item() == 0 and eager.head.item() == eager.n_slots  # every slot was taken
+
+
+@pytest.mark.parametrize("ctx,shared", [(40, False), (40, True), (1500, False), (1500, True)])
+def test_resident_layer_of_a_4_bit_cache(ctx, shared):
+    """A normal layer whose cache is held in 4 bits: the attention's output, its bf16 copy (also where it lies over the
+    queries, which takes a launch of its own) and the FFN on it."""
+    say(f"\n[gpu] kv4 resident layer ctx={ctx} shared={shared}")
+    B, hq, hkv, bs, F = 3, 8, 2, 16, 264
+    st = Run([ctx - r for r in range(B)], 0, hq, hkv, bs, P.PULSE_BF16_KV4, torch.bfloat16, 7)
+    x = st.rows(sum(ctx - r for r in range(B)))
+    st.buffers(x.shape[0])
+    st.write(x)
+    q = torch.randn((B, hq, D), device=DEV).bfloat16()
+    st.q = q
+    st.attend()
+    want, want_lse = st.out.clone(), st.lse.clone()
+    assert st.status.item() == 0
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    wgu, wd = (torch.randn(s, generator=gen, device=DEV).mul_(0.02).bfloat16() for s in ((2 * F, hq * D), (hq * D, F)))
+    bufs = {k: torch.zeros((B, n), dtype=torch.bfloat16, device=DEV) for k, n in (("x", hq * D), ("gu", 2 * F), ("h", F),
+                                                                                  ("y", hq * D))}
+    q2 = q.clone()
+    xb = q2 if shared else bufs["x"]
+    cnt = (st.blk[1:] - st.blk[:-1]).int()
+    out, lse = torch.zeros_like(want), torch.zeros_like(want_lse)
+    n = P.pulse_normal_layer()
+    n.shape, n.B, n.n_slots, n.max_blocks, n.k_max, n.sm_scale, n.d_ff, n.ws_bytes = (
+        st.sh, B, st.n_slots, st.mb, st.mb, SCALE, F, st.ws.numel())
+    for f, t in dict(q=q2, slot_pool=st.pool, block_table=st.table, sel_idx=st.sel, sel_cnt=cnt, ctx_len=st.ctx, out=out,
+                     lse=lse, ws=st.ws, w_gate_up=wgu, w_down=wd, x=xb, gu=bufs["gu"], h=bufs["h"], y=bufs["y"],
+                     dev_status=st.status).items():
+        setattr(n, f, t.data_ptr())
+    # one offload layer beside it, of the same cache type
+    kv = torch.randn((2, 4, hkv, bs, D)).bfloat16()
+    store = host_store(plain64.pack(kv[0], kv[1], bs))
+    dig = torch.zeros((4, 2, D), dtype=torch.bfloat16, device=DEV)
+    o = dict(ctx_len=dev([64]), blk_off=dev([0, 4], torch.int64), q=q[:1].contiguous(), digests=dig, k_mid=dev([4]),
+             sel_idx=dev([[0] * 4]), sel_cnt=dev([0]), block_table=dev([[-1] * 4]), free_slots=dev(np.arange(4)),
+             free_head=dev([0]), slot_pool=torch.zeros((4, P.pulse_block_bytes(st.sh)), dtype=torch.uint8, device=DEV),
+             stats=torch.zeros(2, dtype=torch.int64, device=DEV), out=torch.zeros((1, hq, D), device=DEV),
+             dev_status=st.status)
+    nb = P.pulse_workspace_bytes(st.sh, 1, 4, 4)
+    ws = torch.zeros(nb, dtype=torch.uint8, device=DEV)
+    a = P.pulse_layer_args()
+    a.shape, a.B, a.total_blocks, a.k_max, a.max_blocks, a.n_free, a.n_slots, a.sm_scale = st.sh, 1, 4, 4, 4, 4, 4, SCALE
+    a.host_kv, a.ws, a.ws_bytes = store.ptr, ws.data_ptr(), nb
+    for f, t in o.items():
+        setattr(a, f, t.data_ptr())
+    sched = P.IrqScheduler(torch.cuda.Stream(), torch.cuda.Stream())
+    torch.cuda.synchronize()
+    stats, _ = sched.step([a], [n], mode="blocking")
+    torch.cuda.synchronize()
+    assert st.status.item() == 0 and stats["normal_layers"] == 1
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    assert torch.equal(xb.view(B, hq, D), want.bfloat16())
+    xd, g64 = xb.view(B, -1).double().cpu(), wgu.double().cpu()
+    # one rounding to bf16 and fp32 sums of products
+    for got, ref, mass in ((bufs["gu"], xd @ g64.T, xd.abs() @ g64.abs().T),
+                           (bufs["y"], bufs["h"].double().cpu() @ wd.double().cpu().T,
+                            bufs["h"].double().cpu().abs() @ wd.double().cpu().abs().T)):
+        assert ((got.double().cpu() - ref).abs() <= 2.0**-8 * ref.abs() + 2.0**-20 * mass).all()
+    sched.destroy()
+    store.free()
+    n.slot_pool += 8
+    s2 = P.IrqScheduler(torch.cuda.Stream(), torch.cuda.Stream())
+    with pytest.raises(P.PulseError) as e:
+        s2.step([a], [n], mode="blocking")
+    assert e.value.status == P.PULSE_ERR_INVALID_ARG
+    s2.destroy()
