@@ -44,7 +44,12 @@ constexpr int kCombineThreads = kHeadDim;
 
 // Waves per workgroup (attn_waves): 8 while the LDS merge buffer (waves x G x
 // 128 floats) stays within 32 KiB, else 4.  Fewer, wider workgroups leave
-// fewer partials for the combine kernel.
+// fewer partials for the combine kernel.  A 4-bit cache takes 8 for the larger
+// groups too (64 KiB): its waves wait for instructions more than for loads.
+// In us, 4 waves and 8, G = 16: one request of 400 tokens 12.1 and 10.9, of
+// 4K 13.6 and 12.8; 16 of 4K 17.5 and 14.5; 4 of 64K 35.5 and 26.6 (blocks of
+// 64, whose shortest split is two steps: 1.5K 11.9 and 13.3, 16 of 4K 22.8 and
+// 19.9).
 
 // Entries of one 32-token step, and of the shortest split.
 static int32_t split_step(int32_t bs) { return bs >= kChunkTokens ? 1 : kChunkTokens / bs; }
@@ -54,7 +59,7 @@ static int32_t split_least(const pulse_shape& s) {
     const int t = (is_kv4(s.dtype) ? 1 : 2) * kChunkTokens;
     return s.block_size >= t ? 1 : t / s.block_size;
 }
-int attn_waves(const pulse_shape& s) { return s.num_q_heads / s.num_kv_heads <= 8 ? 8 : 4; }
+int attn_waves(const pulse_shape& s) { return s.num_q_heads / s.num_kv_heads <= 8 || is_kv4(s.dtype) ? 8 : 4; }
 
 struct SplitArgs {
     int32_t eps, n_wg;    // host plan: entries per wave, workgroups per (request, KV head)
@@ -788,7 +793,7 @@ hipError_t launch_attention(const pulse_shape& s, const void* q, const void* poo
 #define PULSE_ATTN_KV4(DT, BS)                \
     if (G <= 4) PULSE_ATTN(DT, BS, 8, 4);      \
     else if (G <= 8) PULSE_ATTN(DT, BS, 8, 8); \
-    else PULSE_ATTN(DT, BS, 4, 16)
+    else PULSE_ATTN(DT, BS, 8, 16)
 #define PULSE_ATTN_BS(WHICH, DT)                   \
     if (s.block_size == 16) { WHICH(DT, 16); }      \
     else if (s.block_size == 32) { WHICH(DT, 32); } \
