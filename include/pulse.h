@@ -376,7 +376,7 @@ PULSE_API pulse_status pulse_gs_last_timing(pulse_gs_engine* engine, float* ms3)
  *   lse[r][hq] = log sum_t exp(logit_t)              (fp32, optional)
  * An empty selection gives out = 0 and lse = -inf.  Products and sums are
  * accumulated in fp32.  The order of a request's sums depends on B, the shape
- * and k_max and, for 2 to 64 requests whose counts are not all k_max, may depend on
+ * and k_max and, for 2 to 64 requests (256 with a 4-bit cache) whose counts are not all k_max, may depend on
  * every request's sel_cnt: the last bits of a request's results may change with its
  * neighbours' counts.  The same call repeats its bits.
  *   out          device float [B][Hq][d];  lse optional device float [B][Hq]
@@ -393,8 +393,9 @@ PULSE_API pulse_status pulse_sparse_decode_attn(const pulse_shape* shape, const 
  * Split-K workgroups per (request, KV head) that pulse_sparse_decode_attn,
  * and the attention of pulse_decode_layer, launch for a batch of B requests
  * with at most k_max selected blocks each (it depends on B, the shape and k_max
- * only; up to 64 requests whose counts differ may share these workgroups out
- * by their counts).  Above 1, a kernel that merges the workgroups' partials
+ * only; up to 64 requests, 256 with a 4-bit cache, whose counts differ may share
+ * these workgroups out by their counts, and with a 4-bit cache and equal counts
+ * some of them may stay without work).  Above 1, a kernel that merges the workgroups' partials
  * follows the split-K kernel, and pulse_layer_args.attn_split_event marks the
  * end of the split-K kernel alone.  At 1, one workgroup covers each (request,
  * KV head) and writes out / lse itself: no merge kernel runs, so a caller that

@@ -83,7 +83,7 @@ size_t pulse_workspace_bytes(const pulse_shape* shape, int32_t B, int32_t k_max,
 int32_t pulse_attention_workgroups(const pulse_shape* shape, int32_t B, int32_t k_max) {
     if (!kv_shape_supported(shape) || B < 1 || k_max < 1) return 0;
     const AttnPlan p = attn_plan(*shape, B, k_max);
-    const int W = attn_waves(*shape);
+    const int W = attn_waves(*shape, B, k_max);
     return (p.n_split + W - 1) / W;
 }
 

@@ -29,6 +29,8 @@
 // write-back on gfx950 measured at about 9 ns per workgroup, plus a merge on
 // the kernel's tail and counters that start at zero in the workspace: it would
 // save well under the combine launch's 3.6 us.)
+#include <algorithm>
+
 #include "kv4.h"
 
 namespace pulse {
@@ -36,10 +38,6 @@ namespace pulse {
 #ifndef PULSE_ATTN_TARGET_WAVES
 #define PULSE_ATTN_TARGET_WAVES 2048
 #endif
-// Steps of a wave up to which one workgroup takes a whole request and head of a 4-bit cache, so that no merge
-// launch follows.  In us, split as far as 2048 waves go and kept together: 272 tokens 9.9 and 7.6, 400 9.9 and 8.7,
-// 600 9.9 and 9.9 (16 requests of them 12.7 and 11.0), 1040 (five steps) 10.0 and 12.2.
-constexpr int kKv4OneSteps = 4;
 constexpr int kCombineThreads = kHeadDim;
 
 // Waves per workgroup (attn_waves): 8 while the LDS merge buffer (waves x G x
@@ -47,9 +45,32 @@ constexpr int kCombineThreads = kHeadDim;
 // fewer partials for the combine kernel.  A 4-bit cache takes 8 for the larger
 // groups too (64 KiB): its waves wait for instructions more than for loads.
 // In us, 4 waves and 8, G = 16: one request of 400 tokens 12.1 and 10.9, of
-// 4K 13.6 and 12.8; 16 of 4K 17.5 and 14.5; 4 of 64K 35.5 and 26.6 (blocks of
-// 64, whose shortest split is two steps: 1.5K 11.9 and 13.3, 16 of 4K 22.8 and
-// 19.9).
+// 4K 13.6 and 12.8; 16 of 4K 17.5 and 14.5; 4 of 64K 35.5 and 26.6.  In blocks
+// of 64, whose shortest split is two steps, calls of few splits take 4, on
+// twice the CUs: 1.5K tokens 11.9 and 13.3, 8 of 2K (1024 splits) 14.0 and
+// 14.8, 16 of 4K 22.8 and 19.9.
+constexpr int kKv4Waves = 8;
+
+// Selected blocks up to which one workgroup takes a whole request and head of a 4-bit cache, so that no merge
+// launch follows: 2 to 4 steps of its waves, the more the more workgroups wait for the memory, the fewer the larger
+// the groups.  In us, split as far as 2048 waves go and kept together, 2, 3 and 4 steps (500, 760 and 1016 tokens):
+//   1 request, 8 heads of 1      9.3  8.0   9.1  9.0   9.2 10.1
+//   9 requests, 8 heads of 8    13.4 12.3  12.4 12.3  13.8 13.7
+//   24 requests, 8 heads of 4   15.4 12.0  17.5 12.2  17.4 13.6
+//   8 requests, 1 head of 16    11.8 11.5  12.9 14.6  13.1 16.7
+static int32_t kv4_one_entries(const pulse_shape& s, int64_t units) {
+    const int steps = units > 64 ? 4 : s.num_q_heads > 8 * s.num_kv_heads ? 2 : 3;
+    return kKv4Waves * steps * kChunkTokens / s.block_size;
+}
+
+int attn_waves(const pulse_shape& s, int32_t B, int32_t k_max) {
+    if (s.num_q_heads / s.num_kv_heads <= 8) return 8;
+    if (!is_kv4(s.dtype)) return 4;
+    const int64_t units = (int64_t)B * s.num_kv_heads;
+    const bool few = s.block_size > kChunkTokens && k_max > kv4_one_entries(s, units) &&
+                     units * k_max <= PULSE_ATTN_TARGET_WAVES / 2;
+    return few ? 4 : kKv4Waves;
+}
 
 // Entries of one 32-token step, and of the shortest split.
 static int32_t split_step(int32_t bs) { return bs >= kChunkTokens ? 1 : kChunkTokens / bs; }
@@ -59,13 +80,15 @@ static int32_t split_least(const pulse_shape& s) {
     const int t = (is_kv4(s.dtype) ? 1 : 2) * kChunkTokens;
     return s.block_size >= t ? 1 : t / s.block_size;
 }
-int attn_waves(const pulse_shape& s) { return s.num_q_heads / s.num_kv_heads <= 8 || is_kv4(s.dtype) ? 8 : 4; }
 
 struct SplitArgs {
     int32_t eps, n_wg;    // host plan: entries per wave, workgroups per (request, KV head)
+    int32_t even, n_even; // the same where every request has k_max blocks
     int32_t step, least;  // granularity and least value of eps
+    int32_t most;         // largest eps of a plan
     int32_t fit;          // pieces that a plan may have
-    bool planned;         // share the grid out by the counts
+    bool planned;         // look whether the counts are equal
+    bool share;           // and if not, share the grid out by them
     bool light_last;      // every (request, KV head)'s last workgroup has fewer waves: start those last
 };
 
@@ -96,6 +119,20 @@ struct SplitArgs {
 //   5 requests, 3 KV heads, around 702 tokens                          11.3  12.1  10.9
 constexpr int kPlanRequests = 64;
 
+// With a 4-bit cache a step is short and a second workgroup on a CU costs more than half as much again, so its calls
+// keep to one round more strictly.  Where all counts are k_max and the host's split takes more than a round, the
+// splits are `even`, the shortest that fit one round, unless the second workgroups are so light that even * W >
+// eps * (W + their waves).  Where the host's pieces do not fit, a plan may take up to `most` = 64 entries per wave.
+// And up to 256 requests are planned (four per lane), from 4K tokens on: the longer search costs 1 to 2 us.  In us,
+// split and planned like a 16-bit cache and as it is, requests x tokens (up to 17 requests 32 query heads over 8 KV
+// heads, from 48 on 8 over 1), r: lognormal around the number:
+//   9 x 12K         41.6 33.7    48 x 4K         22.1 17.9    72 x 1.5K r     24.3 20.7
+//   11 x 4K         27.6 22.3    48 x 12K r      35.3 25.9    72 x 4K r       25.4 27.8
+//   17 x 1.5K       21.0 18.2    88 x 4K         32.8 24.6    112 x 4K r      39.6 34.7
+//   17 x 12K r      52.5 39.7    136 x 1.5K      25.2 19.9    136 x 1.5K r    47.7 27.4
+constexpr int kPlanRequestsKv4 = 256;
+constexpr int kPlanTokensKv4 = 4096;
+
 struct Piece {
     int eps, nwg, base;  // entries per wave, workgroups of the request, its first piece
     int r, wg;
@@ -114,36 +151,91 @@ __device__ inline int pieces_short(int c, int per) {
     return max(1, q);
 }
 
-// Whether every request has k_max blocks (raw: sel_cnt of request `lane`): the host's split as it is.
-__device__ inline bool equal_counts(int32_t raw, int32_t B, int32_t k_max, int lane) {
-    return __ballot(lane < B && raw != k_max) == 0;
-}
+// The counts of a plan: lane l holds those of requests R * l .. R * l + R - 1, 0 behind the last.
+template <int R>
+struct Counts {
+    int32_t raw[R];
+    __device__ explicit Counts(const int32_t* __restrict__ sel_cnt, int32_t B, int lane) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) raw[i] = R * lane + i < B ? sel_cnt[R * lane + i] : 0;
+    }
+    // any(f(raw)) over the requests
+    template <class F>
+    __device__ bool any(int32_t B, int lane, F f) const {
+        bool a = false;
+#pragma unroll
+        for (int i = 0; i < R; ++i) a |= R * lane + i < B && f(raw[i]);
+        return __ballot(a) != 0;
+    }
+    // Whether every request has k_max blocks: the host's split as it is.
+    __device__ bool equal(int32_t B, int32_t k_max, int lane) const {
+        return !any(B, lane, [&](int32_t c) { return c != k_max; });
+    }
+};
 
-// Plan for piece index pr (of all heads of a request at once); all lanes of a wave take
-// part.  raw: sel_cnt of request `lane` (B <= kPlanRequests).  r < 0: no such piece.
-__device__ inline Piece plan_piece(int pr, int32_t raw, int32_t B, int32_t k_max, int32_t W, const SplitArgs& sp,
-                                   int lane) {
-    const int c = (lane < B && raw >= 0 && raw <= k_max) ? raw : 0;
-    Piece p;
-    auto pieces = [&](int eps) { return lane < B ? (uint32_t)pieces_short(c, W * eps) : 0u; };
+// Plan for piece index pr (of all heads of a request at once), or, with pr < 0, for the first piece of request
+// `req`; all lanes of a wave take part.  r < 0: no such piece.
+template <int R>
+__device__ inline Piece plan_piece(int pr, int req, const Counts<R>& counts, int32_t B, int32_t k_max, int32_t W,
+                                   const SplitArgs& sp, int lane) {
+    int c[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) c[i] = counts.raw[i] >= 0 && counts.raw[i] <= k_max ? counts.raw[i] : 0;
+    uint32_t np[R];
+    auto pieces = [&](int eps) {
+        uint32_t n = 0;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            np[i] = R * lane + i < B ? (uint32_t)pieces_short(c[i], W * eps) : 0u;
+            n += np[i];
+        }
+        return n;
+    };
     auto sum = [&](int eps) { return (int)last_lane(wave_scan(pieces(eps), 0u, OpAdd())); };
-    const int fit = sum(sp.eps) <= sp.fit ? sp.fit : B * sp.n_wg;
-    int lo = sp.least, hi = sp.eps;  // hi fits: no request has more than n_wg workgroups then
+    int fit = sp.fit, lo = sp.least, hi = sp.eps;
+    if (sum(sp.eps) > sp.fit) {
+        if (sp.most > sp.eps && sum(sp.most) <= sp.fit) {
+            lo = sp.eps;
+            hi = sp.most;
+        } else {
+            fit = B * sp.n_wg;  // no request has more than n_wg workgroups
+        }
+    }
     while (lo < hi) {
         const int mid = (lo + hi) / 2 / sp.step * sp.step;
         if (sum(mid) <= fit) hi = mid;
         else lo = mid + sp.step;
     }
+    Piece p;
     p.eps = hi;
-    const uint32_t np = pieces(p.eps);
-    const uint32_t incl = wave_scan(np, 0u, OpAdd());
-    const int before = __popcll(__ballot(lane < B && (int)(incl - np) <= pr));
-    p.r = pr < (int)last_lane(incl) ? before - 1 : -1;
-    const int at = max(p.r, 0);
-    p.nwg = __builtin_amdgcn_readlane((int)np, at);
-    p.base = __builtin_amdgcn_readlane((int)(incl - np), at);
-    p.cnt = __builtin_amdgcn_readlane(c, at);
-    p.wg = pr - p.base;
+    const uint32_t own = pieces(p.eps);
+    const uint32_t incl = wave_scan(own, 0u, OpAdd());
+    int at, first;  // the lane whose requests hold the piece, and the piece's or the request's place among theirs
+    if (pr >= 0) {
+        at = __popcll(__ballot((int)incl <= pr));
+        if (at >= kWave) {
+            p.r = -1;
+            return p;
+        }
+        first = pr - (int)(__builtin_amdgcn_readlane((int)incl, at) - __builtin_amdgcn_readlane((int)own, at));
+    } else {
+        at = req / R;
+        first = 0;
+    }
+    p.base = __builtin_amdgcn_readlane((int)(incl - own), at);
+    p.r = R * at;
+    p.nwg = __builtin_amdgcn_readlane((int)np[0], at);
+    p.cnt = __builtin_amdgcn_readlane(c[0], at);
+#pragma unroll
+    for (int i = 1; i < R; ++i) {
+        if (pr >= 0 ? first < p.nwg : R * at + i > req) break;
+        first -= p.nwg;
+        p.base += p.nwg;
+        p.r = R * at + i;
+        p.nwg = __builtin_amdgcn_readlane((int)np[i], at);
+        p.cnt = __builtin_amdgcn_readlane(c[i], at);
+    }
+    p.wg = pr >= 0 ? first : 0;
     return p;
 }
 
@@ -529,8 +621,9 @@ __device__ inline void attend_split_kv4(const uint16_t* __restrict__ q, const ui
 // grid = (Hkv, n_wg, B), or (Hkv, B, n_wg) with light_last; in either, workgroup p is piece p / Hkv of KV head
 // p % Hkv of a plan; wave w of a request's workgroup wg owns split W * wg + w of eps entries.  Dynamic LDS:
 // O [W][G][128] floats then (m, l) [W][G] float2.
-// GP: rows of the P operand that a channel group of the 4-bit cache takes.
-template <int DT, int BS, int W, int GP>
+// GP: rows of the P operand that a channel group of the 4-bit cache takes.  R: counts per lane of a plan (a kernel
+// that held both plans was 1 to 2% slower for fetching its way past the other).
+template <int DT, int BS, int W, int GP, int R>
 __global__ __launch_bounds__(W * kWave) void attn_splitk_kernel(
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ pool, int32_t n_slots,
     const int32_t* __restrict__ table, int32_t max_blocks, const int32_t* __restrict__ sel_idx,
@@ -551,7 +644,7 @@ __global__ __launch_bounds__(W * kWave) void attn_splitk_kernel(
     Piece p;
     p.r = sp.light_last ? blockIdx.y : blockIdx.z;
     p.wg = sp.light_last ? blockIdx.z : blockIdx.y;
-    p.eps = sp.eps;
+    p.eps = is_kv4(DT) ? sp.even : sp.eps;
     int piece = p.r * sp.n_wg + p.wg;
     const bool planned = sp.planned;
     auto load_j = [&]() {
@@ -559,20 +652,32 @@ __global__ __launch_bounds__(W * kWave) void attn_splitk_kernel(
         return (lane < p.eps && e < k_max) ? sel_idx[(size_t)p.r * k_max + e] : -1;
     };
     int32_t j_lane = load_j();
+    bool own = !planned;  // the host's split, cut at the request's own count
     if (planned) {
-        const int32_t raw = lane < B ? sel_cnt[lane] : 0;
-        if (piece == 0 && h == 0 && wave == 0 && (raw < 0 || raw > k_max)) report(status, PULSE_ERR_BAD_INDEX);
+        const Counts<R> counts(sel_cnt, B, lane);
+        if (piece == 0 && h == 0 && wave == 0 && counts.any(B, lane, [&](int32_t c) { return c < 0 || c > k_max; }) &&
+            lane == 0)
+            report(status, PULSE_ERR_BAD_INDEX);
         p.cnt = k_max;
-        p.nwg = sp.n_wg;
-        if (!equal_counts(raw, B, k_max, lane)) {
-            const int r0 = p.r, wg0 = p.wg;
+        p.nwg = is_kv4(DT) ? sp.n_even : sp.n_wg;
+        if (counts.equal(B, k_max, lane)) {
+            if (is_kv4(DT) && p.wg >= p.nwg) return;
+        } else if (is_kv4(DT) && !sp.share) {
+            own = true;
+        } else {
+            const int r0 = p.r, wg0 = p.wg, eps0 = p.eps;
             piece = (int)(blockIdx.z * gridDim.y + blockIdx.y);
-            p = plan_piece(piece, raw, B, k_max, W, sp, lane);
+            p = plan_piece(piece, 0, counts, B, k_max, W, sp, lane);
             if (p.r < 0) return;  // fewer pieces than workgroups
-            if (p.r != r0 || p.wg != wg0 || p.eps != sp.eps) j_lane = load_j();
+            if (p.r != r0 || p.wg != wg0 || p.eps != eps0) j_lane = load_j();
         }
-    } else {
+    }
+    if (own) {
         p.cnt = sel_cnt[p.r];
+        if (is_kv4(DT) && p.eps != sp.eps) {
+            p.eps = sp.eps;
+            j_lane = load_j();
+        }
         if (p.cnt < 0 || p.cnt > k_max) {
             if (tid == 0) report(status, PULSE_ERR_BAD_INDEX);
             p.cnt = 0;
@@ -648,13 +753,16 @@ __global__ __launch_bounds__(W * kWave) void attn_splitk_kernel(
 // are read 8 at a time (16 independent loads per thread) and merged online.
 // Requests whose selection fits one workgroup were finished by the attention
 // kernel.
+// R: counts per lane of a plan.
+template <int R>
 __global__ __launch_bounds__(kCombineThreads) void attn_combine_kernel(
     const float* __restrict__ ws_o, const float2* __restrict__ ws_ml, const int32_t* __restrict__ sel_cnt,
     int32_t k_max, int32_t B, int32_t Hq, int32_t Hkv, int32_t G, SplitArgs sp, int32_t waves,
     float* __restrict__ out, float* __restrict__ lse, __bf16* __restrict__ x) {
     const int c = threadIdx.x, g = blockIdx.x, h = blockIdx.y, r = blockIdx.z;
     // piece i of this (request, head) is partial (base + i) * Hkv + h; with equal counts base = r * n_wg.
-    // The first 8 are loaded there before the counts are known, and again if the base differs.
+    // The first 8 are loaded there before the counts are known, and again if the base differs (later where equal
+    // counts leave nothing to merge).
     const float2* ml = ws_ml + (size_t)h * G + g;
     const float* po = ws_o + ((size_t)h * G + g) * kHeadDim + c;
     float2 mlv[8];
@@ -667,26 +775,30 @@ __global__ __launch_bounds__(kCombineThreads) void attn_combine_kernel(
             ov[i] = i < n ? po[u * kHeadDim] : 0.f;
         }
     };
-    load8(r * sp.n_wg, sp.n_wg);
+    const bool ahead = sp.n_even > 1;
+    if (ahead) load8(r * sp.n_wg, sp.n_wg);
     int nwg, base = r * sp.n_wg;
+    bool own = !sp.planned;
     if (sp.planned) {
         const int lane = c & 63;
-        const int32_t raw = lane < B ? sel_cnt[lane] : 0;
-        nwg = sp.n_wg;
-        if (!equal_counts(raw, B, k_max, lane)) {
-            const Piece p = plan_piece(0, raw, B, k_max, waves, sp, lane);
-            // the request's own pieces: those of lane r
-            const int cl = (raw >= 0 && raw <= k_max) ? raw : 0;
-            const uint32_t np = (uint32_t)pieces_short(cl, waves * p.eps);
-            nwg = __builtin_amdgcn_readlane((int)np, r);
-            base = (int)last_lane(wave_scan(lane < r ? np : 0u, 0u, OpAdd()));
+        const Counts<R> counts(sel_cnt, B, lane);
+        nwg = sp.n_even;
+        if (!counts.equal(B, k_max, lane)) {
+            if (sp.share) {
+                const Piece p = plan_piece(-1, r, counts, B, k_max, waves, sp, lane);
+                nwg = p.nwg;
+                base = p.base;
+            } else {
+                own = true;
+            }
         }
-    } else {
+    }
+    if (own) {
         const int32_t cnt = sel_cnt[r];
         nwg = (cnt < 0 || cnt > k_max) ? 1 : pieces_of(cnt, waves * sp.eps);
     }
     if (nwg <= 1) return;
-    if (base != r * sp.n_wg || nwg > sp.n_wg) load8(base, nwg);
+    if (!ahead || base != r * sp.n_wg || nwg > sp.n_wg) load8(base, nwg);
     float m_run = -INFINITY, L = 0.f, a = 0.f;
     for (int w0 = 0; w0 < nwg; w0 += 8) {
         if (w0 > 0) {
@@ -734,8 +846,7 @@ AttnPlan attn_plan(const pulse_shape& s, int32_t B, int32_t k_max) {
     if (want > max_split) want = max_split;
     if (want < 1) want = 1;
     if (is_kv4(s.dtype)) {
-        const int64_t W = attn_waves(s);
-        if (want > W && k_max <= W * kKv4OneSteps * kChunkTokens / s.block_size) want = W;
+        if (want > kKv4Waves && k_max <= kv4_one_entries(s, units)) want = kKv4Waves;
     }
     int64_t eps = (k_max + want - 1) / want;
     eps = ((eps + step - 1) / step) * step;
@@ -754,7 +865,10 @@ static void launch_attn_t(dim3 grid, size_t lds, hipStream_t st, hipEvent_t done
                           const int32_t* sel_cnt, int32_t k_max, const int32_t* ctx_len, int32_t B, int32_t Hq,
                           int32_t Hkv, int32_t G, const SplitArgs& sp, float scale_log2, float* ws_o, float2* ws_ml,
                           float* out, float* lse, __bf16* x, int32_t* status) {
-    launch_timed(attn_splitk_kernel<DT, BS, W, GP>, grid, dim3(W * kWave), (uint32_t)lds, st, nullptr, done,
+    constexpr int kMany = is_kv4(DT) ? kPlanRequestsKv4 / kWave : 1;
+    const auto kernel =
+        B <= kPlanRequests ? attn_splitk_kernel<DT, BS, W, GP, 1> : attn_splitk_kernel<DT, BS, W, GP, kMany>;
+    launch_timed(kernel, grid, dim3(W * kWave), (uint32_t)lds, st, nullptr, done,
                  (const uint16_t*)q, (const uint16_t*)pool, n_slots, table, max_blocks, sel_idx, sel_cnt, k_max,
                  ctx_len, B, Hq, Hkv, G, sp, scale_log2, ws_o, ws_ml, out, lse, x, status);
 }
@@ -767,7 +881,7 @@ hipError_t launch_attention(const pulse_shape& s, const void* q, const void* poo
     if (B == 0) return hipSuccess;
     const int32_t Hkv = s.num_kv_heads, Hq = s.num_q_heads, G = Hq / Hkv;
     const AttnPlan p = attn_plan(s, B, k_max);
-    const int W = attn_waves(s);
+    const int W = attn_waves(s, B, k_max);
     const int32_t n_wg = (p.n_split + W - 1) / W;
     SplitArgs sp;
     sp.eps = p.entries_per_split;
@@ -777,8 +891,27 @@ hipError_t launch_attention(const pulse_shape& s, const void* q, const void* poo
     const int64_t all = (int64_t)B * n_wg;
     const int32_t round = PULSE_ATTN_TARGET_WAVES / (W * Hkv);  // pieces of one round
     sp.fit = (int32_t)(4 * (int64_t)round >= 5 * (int64_t)B && round < all ? round : all);
-    sp.planned = n_wg > 1 && B <= kPlanRequests && (sp.eps >= 2 * sp.least || all > round) && k_max <= (1 << 22);
-    sp.light_last = p.n_split % W != 0 && all > round && n_wg <= 65535;
+    sp.even = sp.eps;  // (other than eps only where all > round and eps < 64, hence under a plan)
+    sp.n_even = n_wg;
+    sp.most = sp.eps;
+    if (is_kv4(s.dtype)) {
+        sp.most = 64;
+        const int32_t each = B <= kPlanRequestsKv4 ? round / B : 0;  // workgroups of a request in one round
+        if (each >= 1 && n_wg > each) {
+            const int64_t eps = ((int64_t)k_max + W * each - 1) / (W * each);
+            const int32_t even = (int32_t)std::min<int64_t>((eps + sp.step - 1) / sp.step * sp.step, sp.most);
+            const int32_t last = (p.n_split - 1) % W + 1;  // waves of a request's last workgroup
+            if ((int64_t)even * W <= (int64_t)sp.eps * (W + last)) {
+                sp.even = even;
+                sp.n_even = (int32_t)((((int64_t)k_max + even - 1) / even + W - 1) / W);
+            }
+        }
+    }
+    sp.share = B <= kPlanRequests || (int64_t)k_max * s.block_size >= kPlanTokensKv4;
+    if (B <= kPlanRequests) sp.planned = sp.eps >= 2 * sp.least || all > round;
+    else sp.planned = is_kv4(s.dtype) && B <= kPlanRequestsKv4 && (sp.share || sp.even != sp.eps);
+    sp.planned = sp.planned && n_wg > 1 && k_max <= (1 << 22);
+    sp.light_last = (p.n_split % W != 0 || sp.even != sp.eps) && all > round && n_wg <= 65535;
     const dim3 grid = sp.light_last ? dim3((unsigned)Hkv, (unsigned)B, (unsigned)n_wg)
                                     : dim3((unsigned)Hkv, (unsigned)n_wg, (unsigned)B);
     const size_t lds = sizeof(float) * W * G * kHeadDim + sizeof(float2) * W * G;
@@ -793,7 +926,8 @@ hipError_t launch_attention(const pulse_shape& s, const void* q, const void* poo
 #define PULSE_ATTN_KV4(DT, BS)                \
     if (G <= 4) PULSE_ATTN(DT, BS, 8, 4);      \
     else if (G <= 8) PULSE_ATTN(DT, BS, 8, 8); \
-    else PULSE_ATTN(DT, BS, 8, 16)
+    else if (W == 8) PULSE_ATTN(DT, BS, 8, 16); \
+    else PULSE_ATTN(DT, 64, 4, 16)
 #define PULSE_ATTN_BS(WHICH, DT)                   \
     if (s.block_size == 16) { WHICH(DT, 16); }      \
     else if (s.block_size == 32) { WHICH(DT, 32); } \
@@ -809,9 +943,9 @@ hipError_t launch_attention(const pulse_shape& s, const void* q, const void* poo
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (n_wg <= 1) return (done && split_done) ? hipEventRecord(done, st) : hipSuccess;
-    launch_timed(attn_combine_kernel, dim3((unsigned)G, (unsigned)Hkv, (unsigned)B), dim3(kCombineThreads), 0u, st,
-                 nullptr, done, (const float*)ws_o, (const float2*)ws_ml, sel_cnt, k_max, B, Hq, Hkv, G, sp, W, out, lse,
-                 x);
+    const auto combine = B <= kPlanRequests ? attn_combine_kernel<1> : attn_combine_kernel<kPlanRequestsKv4 / kWave>;
+    launch_timed(combine, dim3((unsigned)G, (unsigned)Hkv, (unsigned)B), dim3(kCombineThreads), 0u, st, nullptr, done,
+                 (const float*)ws_o, (const float2*)ws_ml, sel_cnt, k_max, B, Hq, Hkv, G, sp, W, out, lse, x);
     return hipGetLastError();
 }
 

@@ -264,6 +264,16 @@ ATTEND = [
     ([3000, 2999, 17, 1], [40, 94, 1, 1], 28, 4, 32, "bf16"),
     ([1000] * 70, [5] * 70, 2, 2, 64, "bf16"),
     ([9000], [563], 8, 8, 16, "bf16"),
+    # more than a round of workgroups: equal counts in one and in two workgroups each, counts that fit a round with
+    # more entries per wave, more requests than lanes, as many as a plan takes, one more
+    ([1050] * 24, [66] * 24, 8, 8, 16, "bf16"),
+    ([2100] * 12, [132] * 12, 16, 8, 16, "f16"),
+    ([2100] + [1900] * 11, [132] + [119] * 11, 8, 8, 16, "bf16"),
+    ([1300] * 130, [41] * 130, 2, 1, 32, "f16"),
+    ([3200] + [16 * (7 * i % 60) for i in range(69)], [200] + [7 * i % 60 for i in range(69)], 2, 2, 16, "bf16"),
+    ([32 * (11 * i % 50) + 32 for i in range(199)] + [4000], [11 * i % 50 + 1 for i in range(199)] + [125], 16, 1, 32, "f16"),
+    ([16 * (5 * i % 77) for i in range(256)], [5 * i % 77 for i in range(256)], 1, 1, 16, "bf16"),
+    ([16 * (5 * i % 77) for i in range(257)], [5 * i % 77 for i in range(257)], 1, 1, 16, "f16"),
 ]
 
 
@@ -402,13 +412,35 @@ def test_any_scale(scale):
                         int(n.sum()))
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("B", [3, 64, 100])
+def test_counts_out_of_range_among_others(B):
+    """Such a request has no output, whichever lane holds its count, and takes nothing from the others."""
+    ctx, cnt = [1600 + 16 * (r % 9) for r in range(B)], [60 + r % 41 for r in range(B)]
+    gen = torch.Generator().manual_seed(B)
+    sh, q, pool, table, sel = case_state(ctx, cnt, 2, 1, 16, "bf16", gen)
+    d = [x.to(DEV) for x in (q, pool, table, sel)]
+    bad = cnt[:]
+    bad[1], bad[B - 1] = -1, sel.shape[1] + 1
+    out, lse = attend(sh, *d, dev(bad), dev(ctx), status_want=P.PULSE_ERR_BAD_INDEX)
+    for r in range(B):
+        if r in (1, B - 1):
+            assert (out[r] == 0).all() and (lse[r] == -math.inf).all()
+            continue
+        j = sel[r, : cnt[r]].long()
+        k, v = (x.transpose(0, 1).reshape(1, -1, D) for x in plain64.unpack(pool[table[r, j].long()], 1, 16))
+        n = (j[:, None] * 16 + torch.arange(16)).view(-1) < ctx[r]
+        check_attention(out[r], lse[r], *plain64.attention(q[r], k[:, n], v[:, n], SCALE), int(n.sum()))
+
+
 def test_kv4_attention_workgroups():
-    """One workgroup, hence no merge launch, up to four 32-token steps of each of its waves (8, or 4 beyond eight query
-    heads per KV head); splits over several beyond."""
+    """One workgroup of eight waves, hence no merge launch, up to two 32-token steps of each wave (more than eight query
+    heads per KV head), three, or four (more than 64 requests and heads); splits over several beyond."""
     def groups(hq, hkv, bs, B, k):
         return P.pulse_attention_workgroups(P.make_shape(hq, hkv, D, bs, P.PULSE_BF16_KV4), B, k)
 
-    for hq, hkv, bs, k in ((32, 8, 16, 64), (64, 8, 32, 32), (64, 4, 64, 8), (8, 8, 64, 16)):
-        assert groups(hq, hkv, bs, 2, k) == 1
-        assert groups(hq, hkv, bs, 2, k + 1) > 1
+    for hq, hkv, bs, B, k in ((32, 8, 16, 2, 48), (64, 8, 32, 8, 24), (64, 4, 64, 2, 8), (8, 8, 64, 2, 12),
+                              (32, 8, 16, 9, 64), (64, 4, 64, 17, 16)):
+        assert groups(hq, hkv, bs, B, k) == 1
+        assert groups(hq, hkv, bs, B, k + 1) > 1
     assert groups(32, 8, 16, 32, 256) == 1  # 256 requests and heads take a round of workgroups between them
