@@ -192,15 +192,29 @@ __device__ inline Piece plan_piece(int pr, int req, const Counts<R>& counts, int
         return n;
     };
     auto sum = [&](int eps) { return (int)last_lane(wave_scan(pieces(eps), 0u, OpAdd())); };
+    // m = blocks / W of all requests make m / eps to m / eps + B pieces, which leaves few values of eps to try
+    // (rounded outwards by more than the 2^-21 that these floats are off; step is 1 or 2)
+    uint32_t blocks = 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) blocks += R * lane + i < B ? (uint32_t)c[i] : 0u;
+    const float m = (float)last_lane(wave_scan(blocks, 0u, OpAdd())) * __builtin_amdgcn_rcpf((float)W);
     int fit = sp.fit, lo = sp.least, hi = sp.eps;
-    if (sum(sp.eps) > sp.fit) {
-        if (sp.most > sp.eps && sum(sp.most) <= sp.fit) {
+    int enough = INT32_MAX;
+    if (fit > B) {
+        const float x = m * __builtin_amdgcn_rcpf((float)(fit - B)) * 1.000001f;
+        if (x < 64.f) enough = ((int)x + sp.step) & -sp.step;
+    }
+    if (enough <= sp.eps) {
+        hi = max(enough, sp.least);
+    } else if (sum(sp.eps) > fit) {
+        if (sp.most > sp.eps && (enough <= sp.most || sum(sp.most) <= fit)) {
             lo = sp.eps;
-            hi = sp.most;
+            hi = min(sp.most, enough);
         } else {
             fit = B * sp.n_wg;  // no request has more than n_wg workgroups
         }
     }
+    lo = max(lo, (int)(m * __builtin_amdgcn_rcpf((float)fit) * 0.999999f) & -sp.step);
     while (lo < hi) {
         const int mid = (lo + hi) / 2 / sp.step * sp.step;
         if (sum(mid) <= fit) hi = mid;
