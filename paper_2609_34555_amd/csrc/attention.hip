@@ -89,6 +89,7 @@ struct SplitArgs {
     int32_t fit;          // pieces that a plan may have
     bool planned;         // look whether the counts are equal
     bool share;           // and if not, share the grid out by them
+    bool level;           // unless they are three quarters of k_max on average
     bool light_last;      // every (request, KV head)'s last workgroup has fewer waves: start those last
 };
 
@@ -123,7 +124,7 @@ constexpr int kPlanRequests = 64;
 // keep to one round more strictly.  Where all counts are k_max and the host's split takes more than a round, the
 // splits are `even`, the shortest that fit one round, unless the second workgroups are so light that even * W >
 // eps * (W + their waves).  Where the host's pieces do not fit, a plan may take up to `most` = 64 entries per wave.
-// And up to 256 requests are planned (four per lane), from 4K tokens on: the longer search costs 1 to 2 us.  In us,
+// And up to 256 requests are planned (four per lane), from 2K tokens on: the longer search costs up to 2 us.  In us,
 // split and planned like a 16-bit cache and as it is, requests x tokens (up to 17 requests 32 query heads over 8 KV
 // heads, from 48 on 8 over 1), r: lognormal around the number:
 //   9 x 12K         41.6 33.7    48 x 4K         22.1 17.9    72 x 1.5K r     24.3 20.7
@@ -131,7 +132,13 @@ constexpr int kPlanRequests = 64;
 //   17 x 1.5K       21.0 18.2    88 x 4K         32.8 24.6    112 x 4K r      39.6 34.7
 //   17 x 12K r      52.5 39.7    136 x 1.5K      25.2 19.9    136 x 1.5K r    47.7 27.4
 constexpr int kPlanRequestsKv4 = 256;
-constexpr int kPlanTokensKv4 = 4096;
+constexpr int kPlanTokensKv4 = 2048;
+// More requests and heads than a round has workgroups: from 4K tokens on the grid has two workgroups for each, for a
+// plan to share out.  Equal counts leave the second without work, and so do, where the last round is as good as full,
+// counts of three quarters of k_max on average.  In us, one workgroup each and this (8 KV heads; 2 from 132 requests):
+//   33 x 2K r       40.0 30.5    33 x 4K        48.2 48.6    132 x 2K r      49.4 32.5    256 x 2K r      81.3 56.6
+//   64 x 4K r       89.6 83.6    64 x 4K        59.1 59.4    160 x 4K r      87.0 67.8    256 x 2K (25%)  48.2 56.5
+constexpr int kOverTokens = 4096;
 
 struct Piece {
     int eps, nwg, base;  // entries per wave, workgroups of the request, its first piece
@@ -171,6 +178,18 @@ struct Counts {
     __device__ bool equal(int32_t B, int32_t k_max, int lane) const {
         return !any(B, lane, [&](int32_t c) { return c != k_max; });
     }
+    __device__ int valid(int i, int32_t k_max) const { return raw[i] >= 0 && raw[i] <= k_max ? raw[i] : 0; }
+    // Blocks of all requests (up to 256 of up to 2^22).
+    __device__ uint32_t blocks(int32_t k_max) const {
+        uint32_t n = 0;
+#pragma unroll
+        for (int i = 0; i < R; ++i) n += (uint32_t)valid(i, k_max);
+        return last_lane(wave_scan(n, 0u, OpAdd()));
+    }
+    // Whether they have three quarters of k_max blocks on average.
+    __device__ bool level(int32_t B, int32_t k_max) const {
+        return (float)blocks(k_max) >= 0.75f * (float)B * (float)k_max;
+    }
 };
 
 // Plan for piece index pr (of all heads of a request at once), or, with pr < 0, for the first piece of request
@@ -180,7 +199,7 @@ __device__ inline Piece plan_piece(int pr, int req, const Counts<R>& counts, int
                                    const SplitArgs& sp, int lane) {
     int c[R];
 #pragma unroll
-    for (int i = 0; i < R; ++i) c[i] = counts.raw[i] >= 0 && counts.raw[i] <= k_max ? counts.raw[i] : 0;
+    for (int i = 0; i < R; ++i) c[i] = counts.valid(i, k_max);
     uint32_t np[R];
     auto pieces = [&](int eps) {
         uint32_t n = 0;
@@ -194,10 +213,7 @@ __device__ inline Piece plan_piece(int pr, int req, const Counts<R>& counts, int
     auto sum = [&](int eps) { return (int)last_lane(wave_scan(pieces(eps), 0u, OpAdd())); };
     // m = blocks / W of all requests make m / eps to m / eps + B pieces, which leaves few values of eps to try
     // (rounded outwards by more than the 2^-21 that these floats are off; step is 1 or 2)
-    uint32_t blocks = 0;
-#pragma unroll
-    for (int i = 0; i < R; ++i) blocks += R * lane + i < B ? (uint32_t)c[i] : 0u;
-    const float m = (float)last_lane(wave_scan(blocks, 0u, OpAdd())) * __builtin_amdgcn_rcpf((float)W);
+    const float m = (float)counts.blocks(k_max) * __builtin_amdgcn_rcpf((float)W);
     int fit = sp.fit, lo = sp.least, hi = sp.eps;
     int enough = INT32_MAX;
     if (fit > B) {
@@ -667,6 +683,7 @@ __global__ __launch_bounds__(W * kWave) void attn_splitk_kernel(
     };
     int32_t j_lane = load_j();
     bool own = !planned;  // the host's split, cut at the request's own count
+    int own_eps = sp.eps;
     if (planned) {
         const Counts<R> counts(sel_cnt, B, lane);
         if (piece == 0 && h == 0 && wave == 0 && counts.any(B, lane, [&](int32_t c) { return c < 0 || c > k_max; }) &&
@@ -676,8 +693,9 @@ __global__ __launch_bounds__(W * kWave) void attn_splitk_kernel(
         p.nwg = is_kv4(DT) ? sp.n_even : sp.n_wg;
         if (counts.equal(B, k_max, lane)) {
             if (is_kv4(DT) && p.wg >= p.nwg) return;
-        } else if (is_kv4(DT) && !sp.share) {
+        } else if (is_kv4(DT) && (!sp.share || (sp.level && counts.level(B, k_max)))) {
             own = true;
+            if (sp.share) own_eps = sp.even;
         } else {
             const int r0 = p.r, wg0 = p.wg, eps0 = p.eps;
             piece = (int)(blockIdx.z * gridDim.y + blockIdx.y);
@@ -688,8 +706,8 @@ __global__ __launch_bounds__(W * kWave) void attn_splitk_kernel(
     }
     if (own) {
         p.cnt = sel_cnt[p.r];
-        if (is_kv4(DT) && p.eps != sp.eps) {
-            p.eps = sp.eps;
+        if (is_kv4(DT) && p.eps != own_eps) {
+            p.eps = own_eps;
             j_lane = load_j();
         }
         if (p.cnt < 0 || p.cnt > k_max) {
@@ -793,12 +811,16 @@ __global__ __launch_bounds__(kCombineThreads) void attn_combine_kernel(
     if (ahead) load8(r * sp.n_wg, sp.n_wg);
     int nwg, base = r * sp.n_wg;
     bool own = !sp.planned;
+    int own_eps = sp.eps;
     if (sp.planned) {
         const int lane = c & 63;
         const Counts<R> counts(sel_cnt, B, lane);
         nwg = sp.n_even;
         if (!counts.equal(B, k_max, lane)) {
-            if (sp.share) {
+            if (sp.level && sp.share && counts.level(B, k_max)) {
+                own = true;
+                own_eps = sp.even;
+            } else if (sp.share) {
                 const Piece p = plan_piece(-1, r, counts, B, k_max, waves, sp, lane);
                 nwg = p.nwg;
                 base = p.base;
@@ -809,7 +831,7 @@ __global__ __launch_bounds__(kCombineThreads) void attn_combine_kernel(
     }
     if (own) {
         const int32_t cnt = sel_cnt[r];
-        nwg = (cnt < 0 || cnt > k_max) ? 1 : pieces_of(cnt, waves * sp.eps);
+        nwg = (cnt < 0 || cnt > k_max) ? 1 : pieces_of(cnt, waves * own_eps);
     }
     if (nwg <= 1) return;
     if (!ahead || base != r * sp.n_wg || nwg > sp.n_wg) load8(base, nwg);
@@ -849,6 +871,11 @@ __global__ __launch_bounds__(kCombineThreads) void attn_combine_kernel(
             m_run == -INFINITY ? -INFINITY : (m_run + log2f(L)) * 0.69314718055994531f;
 }
 
+// Whether requests and heads alone are more than a round of workgroups, and few enough for a plan.
+static bool kv4_over(const pulse_shape& s, int32_t B) {
+    return is_kv4(s.dtype) && B <= kPlanRequestsKv4 && B > PULSE_ATTN_TARGET_WAVES / (kKv4Waves * s.num_kv_heads);
+}
+
 AttnPlan attn_plan(const pulse_shape& s, int32_t B, int32_t k_max) {
     // a split covers whole 32-token steps, at least two, and at most 64 entries
     const int32_t step = split_step(s.block_size);
@@ -860,7 +887,13 @@ AttnPlan attn_plan(const pulse_shape& s, int32_t B, int32_t k_max) {
     if (want > max_split) want = max_split;
     if (want < 1) want = 1;
     if (is_kv4(s.dtype)) {
+        // All waves of a workgroup have work, however many requests there are: the CU's other workgroups do not make
+        // up for idle waves.  1000 tokens of 8 heads, in us, one round of waves and this: 64 requests 20.8 and 22.6
+        // (lognormal 41.3 and 34.7), 96 32.7 and 29.4, 128 49.8 and 36.5, 256 143 and 69.
+        want = std::max(want, std::min<int64_t>(max_split, kKv4Waves));
         if (want > kKv4Waves && k_max <= kv4_one_entries(s, units)) want = kKv4Waves;
+        if (kv4_over(s, B) && (int64_t)k_max * s.block_size >= kOverTokens)
+            want = std::max<int64_t>(want, 2 * kKv4Waves);
     }
     int64_t eps = (k_max + want - 1) / want;
     eps = ((eps + step - 1) / step) * step;
@@ -908,14 +941,18 @@ hipError_t launch_attention(const pulse_shape& s, const void* q, const void* poo
     sp.even = sp.eps;  // (other than eps only where all > round and eps < 64, hence under a plan)
     sp.n_even = n_wg;
     sp.most = sp.eps;
+    sp.level = false;
     if (is_kv4(s.dtype)) {
         sp.most = 64;
-        const int32_t each = B <= kPlanRequestsKv4 ? round / B : 0;  // workgroups of a request in one round
+        const bool over = kv4_over(s, B);
+        sp.level = over && 4 * (int64_t)((B + round - 1) / std::max(round, 1)) * round <= 5 * (int64_t)B;
+        // workgroups of a request in one round
+        const int32_t each = over ? 1 : B <= kPlanRequestsKv4 ? round / B : 0;
         if (each >= 1 && n_wg > each) {
             const int64_t eps = ((int64_t)k_max + W * each - 1) / (W * each);
             const int32_t even = (int32_t)std::min<int64_t>((eps + sp.step - 1) / sp.step * sp.step, sp.most);
             const int32_t last = (p.n_split - 1) % W + 1;  // waves of a request's last workgroup
-            if ((int64_t)even * W <= (int64_t)sp.eps * (W + last)) {
+            if (over || (int64_t)even * W <= (int64_t)sp.eps * (W + last)) {
                 sp.even = even;
                 sp.n_even = (int32_t)((((int64_t)k_max + even - 1) / even + W - 1) / W);
             }

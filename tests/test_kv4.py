@@ -413,6 +413,35 @@ def test_any_scale(scale):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("B,hq,bs,least", [(132, 4, 32, 130), (132, 2, 32, 3), (256, 2, 32, 130), (256, 2, 32, 100),
+                                           (256, 2, 64, 1), (256, 32, 64, 50), (257, 2, 32, 100)])
+def test_requests_and_heads_beyond_a_round(B, hq, bs, least):
+    """Counts of `least` to 4160 tokens (all that, three quarters and less on average) over blocks that requests share."""
+    say(f"\n[gpu] kv4 attention B={B} hq={hq} bs={bs} least={least}")
+    hkv, most, n_slots = 2, 4160 // bs, 140
+    gen = torch.Generator().manual_seed(B + bs)
+    rng = np.random.default_rng(B + bs + least)
+    kv = torch.randn((2, n_slots, hkv, bs, D), generator=gen).bfloat16()
+    pool = plain64.pack(kv[0], kv[1], bs)
+    cnt = rng.integers(min(least, most), most + 1, size=B)
+    cnt[rng.integers(B)] = most
+    ctx = most * bs - rng.integers(0, bs, size=B)
+    table = rng.permuted(np.tile(np.arange(n_slots, dtype=np.int32), (B, 1)), axis=1)[:, :most].copy()
+    sel = np.full((B, most), -1, np.int32)
+    for r in range(B):
+        sel[r, :cnt[r]] = np.sort(rng.choice(most, size=cnt[r], replace=False))
+    q = torch.randn((B, hq, D), generator=gen).bfloat16()
+    sh = P.make_shape(hq, hkv, D, bs, P.PULSE_BF16_KV4)
+    out, lse = attend(sh, q.to(DEV), pool.to(DEV), dev(table), dev(sel), dev(cnt), dev(ctx))
+    k, v = (x.transpose(0, 1).reshape(hkv, n_slots, bs, D) for x in plain64.unpack(pool, hkv, bs))
+    for r in range(0, B, 3):
+        j = sel[r, :cnt[r]]
+        n = torch.from_numpy(((j[:, None] * bs + np.arange(bs)) < ctx[r]).reshape(-1))
+        rows = [x[:, table[r, j].astype(np.int64)].reshape(hkv, -1, D)[:, n] for x in (k, v)]
+        check_attention(out[r], lse[r], *plain64.attention(q[r], *rows, SCALE), int(n.sum()))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("B", [3, 64, 100])
 def test_counts_out_of_range_among_others(B):
     """Such a request has no output, whichever lane holds its count, and takes nothing from the others."""
