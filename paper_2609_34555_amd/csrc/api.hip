@@ -26,7 +26,7 @@ static size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
 WsLayout ws_layout(const pulse_shape& s, int32_t B, int32_t k_max, int64_t total_blocks) {
     WsLayout w;
     const size_t G = (size_t)(s.num_q_heads / s.num_kv_heads);
-    const size_t units = (size_t)attn_partial_units(s, B, k_max);
+    const size_t units = (size_t)attn_partials_most(s, B, k_max);
     size_t o = 0;
     w.scores = o;    o = align_up(o + sizeof(float) * (size_t)total_blocks);
     w.miss_list = o; o = align_up(o + sizeof(int32_t) * (size_t)B * k_max);

@@ -905,6 +905,21 @@ AttnPlan attn_plan(const pulse_shape& s, int32_t B, int32_t k_max) {
     return p;
 }
 
+// A workspace serves smaller calls too, and those may take more workgroups than a larger one: a batch that fills a
+// round less well, a k_max that divides into more splits, a batch small enough for a plan.  Both bounds grow with B
+// and k_max: no more workgroups than shortest splits fill; and no more splits than waves aimed at, one short of them
+// each request and head more, or those of 64 entries, each request and head's last workgroup not full; and the second
+// workgroups of a plan beyond a round.
+int64_t attn_partials_most(const pulse_shape& s, int32_t B, int32_t k_max) {
+    const bool kv4 = is_kv4(s.dtype);
+    const int64_t W = s.num_q_heads / s.num_kv_heads <= 8 || kv4 ? 8 : 4;
+    const int64_t units = (int64_t)B * s.num_kv_heads, least = split_least(s);
+    const int64_t shortest = units * (((k_max + least - 1) / least + 3) / 4);
+    const int64_t splits = std::max(PULSE_ATTN_TARGET_WAVES + units, units * (((int64_t)k_max + 63) / 64));
+    const int64_t second = kv4 ? std::min<int64_t>(units, (int64_t)kPlanRequestsKv4 * s.num_kv_heads) : 0;
+    return std::min(std::max(shortest, units), splits / W + units + second);
+}
+
 // `done` (optional): the kernel's stop event, carried by the launch.
 template <int DT, int BS, int W, int GP = kMaxGroup>
 static void launch_attn_t(dim3 grid, size_t lds, hipStream_t st, hipEvent_t done, const void* q, const void* pool,

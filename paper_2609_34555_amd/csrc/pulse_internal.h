@@ -163,12 +163,8 @@ struct WsLayout {
 AttnPlan attn_plan(const pulse_shape& s, int32_t B, int32_t k_max);
 // Waves per attention workgroup; and of all of them, those that a plan aims at.
 int attn_waves(const pulse_shape& s, int32_t B, int32_t k_max);
-// Attention partials a call with these arguments writes: one per workgroup.
-inline int64_t attn_partial_units(const pulse_shape& s, int32_t B, int32_t k_max) {
-    const AttnPlan p = attn_plan(s, B, k_max);
-    const int W = attn_waves(s, B, k_max);
-    return (int64_t)B * s.num_kv_heads * ((p.n_split + W - 1) / W);
-}
+// Attention partials, one per workgroup, that a call with these arguments or smaller ones writes at most.
+int64_t attn_partials_most(const pulse_shape& s, int32_t B, int32_t k_max);
 WsLayout ws_layout(const pulse_shape& s, int32_t B, int32_t k_max, int64_t total_blocks);
 bool shape_supported(const pulse_shape* s);      // a 16-bit cache
 bool kv_shape_supported(const pulse_shape* s);   // a 16-bit or a 4-bit cache

@@ -462,6 +462,28 @@ def test_counts_out_of_range_among_others(B):
         check_attention(out[r], lse[r], *plain64.attention(q[r], k[:, n], v[:, n], SCALE), int(n.sum()))
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("kv4", [False, True])
+def test_a_workspace_serves_smaller_calls(dt, kv4):
+    """Batches around a round of workgroups and a plan's limits, selections around whole splits; the partials of every
+    call fit beside the lists."""
+    for hq, hkv, bs in ((32, 8, 16), (16, 1, 64), (28, 4, 32), (2, 2, 16), (48, 4, 64), (3, 3, 32)):
+        sh = P.make_shape(hq, hkv, D, bs, TYPES[dt][2 if kv4 else 1])
+        ks = [1, 2, 3, 8, 9, 17, 63, 64, 65, 127, 128, 130, 255, 256, 257, 500, 512, 513, 1000, 4100]
+        before = None
+        for B in [1, 2, 3, 7, 16, 17, 31, 32, 33, 43, 64, 65, 85, 86, 128, 129, 256, 257, 300, 512, 1000]:
+            row, most = [], 0
+            for k in ks:
+                n = P.pulse_workspace_bytes(sh, B, k, 0)
+                lists = 4 * (B * k + 3 * B)
+                assert n >= lists + P.pulse_attention_workgroups(sh, B, k) * B * hq * (4 * D + 8)
+                most = max(most, n)
+                assert n == most
+                row.append(n)
+            assert before is None or all(a <= b for a, b in zip(before, row))
+            before = row
+
+
 def test_kv4_attention_workgroups():
     """One workgroup of eight waves, hence no merge launch, up to two 32-token steps of each wave (more than eight query
     heads per KV head), three, or four (more than 64 requests and heads); splits over several beyond."""
