@@ -481,8 +481,9 @@ PULSE_API pulse_status pulse_decode_layer(const pulse_layer_args* args, pulse_st
  * that the library holds on each GPU it runs on until the process ends, so the
  * caller passes args->ws = NULL and args->ws_bytes = 0 (else
  * PULSE_ERR_INVALID_ARG) and still owns every input and output buffer.  A call
- * whose workspace (pulse_workspace_bytes(shape, B, k_max, total_blocks)) would
- * exceed that size returns PULSE_ERR_WORKSPACE and enqueues nothing.  The
+ * that would itself use more than that returns PULSE_ERR_WORKSPACE and enqueues
+ * nothing; where pulse_workspace_bytes(shape, B, k_max, total_blocks), which
+ * holds every smaller call too, is no more than that, a call always fits.  The
  * first call on a device looks up that device's array (no allocation); a
  * failed lookup returns PULSE_ERR_HIP.  Results are those of
  * pulse_decode_layer with a workspace of its own.

@@ -26,7 +26,7 @@ static size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
 WsLayout ws_layout(const pulse_shape& s, int32_t B, int32_t k_max, int64_t total_blocks) {
     WsLayout w;
     const size_t G = (size_t)(s.num_q_heads / s.num_kv_heads);
-    const size_t units = (size_t)attn_partials_most(s, B, k_max);
+    const size_t units = (size_t)attn_partials(s, B, k_max);
     size_t o = 0;
     w.scores = o;    o = align_up(o + sizeof(float) * (size_t)total_blocks);
     w.miss_list = o; o = align_up(o + sizeof(int32_t) * (size_t)B * k_max);
@@ -38,6 +38,13 @@ WsLayout ws_layout(const pulse_shape& s, int32_t B, int32_t k_max, int64_t total
     w.attn_ml = o;   o = align_up(o + sizeof(float2) * units * G);
     w.total = o;
     return w;
+}
+
+size_t ws_bytes_most(const pulse_shape& s, int32_t B, int32_t k_max, int64_t total_blocks) {
+    const size_t G = (size_t)(s.num_q_heads / s.num_kv_heads);
+    const size_t units = (size_t)attn_partials_most(s, B, k_max);
+    return ws_layout(s, B, k_max, total_blocks).attn_o + align_up(sizeof(float) * units * G * kHeadDim) +
+           align_up(sizeof(float2) * units * G);
 }
 
 template <typename T>
@@ -77,7 +84,7 @@ size_t pulse_block_bytes(const pulse_shape* shape) {
 
 size_t pulse_workspace_bytes(const pulse_shape* shape, int32_t B, int32_t k_max, int64_t total_blocks) {
     if (!kv_shape_supported(shape) || B < 0 || k_max < 0 || total_blocks < 0) return 0;
-    return ws_layout(*shape, B, k_max, total_blocks).total;
+    return ws_bytes_most(*shape, B, k_max, total_blocks);
 }
 
 int32_t pulse_attention_workgroups(const pulse_shape* shape, int32_t B, int32_t k_max) {
@@ -287,8 +294,8 @@ pulse_status pulse_recall_gather(const pulse_shape* shape, const void* host_kv, 
                                         max_blocks, free_slots, free_head, n_free, slot_pool, n_slots, stats,
                                         dev_status);
     if (st != PULSE_OK || B == 0) return st;
+    PULSE_REQUIRE(ws && ws_bytes >= ws_bytes_most(*shape, B, k_max, 0), PULSE_ERR_WORKSPACE);
     const WsLayout w = ws_layout(*shape, B, k_max, 0);
-    PULSE_REQUIRE(ws && ws_bytes >= w.total, PULSE_ERR_WORKSPACE);
     hipStream_t hs = (hipStream_t)stream;
     hipError_t e = launch_recall_plan(blk_off, B, sel_idx, sel_cnt, k_max, block_table, max_blocks, n_slots,
                                       free_head, at<int32_t>(ws, w.miss_list), at<int32_t>(ws, w.miss_cnt),
@@ -312,8 +319,8 @@ pulse_status pulse_release_recalled(const pulse_shape* shape, int32_t B, int32_t
     PULSE_REQUIRE(B <= kMaxBatch, PULSE_ERR_UNSUPPORTED);
     if (B == 0) return PULSE_OK;
     PULSE_REQUIRE(block_table && free_head && stats && dev_status, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(ws && ws_bytes >= ws_bytes_most(*shape, B, k_max, total_blocks), PULSE_ERR_WORKSPACE);
     const WsLayout w = ws_layout(*shape, B, k_max, total_blocks);
-    PULSE_REQUIRE(ws && ws_bytes >= w.total, PULSE_ERR_WORKSPACE);
     return hip_status(launch_release(at<int32_t>(ws, w.miss_list), at<int32_t>(ws, w.miss_cnt), B, k_max, block_table,
                                      max_blocks, free_head, stats, dev_status, (hipStream_t)stream));
 }
@@ -330,8 +337,8 @@ pulse_status pulse_sparse_decode_attn(const pulse_shape* shape, const void* q, c
     PULSE_REQUIRE(q && slot_pool && block_table && sel_idx && sel_cnt && ctx_len && out && dev_status,
                   PULSE_ERR_INVALID_ARG);
     PULSE_REQUIRE(kv4_aligned(*shape, slot_pool), PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(ws && ws_bytes >= ws_bytes_most(*shape, B, k_max, 0), PULSE_ERR_WORKSPACE);
     const WsLayout w = ws_layout(*shape, B, k_max, 0);
-    PULSE_REQUIRE(ws && ws_bytes >= w.total, PULSE_ERR_WORKSPACE);
     return hip_status(launch_attention(*shape, q, slot_pool, n_slots, block_table, max_blocks, sel_idx, sel_cnt,
                                        k_max, ctx_len, B, sm_scale, out, lse, at<float>(ws, w.attn_o),
                                        at<float2>(ws, w.attn_ml), dev_status, (hipStream_t)stream));
@@ -378,9 +385,8 @@ hipError_t layer_attention(const pulse_layer_args& a, hipStream_t hs, hipEvent_t
                             at<float2>(a.ws, w.attn_ml), a.dev_status, hs, (hipEvent_t)a.attn_split_event, done);
 }
 
-// Full argument check of a chained layer-step.
-pulse_status check_layer_args(const pulse_layer_args* a) {
-    PULSE_REQUIRE(a, PULSE_ERR_INVALID_ARG);
+// Argument check of a chained layer-step but for its workspace.
+static pulse_status check_step_args(const pulse_layer_args* a) {
     pulse_status st = check_select_args(&a->shape, a->q, a->digests, a->blk_off, a->B, a->total_blocks,
                                         a->solo_kv_head, a->k_mid, a->n_sink_blocks, a->n_local_blocks, a->k_max,
                                         a->sel_idx, a->sel_cnt, a->dev_status);
@@ -391,8 +397,27 @@ pulse_status check_layer_args(const pulse_layer_args* a) {
     if (st != PULSE_OK) return st;
     if (a->B == 0) return PULSE_OK;
     PULSE_REQUIRE(a->ctx_len && a->out, PULSE_ERR_INVALID_ARG);
-    PULSE_REQUIRE(a->ws && a->ws_bytes >= ws_layout(a->shape, a->B, a->k_max, a->total_blocks).total,
+    return PULSE_OK;
+}
+
+// Full argument check of a chained layer-step.
+pulse_status check_layer_args(const pulse_layer_args* a) {
+    PULSE_REQUIRE(a, PULSE_ERR_INVALID_ARG);
+    const pulse_status st = check_step_args(a);
+    if (st != PULSE_OK || a->B == 0) return st;
+    PULSE_REQUIRE(a->ws && a->ws_bytes >= ws_bytes_most(a->shape, a->B, a->k_max, a->total_blocks),
                   PULSE_ERR_WORKSPACE);
+    return PULSE_OK;
+}
+
+// A checked layer-step on one stream.
+static pulse_status layer_step(const pulse_layer_args& a, hipStream_t hs) {
+    // the timing events ride on the kernels' own launches (no marker packets); NULL entries are not recorded
+    hipEvent_t* ev = (hipEvent_t*)a.events;
+    auto E = [&](int i) { return ev ? ev[i] : nullptr; };
+    if (layer_select(a, hs, E(0), E(1)) != hipSuccess) return PULSE_ERR_HIP;
+    if (layer_recall(a, hs, 8, E(2), E(3)) != hipSuccess) return PULSE_ERR_HIP;
+    if (layer_attention(a, hs, E(4)) != hipSuccess) return PULSE_ERR_HIP;
     return PULSE_OK;
 }
 
@@ -401,16 +426,9 @@ pulse_status check_layer_args(const pulse_layer_args* a) {
 extern "C" {
 
 pulse_status pulse_decode_layer(const pulse_layer_args* a, pulse_stream_t stream) {
-    pulse_status st = check_layer_args(a);
+    const pulse_status st = check_layer_args(a);
     if (st != PULSE_OK || a->B == 0) return st;
-    hipStream_t hs = (hipStream_t)stream;
-    // the timing events ride on the kernels' own launches (no marker packets); NULL entries are not recorded
-    hipEvent_t* ev = (hipEvent_t*)a->events;
-    auto E = [&](int i) { return ev ? ev[i] : nullptr; };
-    if (layer_select(*a, hs, E(0), E(1)) != hipSuccess) return PULSE_ERR_HIP;
-    if (layer_recall(*a, hs, 8, E(2), E(3)) != hipSuccess) return PULSE_ERR_HIP;
-    if (layer_attention(*a, hs, E(4)) != hipSuccess) return PULSE_ERR_HIP;
-    return PULSE_OK;
+    return layer_step(*a, (hipStream_t)stream);
 }
 
 }  // extern "C"
@@ -447,16 +465,16 @@ pulse_status pulse_decode_layer_noalloc(const pulse_layer_args* args, pulse_stre
     PULSE_REQUIRE(args, PULSE_ERR_INVALID_ARG);
     PULSE_REQUIRE(!args->ws && args->ws_bytes == 0, PULSE_ERR_INVALID_ARG);
     pulse_layer_args a = *args;
-    // other argument errors are reported by pulse_decode_layer's own checks
-    if (kv_shape_supported(&a.shape) && a.B > 0 && a.B <= kMaxBatch && a.k_max >= 1 && a.total_blocks >= 0) {
-        const size_t need = ws_layout(a.shape, a.B, a.k_max, a.total_blocks).total;
-        PULSE_REQUIRE(need <= (size_t)PULSE_NOALLOC_SCRATCH_BYTES, PULSE_ERR_WORKSPACE);
-        void* ws = scratch_for_current_device();
-        if (!ws) return PULSE_ERR_HIP;
-        a.ws = ws;
-        a.ws_bytes = need;
-    }
-    return pulse_decode_layer(&a, stream);
+    // the array serves this call alone, so what the call itself uses has to fit; other argument errors come first
+    // where that cannot be told
+    if (kv_shape_supported(&a.shape) && a.B > 0 && a.B <= kMaxBatch && a.k_max >= 1 && a.total_blocks >= 0)
+        PULSE_REQUIRE(ws_layout(a.shape, a.B, a.k_max, a.total_blocks).total <= (size_t)PULSE_NOALLOC_SCRATCH_BYTES,
+                      PULSE_ERR_WORKSPACE);
+    const pulse_status st = check_step_args(&a);
+    if (st != PULSE_OK || a.B == 0) return st;
+    a.ws = scratch_for_current_device();
+    if (!a.ws) return PULSE_ERR_HIP;
+    return layer_step(a, (hipStream_t)stream);
 }
 
 size_t pulse_tables_workspace_bytes(const pulse_shape* shape, int32_t B, int64_t max_tokens) {

@@ -905,6 +905,11 @@ AttnPlan attn_plan(const pulse_shape& s, int32_t B, int32_t k_max) {
     return p;
 }
 
+int64_t attn_partials(const pulse_shape& s, int32_t B, int32_t k_max) {
+    const int W = attn_waves(s, B, k_max);
+    return (int64_t)B * s.num_kv_heads * ((attn_plan(s, B, k_max).n_split + W - 1) / W);
+}
+
 // A workspace serves smaller calls too, and those may take more workgroups than a larger one: a batch that fills a
 // round less well, a k_max that divides into more splits, a batch small enough for a plan.  Both bounds grow with B
 // and k_max: no more workgroups than shortest splits fill; and no more splits than waves aimed at, one short of them

@@ -416,8 +416,8 @@ pulse_status pulse_gs_recall_submit(pulse_gs_engine* e, const void* host_kv, con
     if (!host_kv || !blk_off || !sel_idx || !sel_cnt || !block_table || !free_head || !slot_pool || !stats ||
         !dev_status || (!free_slots && n_free))
         return PULSE_ERR_INVALID_ARG;
+    if (!ws || ws_bytes < ws_bytes_most(e->shape, B, k_max, 0)) return PULSE_ERR_WORKSPACE;
     const WsLayout w = ws_layout(e->shape, B, k_max, 0);
-    if (!ws || ws_bytes < w.total) return PULSE_ERR_WORKSPACE;
     if (e->completed.load() != e->submitted) return PULSE_ERR_INVALID_ARG;  // one call in flight at a time
     auto at32 = [&](size_t off) { return reinterpret_cast<int32_t*>(static_cast<char*>(ws) + off); };
     hipStream_t hs = (hipStream_t)stream;

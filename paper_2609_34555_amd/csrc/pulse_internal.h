@@ -163,9 +163,12 @@ struct WsLayout {
 AttnPlan attn_plan(const pulse_shape& s, int32_t B, int32_t k_max);
 // Waves per attention workgroup; and of all of them, those that a plan aims at.
 int attn_waves(const pulse_shape& s, int32_t B, int32_t k_max);
-// Attention partials, one per workgroup, that a call with these arguments or smaller ones writes at most.
+// Attention partials, one per workgroup, of a call with these arguments; and the most that it or a smaller one has.
+int64_t attn_partials(const pulse_shape& s, int32_t B, int32_t k_max);
 int64_t attn_partials_most(const pulse_shape& s, int32_t B, int32_t k_max);
+// What one call uses of its workspace; and the bytes that serve this call and every smaller one.
 WsLayout ws_layout(const pulse_shape& s, int32_t B, int32_t k_max, int64_t total_blocks);
+size_t ws_bytes_most(const pulse_shape& s, int32_t B, int32_t k_max, int64_t total_blocks);
 bool shape_supported(const pulse_shape* s);      // a 16-bit cache
 bool kv_shape_supported(const pulse_shape* s);   // a 16-bit or a 4-bit cache
 
