@@ -40,8 +40,8 @@
  *   K(h, t, c) at element ((0 * Hkv + h) * bs + t) * d + c      token-major
  *   V(h, t, c) at element Hkv*bs*d + (h * d + c) * bs + t       channel-major
  * so a block is U = 2 * Hkv * bs * d * 2 bytes (64 KiB at Hkv 8, bs 16).
- * Tokens past the end of a context inside its last block must be zero
- * (4-bit blocks: may hold anything).
+ * Tokens past the end of a context inside its last block may hold anything (a
+ * slot taken again keeps there what its earlier owner left).
  * Requests are ragged: request r owns n_r = ceil(ctx_len[r] / bs) blocks,
  * its global blocks are blk_off[r] .. blk_off[r+1]-1 (blk_off[0] = 0).
  *

@@ -320,6 +320,8 @@ __device__ inline void attend_split(const uint16_t* __restrict__ q, const uint16
         }
         if (my_slot < 0) report(status, PULSE_ERR_BAD_INDEX);
     }
+    constexpr int kPer = BS >= kChunkTokens ? 1 : kChunkTokens / BS;  // entries of a step
+    const uint64_t partial = __ballot(my_slot >= 0 && my_nv < BS);
     // Q^T operand: lane holds q[g = col][8 channels of slice grp + 32 kc]
     vec qb[4];
     {
@@ -360,8 +362,8 @@ __device__ inline void attend_split(const uint16_t* __restrict__ q, const uint16
     };
 
     // One 32-token step at a time: K is loaded first, V once the S tile is issued, so
-    // the V loads overlap the softmax and fewer operands are live (121-128 VGPRs and 4
-    // waves per SIMD with 8-wave workgroups, up to 130 and 3 with 4-wave ones).  The
+    // the V loads overlap the softmax and fewer operands are live (123-127 VGPRs and 4
+    // waves per SIMD with 8-wave workgroups, 156-168 and 3 with 4-wave ones).  The
     // other resident waves hide the load latency.  Measured slower:
     // loading K and V together (154 VGPRs; 2-5%), prefetching the next step into
     // registers as well (223 VGPRs; another 1-2%), and, for splits of two steps,
@@ -425,6 +427,21 @@ __device__ inline void attend_split(const uint16_t* __restrict__ q, const uint16
                 const float av = __shfl(alpha, 4 * grp + v);
 #pragma unroll
                 for (int t = 0; t < 8; ++t) acc[t][v] *= av;
+            }
+        }
+        // behind a context's end lies what an earlier owner of the slot left, NaN perhaps, which a probability of 0
+        // would not take out of the product (0.1 us a call whose last blocks are cut, nothing otherwise)
+        if ((partial >> (t0 / BS)) & ((1u << kPer) - 1)) {
+            const int left = pv_nv - pv_row;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t keep = (2 * i < left ? 0xFFFFu : 0u) | (2 * i + 1 < left ? 0xFFFF0000u : 0u);
+#pragma unroll
+                for (int t = 0; t < 8; ++t) {
+                    u32x4 w = __builtin_bit_cast(u32x4, vb[t]);
+                    w[i] &= keep;
+                    vb[t] = __builtin_bit_cast(vec, w);
+                }
             }
         }
         // --- O += P . V  (hi and lo parts of P)
