@@ -514,7 +514,9 @@ PULSE_API pulse_status pulse_decode_layer_noalloc(const pulse_layer_args* args, 
  *                for g >= tok_off[B], so that a captured step may be padded
  *   block_table  device int32 [B][max_blocks], -1 = not resident; updated
  *   free_slots   device int32 [n_free];  free_head device int32, updated
- *   ws           pulse_tables_workspace_bytes() bytes of device memory
+ *   ws           pulse_tables_workspace_bytes() bytes of device memory; one of
+ *                that size serves any step with the same bs and the same or
+ *                smaller B and max_tokens
  * PULSE_ERR_POOL_EXHAUSTED if the free list has too few slots;
  * PULSE_ERR_BAD_INDEX if ctx_len[r] is negative, new_len[r] is not in
  * 0 .. ctx_len[r], n_r > max_blocks or the new tokens exceed max_tokens; if a

@@ -423,14 +423,16 @@ static int64_t cell_bound(int32_t B, int32_t bs, int64_t max_tokens) {
     return n < max_tokens ? n : max_tokens;
 }
 // Cells of a tile: those of 16 * kTileThreads tokens, or the multiple of them that keeps the tiles few.
+static int64_t least_tile(int32_t bs) { return kTileThreads * 16 / bs; }
 static int64_t tile_cells(int64_t cells, int32_t bs) {
-    const int64_t least = kTileThreads * 16 / bs;
+    const int64_t least = least_tile(bs);
     return least * ((cells + least * kMaxTiles - 1) / (least * kMaxTiles));
 }
 
+// Room for as many tiles as this step or a smaller one has (a step whose tiles are larger has fewer of them).
 size_t tables_ws_bytes(int32_t B, int32_t bs, int64_t max_tokens) {
-    const int64_t cells = cell_bound(B, bs, max_tokens);
-    const int64_t tiles = cells > 0 ? (cells + tile_cells(cells, bs) - 1) / tile_cells(cells, bs) : 0;
+    const int64_t least = least_tile(bs), most = (cell_bound(B, bs, max_tokens) + least - 1) / least;
+    const int64_t tiles = most < kMaxTiles ? most : kMaxTiles;
     return (sizeof(int32_t) * (size_t)(1 + 2 * tiles) + 255) & ~(size_t)255;
 }
 
