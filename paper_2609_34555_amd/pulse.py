@@ -217,8 +217,11 @@ def _stream(stream):
     if stream is None:
         import torch
 
-        # the raw handle: building a torch.cuda.Stream for it took 2.9 us a call
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        # the raw handle where this torch gives it: building a torch.cuda.Stream for it took 2.9 us a call
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is None:
+            return torch.cuda.current_stream().cuda_stream
+        return raw(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
