@@ -21,10 +21,10 @@
 // domain.
 //
 // Merging the splits: a workgroup holds W waves = W consecutive splits of one
-// (r, h) (W = 8 for G <= 8, else 4); they merge through LDS.  With one
-// workgroup per (r, h) it writes the result directly.  Otherwise each workgroup writes one partial (m, l, O) to
-// the workspace and a combine kernel merges those few partials, one thread
-// per output element, with independent loads.  (Merging in the last workgroup
+// (r, h) (attn_waves); they merge through LDS.  With one workgroup per (r, h)
+// it writes the result directly.  Otherwise each workgroup writes one partial
+// (m, l, O) to the workspace and a combine kernel merges those partials, one
+// thread per output element, with independent loads.  (Merging in the last workgroup
 // to finish instead needs a device-scope release per workgroup, an L2
 // write-back on gfx950 measured at about 9 ns per workgroup, plus a merge on
 // the kernel's tail and counters that start at zero in the workspace: it would
@@ -476,7 +476,11 @@ __device__ inline void attend_split(const uint16_t* __restrict__ q, const uint16
 // products of this one (equal), products interleaved over accumulators (equal), 16 waves per workgroup (5 to 10%
 // slower), two workgroups per CU (20% slower), keys multiplied as codes by the scaled 4-bit matrix instruction (Q cut
 // into two or three e4m3 parts; 34 vector instructions fewer a step: 1% faster on 16 ragged requests, 2 to 10% slower
-// on the others for the cutting, and its sums are some hundred times less exact).
+// on the others for the cutting, and its sums are some hundred times less exact).  All that is of GP = 4.
+// Larger groups cut P' into parts twice (GP = 8) and four times (16) a step, and their kernels hold 130 to 133 and 145
+// to 146 VGPRs (GP = 4: 125 and 126), so a CU takes one workgroup at a time where it takes two with GP = 4, and beyond
+// a round nothing runs beside a workgroup's look-ups and merge: 2048 requests and heads of 1000 tokens, 1024 of 2000
+// (floors 49 to 52 us), 4, 8 and 16 query heads each: 64 94 117, 59 77 94 us.
 template <int GP>
 struct Kv4Values {
     u32x4 v[2];        // codes of 8 tokens, channel tiles 0..3 and 4..7
@@ -799,7 +803,9 @@ __global__ __launch_bounds__(W * kWave) void attn_splitk_kernel(
 
 // Merge the workgroup partials of one (request, KV head, query head):
 // grid = (G, Hkv, B), 128 threads, thread c owns output channel c.  Partials
-// are read 8 at a time (16 independent loads per thread) and merged online.
+// are read 8 at a time (16 independent loads per thread) and merged online:
+// 2 to 4 us up to 8 of them, 9 for 64 and 29 for 256 (4 and 1 requests of 64K
+// tokens in the 4-bit cache of one KV head).
 // Requests whose selection fits one workgroup were finished by the attention
 // kernel.
 // R: counts per lane of a plan.

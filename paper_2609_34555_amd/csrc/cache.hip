@@ -11,8 +11,9 @@
 // channels" by exchanges of lane groups in registers.
 // A run shorter than an octet shares words with other tokens, which other rows of the call may be writing: it
 // clears and sets its own bits with atomics, whose order does not matter.
-// 16K rows of 8 heads into 4 bits: 19 us for 85 MB (17.8 at the rate of a large copy), back 15; with a lane per two
-// channels and a wave per row, byte stores and all, 97 and 69.
+// 16K rows of 8 heads into 4 bits: 19 us for 85 MB (17.8 at the rate of a large copy), back 15 where the blocks have
+// just been written and 22 where they come from memory; with a lane per two channels and a wave per row, byte stores and
+// all, 97 and 69.  The same rows into 16-bit blocks and back: 31 and 30 us for 134 MB (28).
 #include "kv4.h"
 
 namespace pulse {
@@ -21,10 +22,14 @@ constexpr int kCacheThreads = 256;
 constexpr int kCacheWaves = kCacheThreads / kWave;
 constexpr int kOct = 8;
 constexpr int64_t kCacheGrid = 65535;
-// Rows times heads up to which a wave looks at one row (each may begin a run), above at an octet's.  In us, one row and
-// an octet per wave, rows that follow one another: 512 x 8 heads 4.1 and 4.8, 1024 x 8 5.0 and 4.9, 2048 x 8 7.4 and 4.9,
-// 16384 x 8 37 and 17; 4096 x 1 4.1 and 4.5, 16384 x 1 7.7 and 4.8.  Rows of a request each: 64 x 8 4.5 and 13.9,
-// 2048 x 8 24.4 and 25.2.
+// Rows times heads up to which a wave looks at one row (each may begin a run), above at an octet's.  In us, appending to
+// 4-bit and to 16-bit blocks with one row and with an octet per wave:
+//   rows that follow one another    512 x 8 heads  4.3 3.9   4.1 3.9     1024 x 8  5.1 4.1   5.4 4.6
+//                                   2048 x 8       7.9 5.2   7.9 6.3    16381 x 8   40  19    50  31
+//                                   4096 x 1       4.5 3.8   4.6 3.5    16384 x 1  8.1 5.2   9.5 6.3
+//   rows of a request each            64 x 8       4.2 13.5  3.8 12.5    2048 x 8  27.3 28.4  48  37
+//                                   8192 x 1      15.7 18.0 15.5 21.3
+// Below the limit a decode batch's rows decide, which may lose 9 us; rows that follow one another lose 1.
 constexpr int64_t kRunRows = 8192;
 
 struct CacheArgs {

@@ -155,13 +155,13 @@ struct WsLayout {
     size_t run_cnt;    // int32 [B]
     size_t req_err;    // int32 [B]          per-request plan error (0 = ok)
     size_t misc;       // int32 [16]         [0] = free_head snapshot
-    size_t attn_o;     // float [B][Hkv][n_wg][G][d]   (per-workgroup partials)
-    size_t attn_ml;    // float2 [B][Hkv][n_wg][G]
+    size_t attn_o;     // float [B * n_wg][Hkv][G][d]   (a partial per workgroup)
+    size_t attn_ml;    // float2 [B * n_wg][Hkv][G]
     size_t total;
 };
 
 AttnPlan attn_plan(const pulse_shape& s, int32_t B, int32_t k_max);
-// Waves per attention workgroup; and of all of them, those that a plan aims at.
+// Waves per attention workgroup of a call.
 int attn_waves(const pulse_shape& s, int32_t B, int32_t k_max);
 // Attention partials, one per workgroup, of a call with these arguments; and the most that it or a smaller one has.
 int64_t attn_partials(const pulse_shape& s, int32_t B, int32_t k_max);
