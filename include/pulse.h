@@ -545,7 +545,9 @@ PULSE_API pulse_status pulse_build_tables(const pulse_shape* shape, const int32_
  *   (y_a, y_b) -> (y_a cos t - y_b sin t, y_a sin t + y_b cos t)
  * with (a, b) = (i, i + rot_dim / 2), or (2i, 2i + 1) if interleaved is 1 (0
  * otherwise); channels from rot_dim on are not rotated.  Statistics and
- * rotation in fp32, angles in 64 bits, one rounding to the 16-bit type.
+ * rotation in fp32, angles in 64 bits, one rounding to the 16-bit type: a
+ * head's squares have to sum to a value of fp32 (they do for |x| below 2^60),
+ * and with eps 0 to one above 0.
  *   q, k         device rows of 16-bit elements; row r begins at r * q_stride
  *                (k_stride) elements, its heads follow one another, so both may
  *                be parts of one projection's output
