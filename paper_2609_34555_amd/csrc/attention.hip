@@ -430,7 +430,7 @@ __device__ inline void attend_split(const uint16_t* __restrict__ q, const uint16
             }
         }
         // behind a context's end lies what an earlier owner of the slot left, NaN perhaps, which a probability of 0
-        // would not take out of the product (0.1 us a call whose last blocks are cut, nothing otherwise)
+        // would not take out of the product (1 x 400 tokens 9.18 -> 9.24 us, 8 x 2048 17.55 -> 17.6)
         if ((partial >> (t0 / BS)) & ((1u << kPer) - 1)) {
             const int left = pv_nv - pv_row;
 #pragma unroll

@@ -29,7 +29,8 @@ constexpr int64_t kCacheGrid = 65535;
 //                                   4096 x 1       4.5 3.8   4.6 3.5    16384 x 1  8.1 5.2   9.5 6.3
 //   rows of a request each            64 x 8       4.2 13.5  3.8 12.5    2048 x 8  27.3 28.4  48  37
 //                                   8192 x 1      15.7 18.0 15.5 21.3
-// Below the limit a decode batch's rows decide, which may lose 9 us; rows that follow one another lose 1.
+// Below the limit a decode batch's rows decide, which would lose 9 us with an octet; rows that follow one another lose 1
+// without.
 constexpr int64_t kRunRows = 8192;
 
 struct CacheArgs {

@@ -7,7 +7,7 @@
 // in fp32 is off by up to 2^-4 turns of the fastest pair), as a fraction of a turn, once per row for all its heads.
 // Sums, norm and rotation are in fp32; the result is rounded to 16 bits once.
 // 16K rows of 32 + 8 heads (335 MB read and written): 67 us, 5.0 TB/s (a large copy: 4.8); 78 us before the loads of a
-// row's first heads were issued ahead of its angles.  One row: 4.0 us.  Without norms 63 and 3.7.
+// row's first heads were issued ahead of its angles.  One row: 4.0 us.  Without norms 63 and 3.8.
 #include "pulse_internal.h"
 
 namespace pulse {
