@@ -27,8 +27,8 @@
  * Element types.  K, V and queries are fp16 or bf16 (pulse_dtype); they are
  *   passed as raw 16-bit element buffers.  Scores, outputs and LSE are fp32.
  *   The blocks of the host store and the slot pool may be held in 4 bits
- *   instead (PULSE_F16_KV4, PULSE_BF16_KV4): queries, digests and rows stay in
- *   the named 16-bit type.
+ *   (PULSE_F16_KV4, PULSE_BF16_KV4) or in 8 (PULSE_F16_KV8, PULSE_BF16_KV8)
+ *   instead: queries, digests and rows stay in the named 16-bit type.
  * Indices.  Block and slot indices are int32; block offsets are int64.
  * Inputs must be finite.
  *
@@ -55,9 +55,24 @@
  *                 channel c of tokens 8o .. 8o+7, token 8o in its lowest 4 bits
  *   key scales    [bs][4] bytes        value scales  [4][bs] bytes
  * Exponents lie in -23 .. 13 (fp16) or -100 .. 125 (bf16), so that every value
- * is one of the 16-bit type; the scale byte 255 makes a group NaN.  Pools and
- * stores of 4-bit blocks are 16-byte aligned (else PULSE_ERR_INVALID_ARG from
- * the recall, the attention, the layer-step and the scheduler).
+ * is one of the 16-bit type; the scale byte 255 makes a group NaN.
+ *
+ * 8-bit KV block (PULSE_F16_KV8, PULSE_BF16_KV8).  The keys of one head in one
+ * block, and its values, are e4m3 codes c (sign, 4 bits of exponent, 3 of
+ * mantissa, up to 448; 0x7F is NaN) under one scale 2^e; a code stands for
+ * c * 2^e.  A block is Hkv regions of 256 * bs bytes, head after head, and the
+ * scales (32 KiB + 128 bytes at Hkv 8, bs 16):
+ *   keys          [bs][128] bytes: channel c of a token
+ *   values        [bs/8][16][8][8] bytes: channel c of token t at
+ *                 [t / 8][c % 16][c / 16][t % 8]
+ *   scales        [Hkv][2] bytes e + 127 of keys and values, padded to a multiple
+ *                 of 128 bytes, behind all regions
+ * Exponents lie in -15 .. 7 (fp16) or -100 .. 119 (bf16), so that every value
+ * is one of the 16-bit type.
+ *
+ * Pools and stores of 4-bit and 8-bit blocks are 16-byte aligned (else
+ * PULSE_ERR_INVALID_ARG from the recall, the attention, the layer-step and the
+ * scheduler).
  * The entry points that take these types: pulse_block_bytes,
  * pulse_workspace_bytes, pulse_build_digests, the selections,
  * pulse_recall_gather, pulse_release_recalled, pulse_sparse_decode_attn,
@@ -97,7 +112,9 @@ typedef enum {
     PULSE_F16 = 0,
     PULSE_BF16 = 1,
     PULSE_F16_KV4 = 2, /* fp16 queries and rows, KV blocks in 4 bits */
-    PULSE_BF16_KV4 = 3 /* bf16 queries and rows, KV blocks in 4 bits */
+    PULSE_BF16_KV4 = 3, /* bf16 queries and rows, KV blocks in 4 bits */
+    PULSE_F16_KV8 = 5, /* fp16 queries and rows, KV blocks in 8 bits */
+    PULSE_BF16_KV8 = 6 /* bf16 queries and rows, KV blocks in 8 bits */
 } pulse_dtype;
 
 typedef struct {
@@ -141,7 +158,7 @@ PULSE_API size_t pulse_workspace_bytes(const pulse_shape* shape, int32_t B, int3
  * exactly, in the KV dtype (-0 orders below +0).
  *   kv           [total_blocks][block] elements; device memory or pinned,
  *                host-mapped memory (the kernel reads it directly); of 4-bit
- *                blocks the values that the codes stand for are taken
+ *                and 8-bit blocks the values that the codes stand for are taken
  *   blk_off      device int64 [B+1];   ctx_len  device int32 [B]
  *   total_blocks = blk_off[B] (host copy of the value, sizes the grid)
  *   digests      device, [total_blocks][2][head_dim] elements, written
@@ -581,6 +598,18 @@ PULSE_API pulse_status pulse_qk_norm_rope(const pulse_shape* shape, const void* 
  * within the range given above), and the nearest code to x / 2^e (the even
  * one of two, the largest beyond 6); a group with an infinity or a NaN becomes
  * NaN as a whole.  pulse_load_kv returns c * 2^e, which the 16-bit type holds.
+ * An 8-bit pool holds the nearest codes to x / 2^e (the even one of two, the
+ * largest beyond 448; infinities and NaN as NaN) under the exponent of the row's
+ * block and head, keys and values apart.  For what a call writes of a block the
+ * least exponent with max|x| <= 448 * 2^e is needed (finite x, within the range
+ * given above).  A call that writes a block's token 0 begins the block anew with
+ * it: the block's tokens that the call does not write are then undefined.  Any
+ * other call keeps the block's exponent if that is no less; else the block takes
+ * the needed one and its other codes are rounded again to it (only codes that
+ * become subnormal change their value).  So an append to one block rewrites
+ * codes of that block and head beside the named tokens', and in one call the
+ * rows of a block stand next to one another in the map (a block whose rows are
+ * apart has undefined contents).
  *   k, v         device, 16-byte aligned, strides multiples of 8 that hold the
  *                heads (else PULSE_ERR_INVALID_ARG)
  *   slot_map     device int64 [n_rows] (as pulse_build_tables writes it)

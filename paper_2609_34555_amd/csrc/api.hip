@@ -6,6 +6,7 @@
 #include <mutex>
 
 #include "kv4.h"
+#include "kv8.h"
 
 namespace pulse {
 
@@ -16,10 +17,10 @@ bool kv_shape_supported(const pulse_shape* s) {
     if (s->num_kv_heads < 1 || s->num_q_heads < s->num_kv_heads) return false;
     if (s->num_q_heads % s->num_kv_heads) return false;
     if (s->num_q_heads / s->num_kv_heads > kMaxGroup) return false;
-    return s->dtype == PULSE_F16 || s->dtype == PULSE_BF16 || is_kv4(s->dtype);
+    return s->dtype == PULSE_F16 || s->dtype == PULSE_BF16 || kv_bits(s->dtype) != 16;
 }
 
-bool shape_supported(const pulse_shape* s) { return kv_shape_supported(s) && !is_kv4(s->dtype); }
+bool shape_supported(const pulse_shape* s) { return kv_shape_supported(s) && kv_bits(s->dtype) == 16; }
 
 static size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -79,6 +80,7 @@ const char* pulse_status_string(pulse_status s) {
 size_t pulse_block_bytes(const pulse_shape* shape) {
     if (!kv_shape_supported(shape)) return 0;
     if (is_kv4(shape->dtype)) return (size_t)shape->num_kv_heads * kv4_head_bytes(shape->block_size);
+    if (is_kv8(shape->dtype)) return (size_t)kv8_block_bytes(shape->num_kv_heads, shape->block_size);
     return (size_t)2 * shape->num_kv_heads * shape->block_size * shape->head_dim * 2;
 }
 
@@ -260,9 +262,9 @@ pulse_status pulse_pick_solo_heads(const float* mam, int32_t rows, int32_t num_k
     return PULSE_OK;
 }
 
-// Pools and stores of 4-bit blocks begin on a 16-byte piece.
-static bool kv4_aligned(const pulse_shape& s, const void* p) {
-    return !is_kv4(s.dtype) || reinterpret_cast<uintptr_t>(p) % 16 == 0;
+// Pools and stores of 4-bit and 8-bit blocks begin on a 16-byte piece.
+static bool codes_aligned(const pulse_shape& s, const void* p) {
+    return kv_bits(s.dtype) == 16 || reinterpret_cast<uintptr_t>(p) % 16 == 0;
 }
 
 static pulse_status check_recall_args(const pulse_shape* shape, const void* host_kv, const int64_t* blk_off,
@@ -280,7 +282,7 @@ static pulse_status check_recall_args(const pulse_shape* shape, const void* host
                       dev_status,
                   PULSE_ERR_INVALID_ARG);
     PULSE_REQUIRE(free_slots || n_free == 0, PULSE_ERR_INVALID_ARG);
-    PULSE_REQUIRE(kv4_aligned(*shape, host_kv) && kv4_aligned(*shape, slot_pool), PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(codes_aligned(*shape, host_kv) && codes_aligned(*shape, slot_pool), PULSE_ERR_INVALID_ARG);
     return PULSE_OK;
 }
 
@@ -336,7 +338,7 @@ pulse_status pulse_sparse_decode_attn(const pulse_shape* shape, const void* q, c
     if (B == 0) return PULSE_OK;
     PULSE_REQUIRE(q && slot_pool && block_table && sel_idx && sel_cnt && ctx_len && out && dev_status,
                   PULSE_ERR_INVALID_ARG);
-    PULSE_REQUIRE(kv4_aligned(*shape, slot_pool), PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(codes_aligned(*shape, slot_pool), PULSE_ERR_INVALID_ARG);
     PULSE_REQUIRE(ws && ws_bytes >= ws_bytes_most(*shape, B, k_max, 0), PULSE_ERR_WORKSPACE);
     const WsLayout w = ws_layout(*shape, B, k_max, 0);
     return hip_status(launch_attention(*shape, q, slot_pool, n_slots, block_table, max_blocks, sel_idx, sel_cnt,

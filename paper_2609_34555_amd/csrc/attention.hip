@@ -32,6 +32,7 @@
 #include <algorithm>
 
 #include "kv4.h"
+#include "kv8.h"
 
 namespace pulse {
 
@@ -669,6 +670,165 @@ __device__ inline void attend_split_kv4(const uint16_t* __restrict__ q, const ui
     if (m_run == -INFINITY && l_run != l_run) m_run = 0.f;
 }
 
+// attend_split over the 8-bit cache (kv8.h).  A lane's 32 bytes of a key row are 32 channels, its 64 bytes of values 8
+// tokens of 8 channels; a block has one scale for its keys and one for its values, so both are decoded with it, exactly,
+// into the operands of the products: keys into the type of the queries, values into bf16, so that the probabilities can
+// be cut into three bf16 parts, all 24 bits of them (as in attend_split_kv4).
+template <int DT, int BS>
+__device__ inline void attend_split_kv8(const uint16_t* __restrict__ q, const uint8_t* __restrict__ pool,
+                                        int32_t n_slots, const int32_t* __restrict__ table, int32_t max_blocks,
+                                        int32_t j_lane, const int32_t* __restrict__ ctx_len, int32_t Hq, int32_t Hkv,
+                                        int32_t G, int r, int h, int ne, float scale_log2, int32_t* status, int lane,
+                                        float& m_run, float& l_run, f32x4 (&acc)[8]) {
+    constexpr int ET = elem_type(DT);
+    using MQ = Mfma<ET>;
+    using MP = Mfma<PULSE_BF16>;
+    using vec = typename MQ::vec;
+    const int col = lane & 15;
+    const int grp = lane >> 4;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m_run = -INFINITY;
+    l_run = 0.f;
+    if (ne <= 0) return;
+    // entry metadata, one entry per lane; an entry without a block reads slot 0 and counts no token
+    const int32_t j = lane < ne ? j_lane : -1;
+    const int32_t sl = (j >= 0 && j < max_blocks) ? table[(size_t)r * max_blocks + j] : -1;
+    const int ctx = ctx_len[r];
+    const int64_t n_r = ((int64_t)ctx + BS - 1) / BS;
+    int my_slot = 0, my_nv = 0;
+    if (lane < ne) {
+        if (j >= 0 && j < n_r && sl >= 0 && sl < n_slots) {
+            my_slot = sl;
+            const int64_t v = (int64_t)ctx - (int64_t)j * BS;
+            my_nv = v >= BS ? BS : (int)v;
+        } else {
+            report(status, PULSE_ERR_BAD_INDEX);
+        }
+    }
+    const uint64_t U = (uint64_t)kv8_block_bytes(Hkv, BS);
+    // scales of the lane's own entry
+    const uint32_t my_scales = *reinterpret_cast<const uint16_t*>(pool + (uint64_t)my_slot * U + kv8_scales(Hkv, BS) + 2 * h);
+    const uint64_t whole = __ballot(my_nv == BS);
+    // Q^T operand: channels 32 * grp + 8 * kc .. + 7 of the column's query head
+    vec qb[4];
+    {
+        const uint16_t* qr = q + ((size_t)r * Hq + (size_t)h * G + col) * kHeadDim + grp * 32;
+#pragma unroll
+        for (int kc = 0; kc < 4; ++kc) qb[kc] = col < G ? load_vec<ET>(qr + 8 * kc) : zero_vec<ET>();
+    }
+    // Step i covers tokens 32 i ..: K: MFMA row m = col is token 8 * (col / 4) + 4 * sub + col % 4; V: lane group grp
+    // holds tokens 8 * grp .. + 7, channels col + 16 * t in unit t.
+    constexpr int kPer = BS >= kChunkTokens ? 1 : kChunkTokens / BS;  // entries of a step
+    constexpr int kHalves = BS > kChunkTokens ? BS / kChunkTokens : 1;  // steps of an entry
+    const uint8_t* head = pool + (size_t)h * kv8_head_bytes(BS);
+    const int k_tok = 8 * (col >> 2), v_tok = 8 * grp;
+    const uint8_t* k_at = head + (k_tok % BS + (col & 3)) * kHeadDim + grp * 32;
+    const uint8_t* v_at = head + kv8_values(BS) + v_tok % BS * kHeadDim + col * 64;
+    const int steps = (ne * BS + kChunkTokens - 1) / kChunkTokens;
+
+    u32x4 kw[2][2], vw[4];
+    auto load_k = [&](int i) {
+        const uint32_t slot = (uint32_t)__shfl(my_slot, i / kHalves * kPer + k_tok / BS);
+        const uint8_t* kb = k_at + (uint64_t)slot * U + i % kHalves * kChunkTokens * kHeadDim;
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) kw[sub][n] = reinterpret_cast<const u32x4*>(kb + 4 * sub * kHeadDim)[n];
+    };
+    auto load_v = [&](int i) {
+        const uint32_t slot = (uint32_t)__shfl(my_slot, i / kHalves * kPer + v_tok / BS);
+        const uint8_t* vb = v_at + (uint64_t)slot * U + i % kHalves * kChunkTokens * kHeadDim;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) vw[n] = reinterpret_cast<const u32x4*>(vb)[n];
+    };
+    load_k(0);
+    load_v(0);
+#pragma unroll 1
+    for (int i = 0; i < steps; ++i) {
+        u32x4 vn[4];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) vn[n] = vw[n];
+        const int e0 = i / kHalves * kPer;
+        const float ks = kv8_pow2((int)(__shfl((int)my_scales, e0 + k_tok / BS) & 255) - 127);
+        float vs = kv8_pow2((__shfl((int)my_scales, e0 + v_tok / BS) >> 8) - 127);
+        // --- S^T = K . Q^T
+        f32x4 s[2] = {};
+#pragma unroll
+        for (int kc = 0; kc < 4; ++kc)
+#pragma unroll
+            for (int sub = 0; sub < 2; ++sub) {
+                const u32x2 w = {kw[sub][kc / 2][2 * (kc % 2)], kw[sub][kc / 2][2 * (kc % 2) + 1]};
+                s[sub] = MQ::mac(kv8_decode8<ET>(w, ks), qb[kc], s[sub]);
+            }
+        if (i + 1 < steps) {
+            load_k(i + 1);
+            load_v(i + 1);
+        }
+        float x[8];
+#pragma unroll
+        for (int n = 0; n < 8; ++n) x[n] = s[n / 4][n % 4] * scale_log2;
+        // blocks that are not whole (the last of the context, a missing one, none behind an odd count): their other
+        // tokens count nothing, whatever codes and scales are there
+        if ((~whole >> e0) & ((1u << kPer) - 1)) {
+            const int left = __shfl(my_nv, e0 + v_tok / BS) - v_tok % BS - i % kHalves * kChunkTokens;
+            if (left <= 0) vs = 1.f;
+#pragma unroll
+            for (int n = 0; n < 8; ++n) {
+                if (n >= left) x[n] = -INFINITY;
+                const uint32_t keep = n >= left ? ~(255u << (8 * (n % 4))) : ~0u;
+#pragma unroll
+                for (int t = 0; t < 8; ++t) vn[t / 2][t % 2 * 2 + n / 4] &= keep;
+            }
+        }
+        float cm = x[0];
+#pragma unroll
+        for (int n = 1; n < 8; ++n) cm = fmaxf(cm, x[n]);
+        cm = across_groups(cm, [](float a, float b) { return fmaxf(a, b); });
+        const float m_new = fmaxf(m_run, cm);
+        const float m_use = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = exp2_fast(m_run - m_use);
+        float psum = 0.f;
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+            x[n] = exp2_fast(x[n] - m_use);
+            psum += x[n];
+        }
+        l_run = l_run * alpha + psum;
+        m_run = m_new;
+        if (i > 0 && __ballot(alpha != 1.f)) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const float av = __shfl(alpha, 4 * grp + v);
+#pragma unroll
+                for (int t = 0; t < 8; ++t) acc[t][v] *= av;
+            }
+        }
+        // --- O += P . V
+        u32x4 part[3];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            float a = x[2 * n], b = x[2 * n + 1];
+#pragma unroll
+            for (int m = 0; m < 3; ++m) {
+                part[m][n] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+                a -= __uint_as_float(__float_as_uint(a) & 0xFFFF0000u);
+                b -= __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            const u32x2 w = {vn[t / 2][t % 2 * 2], vn[t / 2][t % 2 * 2 + 1]};
+            const bf16x8 v = kv8_decode8<PULSE_BF16>(w, vs);
+#pragma unroll
+            for (int m = 0; m < 3; ++m) acc[t] = MP::mac(__builtin_bit_cast(bf16x8, part[m]), v, acc[t]);
+        }
+    }
+    l_run = across_groups(l_run, [](float a, float b) { return a + b; });
+    // a split whose every logit is NaN (keys of NaN codes) keeps its weight in the merge
+    if (m_run == -INFINITY && l_run != l_run) m_run = 0.f;
+}
+
 // grid = (Hkv, n_wg, B), or (Hkv, B, n_wg) with light_last; in either, workgroup p is piece p / Hkv of KV head
 // p % Hkv of a plan; wave w of a request's workgroup wg owns split W * wg + w of eps entries.  Dynamic LDS:
 // O [W][G][128] floats then (m, l) [W][G] float2.
@@ -756,6 +916,9 @@ __global__ __launch_bounds__(W * kWave) void attn_splitk_kernel(
     if constexpr (is_kv4(DT))
         attend_split_kv4<DT, BS, GP>(q, reinterpret_cast<const uint8_t*>(pool), n_slots, table, max_blocks, j_lane,
                                      ctx_len, Hq, Hkv, G, r, h, ne, scale_log2, status, lane, m_run, l_run, acc);
+    else if constexpr (is_kv8(DT))
+        attend_split_kv8<DT, BS>(q, reinterpret_cast<const uint8_t*>(pool), n_slots, table, max_blocks, j_lane, ctx_len,
+                                 Hq, Hkv, G, r, h, ne, scale_log2, status, lane, m_run, l_run, acc);
     else
         attend_split<DT, BS>(q, pool, n_slots, table, max_blocks, j_lane, ctx_len, Hq, Hkv, G, r, h, ne, scale_log2,
                              status, lane, m_run, l_run, acc);
@@ -1028,6 +1191,8 @@ hipError_t launch_attention(const pulse_shape& s, const void* q, const void* poo
     else { WHICH(DT, 64); }
     if (s.dtype == PULSE_BF16) { PULSE_ATTN_BS(PULSE_ATTN_W, PULSE_BF16) }
     else if (s.dtype == PULSE_F16) { PULSE_ATTN_BS(PULSE_ATTN_W, PULSE_F16) }
+    else if (s.dtype == PULSE_BF16_KV8) { PULSE_ATTN_BS(PULSE_ATTN_W, PULSE_BF16_KV8) }
+    else if (s.dtype == PULSE_F16_KV8) { PULSE_ATTN_BS(PULSE_ATTN_W, PULSE_F16_KV8) }
     else if (s.dtype == PULSE_BF16_KV4) { PULSE_ATTN_BS(PULSE_ATTN_KV4, PULSE_BF16_KV4) }
     else { PULSE_ATTN_BS(PULSE_ATTN_KV4, PULSE_F16_KV4) }
 #undef PULSE_ATTN_BS

@@ -15,6 +15,7 @@
 // just been written and 22 where they come from memory; with a lane per two channels and a wave per row, byte stores and
 // all, 97 and 69.  The same rows into 16-bit blocks and back: 31 and 30 us for 134 MB (28).
 #include "kv4.h"
+#include "kv8.h"
 
 namespace pulse {
 
@@ -127,7 +128,7 @@ __device__ inline uint32_t row_bytes(uint32_t x, int l) {
     return u;
 }
 
-template <int DT, int BS, bool KV4>
+template <int DT, int BS, int BITS>
 __device__ inline void append_run(const CacheArgs& a, const Run& run, int lane) {
     const int l = lane & 15, grp = lane >> 4;
     const int64_t slot = run.at / BS;
@@ -149,7 +150,7 @@ __device__ inline void append_run(const CacheArgs& a, const Run& run, int lane) 
         }
     }
     const bool full = run.n == kOct;
-    if constexpr (KV4) {
+    if constexpr (BITS == 4) {
         uint8_t* base = a.pool + ((size_t)slot * a.Hkv + run.h) * kv4_head_bytes(BS);
         uint32_t vc[2], vs[2];
 #pragma unroll
@@ -228,7 +229,7 @@ __device__ inline void append_run(const CacheArgs& a, const Run& run, int lane) 
     }
 }
 
-template <int DT, int BS, bool KV4>
+template <int DT, int BS, int BITS>
 __device__ inline void load_run(const CacheArgs& a, const Run& run, int lane) {
     const int l = lane & 15, grp = lane >> 4;
     const int64_t slot = run.at / BS;
@@ -238,7 +239,7 @@ __device__ inline void load_run(const CacheArgs& a, const Run& run, int lane) {
     for (int i = 0; i < 2; ++i) on[i] = 2 * grp + i >= t0 && 2 * grp + i < t0 + run.n;
     u32x4 k[2] = {}, v[2];
     uint32_t w[8];
-    if constexpr (KV4) {
+    if constexpr (BITS == 4) {
         const uint8_t* base = a.pool + ((size_t)slot * a.Hkv + run.h) * kv4_head_bytes(BS);
         uint32_t kc[2] = {}, ks[2] = {}, vs = 0, mine[2];
 #pragma unroll
@@ -272,6 +273,30 @@ __device__ inline void load_run(const CacheArgs& a, const Run& run, int lane) {
             for (int n = 0; n < 8; ++n) c |= (w[n] >> (8 * grp + 4 * i) & 15u) << (4 * n);
             v[i] = __builtin_bit_cast(u32x4, kv4_decode8<DT>(c, kv4_scale(vs >> (8 * i) & 0xFFu)));
         }
+    } else if constexpr (BITS == 8) {
+        const uint8_t* blk = a.pool + (size_t)slot * kv8_block_bytes(a.Hkv, BS);
+        const uint8_t* base = blk + (size_t)run.h * kv8_head_bytes(BS);
+        const uint16_t scales = *reinterpret_cast<const uint16_t*>(blk + kv8_scales(a.Hkv, BS) + 2 * run.h);
+        const float ks = kv8_pow2((int)(scales & 255) - 127), vs = kv8_pow2((int)(scales >> 8) - 127);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int c = 8 * l + 2 * grp + i;
+            if (on[i])
+                k[i] = __builtin_bit_cast(u32x4, kv8_decode8<DT>(*reinterpret_cast<const u32x2*>(
+                                                                     base + (o0 + 2 * grp + i) * kHeadDim + 8 * l), ks));
+            const u32x2 x = *reinterpret_cast<const u32x2*>(base + kv8_values(BS) +
+                                                            (((o0 / kOct) * 16 + c % 16) * 8 + c / 16) * kOct);
+#pragma unroll
+            for (int n = 0; n < 4; ++n) w[4 * i + n] = x[n / 2] >> (16 * (n % 2)) & 0xFFFFu;  // tokens 2n, 2n + 1
+        }
+        untranspose_groups(w);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            u32x2 c = {0, 0};
+#pragma unroll
+            for (int n = 0; n < 8; ++n) c[n / 4] |= (w[n] >> (8 * i) & 255u) << (8 * (n % 4));
+            v[i] = __builtin_bit_cast(u32x4, kv8_decode8<DT>(c, vs));
+        }
     } else {
         const uint16_t* base = reinterpret_cast<const uint16_t*>(a.pool) + (size_t)slot * 2 * a.Hkv * BS * kHeadDim;
         const uint16_t* kd = base + (size_t)run.h * BS * kHeadDim + 8 * l;
@@ -302,7 +327,7 @@ __device__ inline void load_run(const CacheArgs& a, const Run& run, int lane) {
 
 // grid = (Hkv, groups of kCacheWaves * per rows): a wave takes one head of the runs that begin in its `per` rows (1 or
 // kOct); neighbouring workgroups take neighbouring heads, which lie together in rows and blocks.
-template <int DT, int BS, bool KV4, bool APPEND>
+template <int DT, int BS, int BITS, bool APPEND>
 __global__ __launch_bounds__(kCacheThreads) void cache_kernel(CacheArgs a, int32_t per) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t step = (int64_t)kCacheWaves * per;
@@ -327,33 +352,238 @@ __global__ __launch_bounds__(kCacheThreads) void cache_kernel(CacheArgs a, int32
             run.at = (int64_t)((uint64_t)hi << 32 | lo);
             run.n = 1 + __builtin_ctzll(~(on >> (at + 1)));
             run.h = blockIdx.x;
-            if constexpr (APPEND) append_run<DT, BS, KV4>(a, run, lane);
-            else load_run<DT, BS, KV4>(a, run, lane);
+            if constexpr (APPEND) append_run<DT, BS, BITS>(a, run, lane);
+            else load_run<DT, BS, BITS>(a, run, lane);
         }
     }
 }
 
-template <int DT, int BS, bool KV4>
+// Rows into 8-bit blocks.  A block's keys of one head share a scale, and so do its values, so the unit is a block
+// and head: the rows that follow one another in one block (in any order of its tokens).  A workgroup of BS / 16 waves
+// takes a unit, a wave 16 tokens of it, all of whose values stay in registers between the largest magnitude and the
+// codes: one pass.  It alone writes the unit, so partial octets are read, joined and written without atomics; codes that
+// were there are rounded again where the scale grows, which a decode step's token rarely causes.  Lanes hold channels and
+// tokens as in append_run, two octets of it.
+template <int DT>
+__device__ inline uint32_t top_finite(u32x4 v, uint32_t top) {
+    constexpr uint32_t inf = DT == PULSE_BF16 ? 0x7F80u : 0x7C00u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t a = v[i] & 0x7FFFu, b = v[i] >> 16 & 0x7FFFu;
+        top = max(max(top, a < inf ? a : 0u), b < inf ? b : 0u);
+    }
+    return top;
+}
+
+// 8 values times `factor` as 8 codes, channel by channel.
+template <int DT>
+__device__ inline u32x2 encode8b(u32x4 v, float factor) {
+    u32x2 c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t two = kv8_encode(elem_to_float<DT>((uint16_t)(v[i] & 0xFFFF)) * factor,
+                                        elem_to_float<DT>((uint16_t)(v[i] >> 16)) * factor);
+        c[i / 2] = i % 2 ? c[i / 2] | two << 16 : two;
+    }
+    return c;
+}
+
+struct Scale8 {
+    uint32_t byte;   // of the scale that the unit gets
+    float to_codes;  // values to codes
+    float rescale;   // codes that were there to the new scale's (1: as they are)
+};
+
+template <int DT>
+__device__ inline Scale8 scale8(uint32_t top, uint32_t old_byte, bool anew) {
+    using R = Kv8Range<DT>;
+    const int need = kv8_exponent<DT>(elem_to_float<DT>((uint16_t)top));
+    const int old = min(max((int)old_byte - 127, R::lo), R::hi);
+    const int e = anew ? need : max(need, old);
+    return Scale8{(uint32_t)(e + 127), kv8_pow2(-e), anew || e == old ? 1.f : kv8_pow2(max(old - e, -126))};
+}
+
+// grid = (Hkv, groups of `per` rows): a workgroup takes one head of the runs that begin in its `per` rows (1 or BS).
+template <int DT, int BS>
+__global__ __launch_bounds__(BS / 16 * kWave) void append8_kernel(CacheArgs a, int32_t per) {
+    constexpr int kWaves = BS / 16;
+    __shared__ int8_t s_row[kWaves][BS];  // row of the run that is the token, -1: none (a copy per wave)
+    __shared__ u32x2 s_top[kWaves];
+    __shared__ uint32_t s_old;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l = lane & 15, grp = lane >> 4, h = blockIdx.x;
+    for (int64_t r0 = blockIdx.y * (int64_t)per; r0 < a.rows; r0 += gridDim.y * (int64_t)per) {
+        // slots of the row before, of the group's rows and of those that its last run may go on to: two places a lane
+        int64_t m[2], slot[2], prev[2];
+        uint64_t on[2], same[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int64_t row = r0 - 1 + 64 * i + lane;
+            m[i] = -1;
+            if (64 * i + lane <= per + BS && row >= 0 && row < a.rows) m[i] = a.slot_map[row];
+            const bool ok = m[i] >= 0 && m[i] < a.places;
+            if (h == 0 && wave == 0 && m[i] != -1 && !ok && 64 * i + lane >= 1 && 64 * i + lane <= per)
+                report(a.status, PULSE_ERR_BAD_INDEX);
+            slot[i] = ok ? m[i] / BS : -1;
+            prev[i] = __shfl_up(slot[i], 1);
+            on[i] = __ballot(ok);
+        }
+        const int64_t across = __shfl(slot[0], 63);
+        if (lane == 0) {
+            prev[0] = -1;
+            prev[1] = across;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) same[i] = __ballot(slot[i] >= 0 && slot[i] == prev[i]);
+        for (int at = 1; at <= per; ++at) {
+            const int w = at >> 6, b = at & 63;
+            if (!(on[w] >> b & 1) || (same[w] >> b & 1)) continue;
+            // rows of the run: those behind its first that are in the same slot, at most a block's
+            int n = 1;
+            while (n < BS && at + n < 128 && (same[(at + n) >> 6] >> ((at + n) & 63) & 1)) ++n;
+            const int64_t blk = __shfl(w ? slot[1] : slot[0], b);
+            const int64_t first = r0 - 1 + at;
+            if (lane < BS) s_row[wave][lane] = -1;
+            wave_lds_order();
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int x = 64 * i + lane - at;
+                if (x >= 0 && x < n) s_row[wave][m[i] % BS] = (int8_t)x;
+            }
+            wave_lds_order();
+            // this wave's 16 tokens: of octet o a lane group holds tokens 2 * grp + i
+            u32x4 k[2][2], v[2][2];
+            bool have[2][2];
+            uint32_t kt = 0, vt = 0;
+            uint64_t fresh[2], held[2];  // lanes whose tokens of an octet are, or are not, all written by this call
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int x = s_row[wave][16 * wave + 8 * o + 2 * grp + i];
+                    have[o][i] = x >= 0;
+                    k[o][i] = v[o][i] = u32x4{0, 0, 0, 0};
+                    if (x >= 0) {
+                        const size_t c = (size_t)h * kHeadDim + 8 * l;
+                        k[o][i] = __builtin_nontemporal_load(
+                            reinterpret_cast<const u32x4*>(a.k_in + (first + x) * a.k_stride + c));
+                        v[o][i] = __builtin_nontemporal_load(
+                            reinterpret_cast<const u32x4*>(a.v_in + (first + x) * a.v_stride + c));
+                    }
+                    kt = top_finite<DT>(k[o][i], kt);
+                    vt = top_finite<DT>(v[o][i], vt);
+                }
+                fresh[o] = __ballot(have[o][0] || have[o][1]);
+                held[o] = __ballot(!have[o][0] || !have[o][1]);
+            }
+            const bool anew = __builtin_amdgcn_readfirstlane(s_row[wave][0]) >= 0;
+            uint8_t* block = a.pool + (size_t)blk * kv8_block_bytes(a.Hkv, BS);
+            uint8_t* base = block + (size_t)h * kv8_head_bytes(BS);
+            uint16_t* scales = reinterpret_cast<uint16_t*>(block + kv8_scales(a.Hkv, BS)) + h;
+            uint32_t old = anew || wave != 0 ? 0 : *scales;
+            kt = last_lane(wave_scan(kt, 0u, OpMax()));
+            vt = last_lane(wave_scan(vt, 0u, OpMax()));
+            if (kWaves > 1) {
+                if (lane == 0) {
+                    s_top[wave] = u32x2{kt, vt};
+                    if (wave == 0) s_old = old;
+                }
+                __syncthreads();
+                old = s_old;
+#pragma unroll
+                for (int i = 0; i < kWaves; ++i) {
+                    const u32x2 t = s_top[i];
+                    kt = max(kt, t[0]);
+                    vt = max(vt, t[1]);
+                }
+                __syncthreads();  // (before the next run writes them)
+            }
+            const Scale8 ks = scale8<DT>(kt, old & 255, anew), vs = scale8<DT>(vt, old >> 8, anew);
+            if (wave == 0 && lane == 0) *scales = (uint16_t)(ks.byte | vs.byte << 8);
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {
+                const int t0 = 16 * wave + 8 * o;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    u32x2* dst = reinterpret_cast<u32x2*>(base + (t0 + 2 * grp + i) * kHeadDim + 8 * l);
+                    if (have[o][i]) {
+                        *dst = encode8b<DT>(k[o][i], ks.to_codes);
+                    } else if (ks.rescale != 1.f) {
+                        const u32x2 c = *dst;
+                        *dst = u32x2{kv8_rescale4(c[0], ks.rescale), kv8_rescale4(c[1], ks.rescale)};
+                    }
+                }
+                // values: units of 8 tokens of a channel; pairs of tokens of 8 channels change to all tokens of two
+                if (!fresh[o] && vs.rescale == 1.f) continue;
+                const u32x2 c0 = encode8b<DT>(v[o][0], vs.to_codes), c1 = encode8b<DT>(v[o][1], vs.to_codes);
+                uint32_t x[8];
+#pragma unroll
+                for (int n = 0; n < 8; ++n)
+                    x[n] = (c0[n / 4] >> (8 * (n % 4)) & 255u) | (c1[n / 4] >> (8 * (n % 4)) & 255u) << 8;
+                transpose_groups(x);
+                u32x2 mine = {0, 0};  // bytes of the octet's written tokens
+                if (held[o]) {
+#pragma unroll
+                    for (int t = 0; t < kOct; ++t)
+                        if (s_row[wave][t0 + t] >= 0) mine[t / 4] |= 255u << (8 * (t % 4));
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int c = 8 * l + 2 * grp + i;
+                    u32x2* dst = reinterpret_cast<u32x2*>(base + kv8_values(BS) + ((t0 / kOct * 16 + c % 16) * 8 + c / 16) * kOct);
+                    u32x2 unit = {x[4 * i] | x[4 * i + 1] << 16, x[4 * i + 2] | x[4 * i + 3] << 16};
+                    if (held[o]) {
+                        u32x2 was = *dst;
+#pragma unroll
+                        for (int n = 0; n < 2; ++n) {
+                            if (vs.rescale != 1.f) was[n] = kv8_rescale4(was[n], vs.rescale);
+                            unit[n] = (unit[n] & mine[n]) | (was[n] & ~mine[n]);
+                        }
+                    }
+                    *dst = unit;
+                }
+            }
+        }
+    }
+}
+
+template <int DT, int BS>
+static void launch_append8_t(const CacheArgs& a, hipStream_t st) {
+    const int32_t per = (int64_t)a.rows * a.Hkv > kRunRows ? BS / 2 : 1;
+    const int64_t groups = ((int64_t)a.rows + per - 1) / per;
+    const dim3 grid((unsigned)a.Hkv, (unsigned)(groups < kCacheGrid ? groups : kCacheGrid));
+    hipLaunchKernelGGL((append8_kernel<DT, BS>), grid, dim3(BS / 16 * kWave), 0, st, a, per);
+}
+
+template <int DT, int BS, int BITS>
 static void launch_cache_t(const CacheArgs& a, bool append, hipStream_t st) {
     const int32_t per = (int64_t)a.rows * a.Hkv > kRunRows ? kOct : 1;
     const int64_t groups = ((int64_t)a.rows + kCacheWaves * per - 1) / (kCacheWaves * per);
     const dim3 grid((unsigned)a.Hkv, (unsigned)(groups < kCacheGrid ? groups : kCacheGrid));
-    if (append) hipLaunchKernelGGL((cache_kernel<DT, BS, KV4, true>), grid, dim3(kCacheThreads), 0, st, a, per);
-    else hipLaunchKernelGGL((cache_kernel<DT, BS, KV4, false>), grid, dim3(kCacheThreads), 0, st, a, per);
+    if constexpr (BITS == 8) {
+        if (append) return launch_append8_t<DT, BS>(a, st);
+    } else {
+        if (append) hipLaunchKernelGGL((cache_kernel<DT, BS, BITS, true>), grid, dim3(kCacheThreads), 0, st, a, per);
+    }
+    if (!append) hipLaunchKernelGGL((cache_kernel<DT, BS, BITS, false>), grid, dim3(kCacheThreads), 0, st, a, per);
 }
 
-template <int DT, bool KV4>
+template <int DT, int BITS>
 static void launch_cache_bs(int32_t bs, const CacheArgs& a, bool append, hipStream_t st) {
-    if (bs == 16) launch_cache_t<DT, 16, KV4>(a, append, st);
-    else if (bs == 32) launch_cache_t<DT, 32, KV4>(a, append, st);
-    else launch_cache_t<DT, 64, KV4>(a, append, st);
+    if (bs == 16) launch_cache_t<DT, 16, BITS>(a, append, st);
+    else if (bs == 32) launch_cache_t<DT, 32, BITS>(a, append, st);
+    else launch_cache_t<DT, 64, BITS>(a, append, st);
 }
 
 static hipError_t launch_cache(const pulse_shape& s, const CacheArgs& a, bool append, hipStream_t st) {
     // copies of 16-bit elements do not look at their type
-    if (!is_kv4(s.dtype)) launch_cache_bs<PULSE_BF16, false>(s.block_size, a, append, st);
-    else if (elem_type(s.dtype) == PULSE_BF16) launch_cache_bs<PULSE_BF16, true>(s.block_size, a, append, st);
-    else launch_cache_bs<PULSE_F16, true>(s.block_size, a, append, st);
+    const bool bf16 = elem_type(s.dtype) == PULSE_BF16;
+    const int bits = kv_bits(s.dtype);
+    if (bits == 16) launch_cache_bs<PULSE_BF16, 16>(s.block_size, a, append, st);
+    else if (bits == 8 && bf16) launch_cache_bs<PULSE_BF16, 8>(s.block_size, a, append, st);
+    else if (bits == 8) launch_cache_bs<PULSE_F16, 8>(s.block_size, a, append, st);
+    else if (bf16) launch_cache_bs<PULSE_BF16, 4>(s.block_size, a, append, st);
+    else launch_cache_bs<PULSE_F16, 4>(s.block_size, a, append, st);
     return hipGetLastError();
 }
 

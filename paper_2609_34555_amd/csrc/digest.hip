@@ -13,6 +13,7 @@
 // kernels are HBM-bound streams over the digests (512 B per block); one
 // 16-lane group owns one block, each lane 8 channels (one 16-byte load).
 #include "kv4.h"
+#include "kv8.h"
 
 namespace pulse {
 
@@ -63,6 +64,14 @@ __global__ __launch_bounds__(256) void build_digests_kernel(const uint16_t* __re
             const uint32_t scale = K[kv4_key_scales(BS) + row * kGroups + c8 / kGroup];
             v[i] = __builtin_bit_cast(u32x4, kv4_decode8<elem_type(DT)>(code, kv4_scale(scale)));
         }
+    } else if constexpr (is_kv8(DT)) {
+        const uint8_t* blk = reinterpret_cast<const uint8_t*>(kv) + (size_t)b * kv8_block_bytes(Hkv, BS);
+        const uint8_t* K = blk + (size_t)kv_head * kv8_head_bytes(BS);
+        const float scale = kv8_pow2((int)blk[kv8_scales(Hkv, BS) + 2 * kv_head] - 127);
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            v[i] = __builtin_bit_cast(u32x4, kv8_decode8<elem_type(DT)>(
+                       *reinterpret_cast<const u32x2*>(K + (4 * i + tg) * kHeadDim + c8), scale));
     } else {
         const size_t E = (size_t)2 * Hkv * BS * kHeadDim;
         const uint16_t* K = kv + (size_t)b * E + (size_t)kv_head * BS * kHeadDim + tg * kHeadDim + c8;
@@ -360,6 +369,8 @@ hipError_t launch_build_digests(const pulse_shape& s, const void* kv, const int6
     else PULSE_DIGEST(64, DT)
     if (s.dtype == PULSE_F16_KV4) { PULSE_DIGEST_BS(PULSE_F16_KV4); }
     else if (s.dtype == PULSE_BF16_KV4) { PULSE_DIGEST_BS(PULSE_BF16_KV4); }
+    else if (s.dtype == PULSE_F16_KV8) { PULSE_DIGEST_BS(PULSE_F16_KV8); }
+    else if (s.dtype == PULSE_BF16_KV8) { PULSE_DIGEST_BS(PULSE_BF16_KV8); }
     else { PULSE_DIGEST_BS(PULSE_BF16); }
 #undef PULSE_DIGEST_BS
 #undef PULSE_DIGEST

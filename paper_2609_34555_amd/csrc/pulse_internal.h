@@ -27,11 +27,14 @@ constexpr int kMaxBatch = 4096;   // requests per call: the recall and publish k
 
 // ---- dtypes -----------------------------------------------------------------
 
-// 16-bit type of the queries and rows of a dtype, and whether its cache is held in 4 bits.
+// 16-bit type of the queries and rows of a dtype, and whether its cache is held in 4 or in 8 bits.
 __host__ __device__ constexpr int elem_type(int dtype) {
-    return dtype == PULSE_BF16 || dtype == PULSE_BF16_KV4 ? PULSE_BF16 : PULSE_F16;
+    return dtype == PULSE_BF16 || dtype == PULSE_BF16_KV4 || dtype == PULSE_BF16_KV8 ? PULSE_BF16 : PULSE_F16;
 }
 __host__ __device__ constexpr bool is_kv4(int dtype) { return dtype == PULSE_F16_KV4 || dtype == PULSE_BF16_KV4; }
+__host__ __device__ constexpr bool is_kv8(int dtype) { return dtype == PULSE_F16_KV8 || dtype == PULSE_BF16_KV8; }
+// Bits of a cached element.
+__host__ __device__ constexpr int kv_bits(int dtype) { return is_kv4(dtype) ? 4 : is_kv8(dtype) ? 8 : 16; }
 
 // ---- timed launches ---------------------------------------------------------
 
@@ -170,7 +173,7 @@ int64_t attn_partials_most(const pulse_shape& s, int32_t B, int32_t k_max);
 WsLayout ws_layout(const pulse_shape& s, int32_t B, int32_t k_max, int64_t total_blocks);
 size_t ws_bytes_most(const pulse_shape& s, int32_t B, int32_t k_max, int64_t total_blocks);
 bool shape_supported(const pulse_shape* s);      // a 16-bit cache
-bool kv_shape_supported(const pulse_shape* s);   // a 16-bit or a 4-bit cache
+bool kv_shape_supported(const pulse_shape* s);   // a 16-bit, an 8-bit or a 4-bit cache
 
 // ---- launchers (each returns hipSuccess or the launch error) --------------
 

@@ -29,6 +29,8 @@ PULSE_F16 = 0
 PULSE_BF16 = 1
 PULSE_F16_KV4 = 2  # 16-bit queries and rows, KV blocks in 4 bits
 PULSE_BF16_KV4 = 3
+PULSE_F16_KV8 = 5  # in 8 bits
+PULSE_BF16_KV8 = 6
 
 EXPORTED = (
     "pulse_status_string", "pulse_block_bytes", "pulse_workspace_bytes", "pulse_build_digests",
