@@ -625,6 +625,47 @@ PULSE_API pulse_status pulse_load_kv(const pulse_shape* shape, const void* slot_
                                      const int64_t* slot_map, int32_t n_rows, void* k, int64_t k_stride, void* v,
                                      int64_t v_stride, int32_t* dev_status, pulse_stream_t stream);
 
+/*
+ * Attention of a step's new tokens over the cache: whole prompts, the next part of
+ * a prompt that is taken in parts, or a few tokens of each request (drafted
+ * tokens to be verified).  Request r's new tokens are rows tok_off[r] ..
+ * tok_off[r+1] - 1 (as pulse_build_tables packs them) and the last of its
+ * ctx_len[r] tokens; the row of position p, query head hq (KV head h = hq / G):
+ *   logit_t = sm_scale * q[row][hq] . K(h, t)   over the tokens t = 0 .. p,
+ *             read from slot_pool[block_table[r][t / bs]]
+ *   out[row][hq] = sum_t softmax(logit)_t V(h, t)   (rounded to the 16-bit type)
+ *   lse[row][hq] = log sum_t exp(logit_t)           (fp32, optional)
+ * so the new tokens' own keys and values are in the cache before the call
+ * (pulse_append_kv).  The cache may be in 16, 8 or 4 bits.  Products and sums in
+ * fp32; probabilities are rounded to the 16-bit type before they meet V.
+ *   q            device rows of 16-bit elements, row i at i * q_stride elements,
+ *                its heads one after another (out: the same at out_stride)
+ *   tok_off      device int32 [B+1];  ctx_len  device int32 [B]
+ *   max_tokens   rows that q and out have room for; rows from tok_off[B] on are
+ *                neither read nor written, so that a captured step may be padded
+ *   lse          device float [max_tokens][Hq] or NULL
+ *   ws           pulse_prompt_workspace_bytes() bytes of device memory; one of that
+ *                size serves any call with the same or smaller B, max_tokens and
+ *                max_blocks
+ * PULSE_ERR_BAD_INDEX if a request's offsets are out of order or outside
+ * [0, max_tokens] (its rows are then undefined), if ctx_len[r] is less than its
+ * new tokens or more than max_blocks blocks (its rows get out = 0, lse = -inf), or
+ * if a block of the context has no slot (its tokens count nothing; a row without
+ * any gets out = 0, lse = -inf).  The order of a row's sums depends on the shape, B,
+ * max_tokens, max_blocks and the request's own lengths and offset; the same call
+ * repeats its bits.
+ * out must overlap no input.  q, out and the pool are 16-byte aligned, strides
+ * multiples of 8 that hold the heads (else PULSE_ERR_INVALID_ARG); B <= 4096 and
+ * max_tokens * G < 2^28 (else PULSE_ERR_UNSUPPORTED).
+ */
+PULSE_API size_t pulse_prompt_workspace_bytes(const pulse_shape* shape, int32_t B, int64_t max_tokens,
+                                              int32_t max_blocks);
+PULSE_API pulse_status pulse_prompt_attn(const pulse_shape* shape, const void* q, int64_t q_stride,
+                                         const int32_t* tok_off, int64_t max_tokens, const int32_t* ctx_len, int32_t B,
+                                         const void* slot_pool, int32_t n_slots, const int32_t* block_table,
+                                         int32_t max_blocks, float sm_scale, void* out, int64_t out_stride, float* lse,
+                                         int32_t* dev_status, void* ws, size_t ws_bytes, pulse_stream_t stream);
+
 /* ---- Interruptible layer-wise scheduling (IRQ, Sec. 4.2) ---- */
 
 /*

@@ -564,6 +564,37 @@ pulse_status pulse_load_kv(const pulse_shape* shape, const void* slot_pool, int3
                                      dev_status, (hipStream_t)stream));
 }
 
+static bool prompt_fits(const pulse_shape& s, int64_t max_tokens) {
+    return max_tokens * (s.num_q_heads / s.num_kv_heads) < kMaxPromptRows;
+}
+
+size_t pulse_prompt_workspace_bytes(const pulse_shape* shape, int32_t B, int64_t max_tokens, int32_t max_blocks) {
+    if (!kv_shape_supported(shape) || B < 0 || B > kMaxBatch || max_tokens < 0 || max_tokens > INT32_MAX || max_blocks < 1 ||
+        !prompt_fits(*shape, max_tokens))
+        return 0;
+    return prompt_ws_bytes(*shape, B, max_tokens, max_blocks);
+}
+
+pulse_status pulse_prompt_attn(const pulse_shape* shape, const void* q, int64_t q_stride, const int32_t* tok_off,
+                               int64_t max_tokens, const int32_t* ctx_len, int32_t B, const void* slot_pool,
+                               int32_t n_slots, const int32_t* block_table, int32_t max_blocks, float sm_scale, void* out,
+                               int64_t out_stride, float* lse, int32_t* dev_status, void* ws, size_t ws_bytes,
+                               pulse_stream_t stream) {
+    PULSE_REQUIRE(shape, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(kv_shape_supported(shape), PULSE_ERR_UNSUPPORTED);
+    PULSE_REQUIRE(B >= 0 && max_tokens >= 0 && max_blocks >= 1 && n_slots >= 1, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(B <= kMaxBatch && max_tokens <= INT32_MAX && prompt_fits(*shape, max_tokens), PULSE_ERR_UNSUPPORTED);
+    if (B == 0 || max_tokens == 0) return PULSE_OK;
+    PULSE_REQUIRE(q && tok_off && ctx_len && slot_pool && block_table && out && dev_status, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(rows_ok(q, q_stride, shape->num_q_heads) && rows_ok(out, out_stride, shape->num_q_heads),
+                  PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(reinterpret_cast<uintptr_t>(slot_pool) % 16 == 0, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(ws && ws_bytes >= prompt_ws_bytes(*shape, B, max_tokens, max_blocks), PULSE_ERR_WORKSPACE);
+    return hip_status(launch_prompt_attn(*shape, q, q_stride, tok_off, max_tokens, ctx_len, B, slot_pool, n_slots,
+                                         block_table, max_blocks, sm_scale, out, out_stride, lse, dev_status, ws,
+                                         (hipStream_t)stream));
+}
+
 pulse_status pulse_probe_hbm_read(const void* src, size_t bytes, void* sink, void* start_event, void* stop_event,
                                   pulse_stream_t stream) {
     PULSE_REQUIRE(bytes % 16 == 0 && (src || bytes == 0) && sink, PULSE_ERR_INVALID_ARG);

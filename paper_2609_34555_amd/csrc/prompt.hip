@@ -1,0 +1,559 @@
+// prompt.hip -- attention of new tokens (whole prompts, or the last tokens of longer contexts) over the slot pool, for
+// gfx950.  Token i of request r's new tokens stands at position p = ctx - new + i and attends to tokens 0 .. p.
+//
+// The G query heads of a KV head share its keys and values, so the rows of the contraction are (token, query head of the
+// group) in this order: row m is token m / G, head m % G.  A workgroup takes W * 32 rows, a wave 32 of them, and goes
+// through the context in tiles of 64 keys that are staged in LDS, the next one while this one is multiplied:
+//   S^T[64 keys x 32 rows]     = K[64 x 128] . Q^T[128 x 32]
+//   O^T[128 channels x 32 rows] += V^T[128 x 64] . P^T[64 x 32]
+// on v_mfma_f32_32x32x16.  With the rows of the K operand assigned to keys by key_of_row, a lane's accumulators of S^T
+// are its operand of the second product: probabilities never leave its registers, and as the accumulators of O^T have
+// the same column, maxima, sums and rescaling are a lane's own but for one exchange between the wave's halves.  Keys lie
+// token by token and values channel by channel in the 16-bit cache, which is what either operand takes, so no tile is
+// transposed.
+//
+// Precision: products of 16-bit factors, exact, summed in fp32; maxima, sums and rescaling in fp32.  Probabilities are
+// rounded to the 16-bit type for the second product (half a step of it, at random, beside half a step of the output's own
+// rounding to the same type); their sum is that of the values before rounding.
+#include <algorithm>
+
+#include "kv4.h"
+#include "kv8.h"
+
+namespace pulse {
+
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+
+constexpr int kKeys = 64;                     // keys of a tile
+constexpr int kRowsPerWave = 32;
+constexpr int kWaves = 4;                     // of a workgroup
+constexpr int kTileBytes = kKeys * kHeadDim * 2;  // of keys, and of values, in LDS
+
+template <int ET>
+__device__ inline f32x16 mac32(typename Mfma<ET>::vec a, typename Mfma<ET>::vec b, f32x16 c) {
+    if constexpr (ET == PULSE_BF16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+// Two floats as 16-bit values, rounded to nearest.
+template <int ET>
+__device__ inline uint32_t pack2(float a, float b) {
+    if constexpr (ET == PULSE_BF16) {
+        const bf16x2 v = {(__bf16)a, (__bf16)b};
+        return __builtin_bit_cast(uint32_t, v);
+    } else {
+        const f16x2 v = {(_Float16)a, (_Float16)b};
+        return __builtin_bit_cast(uint32_t, v);
+    }
+}
+
+// Key (of 32) that row m of the K operand holds: accumulator register 4 b + i of lane half h is row 8 b + 4 h + i, and
+// the operand of 16 keys takes 8 h + 0 .. 7 from half h.
+__device__ constexpr int key_of_row(int m) { return 16 * (m >> 4) + 8 * (m >> 2 & 1) + 4 * (m >> 3 & 1) + (m & 3); }
+
+// Places of 16-byte pieces in the LDS tiles, changed so that the lanes that read together read different banks.
+// Keys: piece c of a key's 16.  Values: octet o of the BS / 8 that a block has of a channel.
+__device__ inline int key_piece(int key, int c) { return c ^ ((key & 3) | (key >> 3 & 1) << 2 | (key >> 2 & 1) << 3); }
+template <int BS>
+__device__ inline int value_octet(int c, int o) {
+    if constexpr (BS == 16) return o ^ ((c >> 2 ^ c >> 3) & 1);
+    else if constexpr (BS == 32) return o ^ ((c >> 1 ^ (c >> 3 & 1)) & 3);
+    else return o ^ ((c ^ c >> 3) & 7);
+}
+
+struct PromptArgs {
+    const uint16_t* q;
+    int64_t q_stride;
+    const int32_t* tok_off;
+    const int32_t* ctx_len;
+    int32_t B, max_tokens;
+    const uint8_t* pool;
+    int32_t n_slots;
+    const int32_t* table;
+    int32_t max_blocks;
+    int32_t Hkv, G;
+    uint64_t g_magic;       // m / G = m * g_magic >> 32 for rows m below 2^28
+    float scale_log2;
+    uint16_t* out;
+    int64_t out_stride;
+    float* lse;
+    float* ws_o;            // [n_split][max_tokens * Hq][128]
+    float2* ws_ml;
+    int32_t n_tiles, n_split;
+    int32_t* status;
+};
+
+// The request and tile of rows that a place in the grid stands for.  Request r's tiles take places first(r) = tok_off[r]
+// * G / rows + r and on: as many as it needs are free before first(r + 1), so no sum over the requests is needed.
+struct Place {
+    int r, tile;
+};
+__device__ inline Place find_place(const int32_t* __restrict__ tok_off, int32_t B, int32_t G, int rows, int at) {
+    int lo = 0, hi = B - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if ((int64_t)tok_off[mid] * G / rows + mid <= at) lo = mid;
+        else hi = mid - 1;
+    }
+    return Place{lo, at - (int)((int64_t)tok_off[lo] * G / rows + lo)};
+}
+
+// Tile `t` of the cache of KV head h into LDS, 16-bit blocks: 1 KiB a wave and instruction, straight from memory.
+template <int BS, int W>
+__device__ inline void stage16(const PromptArgs& a, const int (&slot)[kKeys / BS], int h, uint8_t* lds, int wave, int lane) {
+    const size_t E = (size_t)2 * a.Hkv * BS * kHeadDim * 2;
+    constexpr int kParts = kTileBytes / 1024;
+    constexpr int kBlockParts = kParts / (kKeys / BS);  // of a block's keys, and of its values
+#pragma unroll
+    for (int i = 0; i < kParts / W; ++i) {
+        const int part = i * W + wave, blk = part / kBlockParts, in = part % kBlockParts;
+        const int s = __builtin_amdgcn_readfirstlane(slot[blk]);
+        const uint8_t* k = a.pool + (size_t)s * E + (size_t)h * BS * kHeadDim * 2;
+        const uint8_t* v = k + (size_t)a.Hkv * BS * kHeadDim * 2;
+        const int key = in * 4 + (lane >> 4);  // within the block
+        const uint8_t* ks = k + key * 256 + key_piece(key % 32, lane & 15) * 16;
+        constexpr int kOct = BS / 8;
+        const int c = in * (64 / kOct) + lane / kOct;
+        const uint8_t* vs = v + (c * kOct + value_octet<BS>(c, lane % kOct)) * 16;
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)ks,
+                                         (__attribute__((address_space(3))) void*)(lds + part * 1024), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)vs,
+                                         (__attribute__((address_space(3))) void*)(lds + kTileBytes + part * 1024), 16, 0, 0);
+    }
+}
+
+// The same tile of 8-bit or 4-bit blocks: fetch() loads codes and scales, a 16-byte piece at a time, into registers; put()
+// decodes them, exactly, into the 16-bit type and writes what stage16 would have written.  Decoding costs a workgroup
+// once what W waves then use.
+template <int DT, int BS, int W>
+struct Codes {
+    static constexpr int ET = elem_type(DT);
+    static constexpr int kThreads = W * kWave;
+    static constexpr bool k4 = is_kv4(DT);
+    static constexpr int kUnits = kKeys * kHeadDim / (k4 ? 32 : 16);  // pieces of keys, and of values
+    static constexpr int kEach = (kUnits + kThreads - 1) / kThreads;
+    static constexpr int kPer = k4 ? 4 : 8;  // pieces of a key
+    u32x4 k[kEach], v[kEach];
+    uint32_t ks[kEach];  // 8 bits: exponent byte of the piece's block (keys low, values high, of their blocks); 4: its scale
+    u32x2 vs[kEach][2];  // 4 bits: scale bytes of 8 tokens, of the piece's two channel groups
+
+    // Piece u of keys: key u / kPer, of values: octet u / (kUnits / 8).  A wave's pieces lie in one block.
+    __device__ inline void fetch(const PromptArgs& a, const int (&slot)[kKeys / BS], int h, int tid) {
+        const size_t U = k4 ? (size_t)a.Hkv * kv4_head_bytes(BS) : (size_t)kv8_block_bytes(a.Hkv, BS);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int u = i * kThreads + tid;
+            if (kUnits % kThreads && u >= kUnits) break;
+            const int key = u / kPer, oct = u / (kUnits / 8);
+            const uint8_t* kb = a.pool + (size_t)__builtin_amdgcn_readfirstlane(slot[key / BS]) * U;
+            const uint8_t* vb = a.pool + (size_t)__builtin_amdgcn_readfirstlane(slot[oct * 8 / BS]) * U;
+            if constexpr (k4) {
+                kb += (size_t)h * kv4_head_bytes(BS);
+                vb += (size_t)h * kv4_head_bytes(BS);
+                k[i] = *reinterpret_cast<const u32x4*>(kb + key % BS * 64 + u % 4 * 16);
+                ks[i] = kb[kv4_key_scales(BS) + key % BS * kGroups + u % 4];
+                const int at = u % 32;  // channels at / 2 + 16 * (4 * (at % 2) + 0 .. 3)
+                v[i] = *reinterpret_cast<const u32x4*>(vb + kv4_values(BS) + oct % (BS / 8) * 512 + at * 16);
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+                    vs[i][n] = *reinterpret_cast<const u32x2*>(vb + kv4_value_scales(BS) + (2 * (at % 2) + n) * BS +
+                                                               oct % (BS / 8) * 8);
+            } else {
+                const size_t head = (size_t)h * kv8_head_bytes(BS), scale = (size_t)kv8_scales(a.Hkv, BS) + 2 * h;
+                k[i] = *reinterpret_cast<const u32x4*>(kb + head + key % BS * kHeadDim + u % 8 * 16);
+                const int at = u % 64;  // channels at / 4 + 16 * (2 * (at % 4) + 0 .. 1)
+                v[i] = *reinterpret_cast<const u32x4*>(vb + head + kv8_values(BS) + oct % (BS / 8) * 1024 + at * 16);
+                ks[i] = kb[scale] | (uint32_t)vb[scale + 1] << 8;
+            }
+        }
+    }
+
+    __device__ inline void put(uint8_t* lds, int tid) const {
+        uint8_t* vals = lds + kTileBytes;
+        constexpr int kOct = BS / 8;
+        auto value_at = [&](int oct, int c) {
+            return reinterpret_cast<u32x4*>(vals + oct / kOct * (256 * BS) + (c * kOct + value_octet<BS>(c, oct % kOct)) * 16);
+        };
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int u = i * kThreads + tid;
+            if (kUnits % kThreads && u >= kUnits) break;
+            const int key = u / kPer, oct = u / (kUnits / 8);
+            if constexpr (k4) {
+                const int at = u % 32;
+                const float scale = kv4_scale(ks[i]);
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    *reinterpret_cast<u32x4*>(lds + key * 256 + key_piece(key % 32, 4 * (u % 4) + n) * 16) =
+                        __builtin_bit_cast(u32x4, kv4_decode8<ET>(k[i][n], scale));
+                    // 8 tokens, a scale each
+                    const u32x2 sb = vs[i][n / 2];
+                    u32x4 w;
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const float s0 = kv4_scale(sb[t / 2] >> (16 * (t % 2)) & 255u);
+                        const float s1 = kv4_scale(sb[t / 2] >> (16 * (t % 2) + 8) & 255u);
+                        w[t] = (decode_pair(v[i][n], t, s0) & 0xFFFFu) | (decode_pair(v[i][n], t, s1) & 0xFFFF0000u);
+                    }
+                    *value_at(oct, at / 2 + 16 * (4 * (at % 2) + n)) = w;
+                }
+            } else {
+                const int at = u % 64;
+                const float kf = kv8_pow2((int)(ks[i] & 255) - 127), vf = kv8_pow2((int)(ks[i] >> 8) - 127);
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    *reinterpret_cast<u32x4*>(lds + key * 256 + key_piece(key % 32, 2 * (u % 8) + n) * 16) =
+                        __builtin_bit_cast(u32x4, kv8_decode8<ET>(u32x2{k[i][2 * n], k[i][2 * n + 1]}, kf));
+                    *value_at(oct, at / 4 + 16 * (2 * (at % 4) + n)) =
+                        __builtin_bit_cast(u32x4, kv8_decode8<ET>(u32x2{v[i][2 * n], v[i][2 * n + 1]}, vf));
+                }
+            }
+        }
+    }
+
+    // Codes of byte t of w times `scale`.
+    __device__ static inline uint32_t decode_pair(uint32_t w, int t, float scale) {
+        return t == 0 ? kv4_decode<ET, 0>(w, scale) : t == 1 ? kv4_decode<ET, 1>(w, scale)
+             : t == 2 ? kv4_decode<ET, 2>(w, scale) : kv4_decode<ET, 3>(w, scale);
+    }
+};
+
+// This wave's pieces are in LDS, and so are the others', which are done with the other tile.
+__device__ inline void tile_arrived() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
+// grid = Hkv * n_tiles * n_split workgroups: neighbours take the KV heads of one tile (a head's tiles then mostly run on
+// one XCD, whose L2 holds its keys), splits next, and the last tiles, which attend to the most keys, begin first.
+template <int DT, int BS, int W>
+__global__ __launch_bounds__(W * kWave, 2) void prompt_kernel(PromptArgs a) {
+    constexpr int ET = elem_type(DT);
+    using vec = typename Mfma<ET>::vec;
+    constexpr int kRows = W * kRowsPerWave;
+    constexpr int kBlocks = kKeys / BS;
+    __shared__ __align__(1024) uint8_t s_tile[2][2 * kTileBytes];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const int h = blockIdx.x % a.Hkv;
+    const int rest = blockIdx.x / a.Hkv;
+    const int split = rest % a.n_split;
+    const Place pl = find_place(a.tok_off, a.B, a.G, kRows, a.n_tiles - 1 - rest / a.n_split);
+    const int t0 = a.tok_off[pl.r], t1 = a.tok_off[pl.r + 1], ctx = a.ctx_len[pl.r];
+    if (blockIdx.x == 0) {  // every request's lengths
+        for (int r = threadIdx.x; r < a.B; r += W * kWave) {
+            const int64_t x = a.tok_off[r], y = a.tok_off[r + 1], c = a.ctx_len[r];
+            if (x < 0 || y < x || y > a.max_tokens || c < y - x || c > (int64_t)a.max_blocks * BS)
+                report(a.status, PULSE_ERR_BAD_INDEX);
+        }
+    }
+    if (t0 < 0 || t1 < t0 || t1 > a.max_tokens) return;
+    const int fresh = t1 - t0;
+    const int64_t n_rows = (int64_t)fresh * a.G;
+    const int64_t row0 = (int64_t)pl.tile * kRows;
+    if (pl.tile < 0 || row0 >= n_rows) return;
+    const bool ok = ctx >= fresh && ctx <= (int64_t)a.max_blocks * BS;  // else no token is attended to
+    const int base = ctx - fresh;
+    // this lane's row
+    const int64_t m = row0 + wave * kRowsPerWave + col;
+    const bool live = m < n_rows;
+    const int mi = (int)(live ? m : n_rows - 1);
+    const int tok = (int)((uint64_t)mi * a.g_magic >> 32);
+    const int g = mi - tok * a.G;
+    const int p = base + tok;  // its position
+    const int Hq = a.Hkv * a.G;
+    const int64_t wave_row = row0 + wave * kRowsPerWave;
+    // keys that the workgroup, and the wave, attend to at all; keys that all of the wave's rows attend to
+    auto token_of = [&](int64_t row) { return (int)((uint64_t)min(row, n_rows - 1) * a.g_magic >> 32); };
+    const int wg_keys = ok ? base + token_of(row0 + kRows - 1) + 1 : 0;
+    const int wave_keys = wave_row < n_rows && ok ? base + token_of(wave_row + kRowsPerWave - 1) + 1 : 0;
+    const int wave_all = base + token_of(wave_row) + 1;
+    const int n_kt = (wg_keys + kKeys - 1) / kKeys;
+    const int kt0 = (int)((int64_t)n_kt * split / a.n_split), kt1 = (int)((int64_t)n_kt * (split + 1) / a.n_split);
+
+    vec qb[8];
+    {
+        const uint16_t* qr = a.q + (int64_t)(t0 + tok) * a.q_stride + (size_t)(h * a.G + g) * kHeadDim + half * 8;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) qb[c] = load_vec<ET>(qr + 16 * c);
+        // logits are scaled after their maximum is taken: the sign of the scale goes to Q, a zero becomes tiny
+        if (a.scale_log2 < 0.f) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) qb[c] = -qb[c];
+        }
+    }
+    const float scale = fmaxf(fabsf(a.scale_log2), 1e-30f);
+    f32x16 acc[4] = {};
+    float m_run = -INFINITY, l_run = 0.f;
+
+    // slots of a tile's blocks, read one tile ahead; a block without one is looked at as slot 0 and counts nothing
+    const auto* row = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(a.table + (size_t)pl.r * a.max_blocks);
+    const int n_blk = ok ? (ctx + BS - 1) / BS : 0;
+    int next[kBlocks];
+    auto look_up = [&](int kt) {
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) next[b] = row[min(kt * kBlocks + b, n_blk - 1)];
+    };
+    Codes<DT, BS, W> codes;
+    uint32_t bad = 0;  // blocks without a slot of the tile staged last
+    auto stage = [&](int kt, int buf) {
+        bad = 0;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+            if ((uint32_t)next[b] >= (uint32_t)a.n_slots) {
+                bad |= 1u << b;
+                next[b] = 0;
+            }
+        if constexpr (kv_bits(DT) == 16) stage16<BS, W>(a, next, h, s_tile[buf], wave, lane);
+        else codes.fetch(a, next, h, threadIdx.x);
+        if (bad && threadIdx.x == 0) report(a.status, PULSE_ERR_BAD_INDEX);
+        if (kt + 1 < kt1) look_up(kt + 1);
+    };
+    uint32_t bad_now = 0;
+    if (kt0 < kt1) {
+        look_up(kt0);
+        stage(kt0, 0);
+        bad_now = bad;
+        if constexpr (kv_bits(DT) != 16) codes.put(s_tile[0], threadIdx.x);
+    }
+    tile_arrived();
+    int buf = 0;
+#pragma unroll 1
+    for (int kt = kt0; kt < kt1; ++kt, buf ^= 1) {
+        if (kt + 1 < kt1) stage(kt + 1, buf ^ 1);
+        const int k0 = kt * kKeys;
+        uint8_t* ks = s_tile[buf];
+        uint8_t* vs = s_tile[buf] + kTileBytes;
+        if (k0 + kKeys > ctx || bad_now) {
+            // behind a context's end lies what an earlier owner of the slot left, NaN perhaps, which a probability of 0
+            // would not take out of the product; and a block without a slot was read from another's
+            for (int i = threadIdx.x; i < kTileBytes / 16; i += W * kWave) {
+                constexpr int kOct = BS / 8;
+                const int c = i / kOct % kHeadDim, o = i % kOct, blk = i / (kOct * kHeadDim);
+                const int end = bad_now >> blk & 1 ? 0 : ctx - k0 - blk * BS - 8 * value_octet<BS>(c, o);
+                u32x4* at = reinterpret_cast<u32x4*>(vs) + i;
+                if (end < 8) {
+                    u32x4 v = *at;
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+                        v[n] &= (2 * n < end ? 0xFFFFu : 0u) | (2 * n + 1 < end ? 0xFFFF0000u : 0u);
+                    *at = v;
+                }
+            }
+            __syncthreads();
+        }
+        if (k0 < wave_keys) {
+            f32x16 s[2] = {};
+            const int key = key_of_row(col);
+#pragma unroll
+            for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    const vec kv = __builtin_bit_cast(vec, *reinterpret_cast<const u32x4*>(
+                                                               ks + (32 * sub + key) * 256 + key_piece(key, 2 * c + half) * 16));
+                    s[sub] = mac32<ET>(kv, qb[c], s[sub]);
+                }
+            float x[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[i] = s[i / 16][i % 16];
+            if (k0 + kKeys > wave_all) {
+                const int left = p + 1 - k0 - 8 * half;  // keys of this half's numbering that the row attends to
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (32 * (i / 16) + 16 * (i % 16 / 8) + i % 8 >= left) x[i] = -INFINITY;
+            }
+            if (bad_now) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const int k = 32 * (i / 16) + 16 * (i % 16 / 8) + i % 8 + 8 * half;
+                    if (bad_now >> (k / BS) & 1) x[i] = -INFINITY;
+                }
+            }
+            float cm = x[0];
+#pragma unroll
+            for (int i = 1; i < 32; ++i) cm = __builtin_elementwise_maximum(cm, x[i]);
+            {
+                const uint32_t u = __float_as_uint(cm);
+                const u32x2 w = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+                cm = __builtin_elementwise_maximum(__uint_as_float(w[0]), __uint_as_float(w[1]));
+            }
+            const float m_new = __builtin_elementwise_maximum(m_run, cm * scale);
+            const float m_use = m_new == -INFINITY ? 0.f : m_new;
+            const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
+            m_run = m_new;
+            float psum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], scale, -m_use));
+                psum += x[i];
+            }
+            l_run = l_run * alpha + psum;
+            if (__ballot(alpha != 1.f)) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) acc[t] *= alpha;
+            }
+#pragma unroll
+            for (int st = 0; st < 4; ++st) {
+                const u32x4 pw = {pack2<ET>(x[8 * st], x[8 * st + 1]), pack2<ET>(x[8 * st + 2], x[8 * st + 3]),
+                                  pack2<ET>(x[8 * st + 4], x[8 * st + 5]), pack2<ET>(x[8 * st + 6], x[8 * st + 7])};
+                const vec pv = __builtin_bit_cast(vec, pw);
+                const int oct = 2 * st + half, blk = oct / (BS / 8), o = oct % (BS / 8);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const int c = 32 * t + col;
+                    const u32x4 v = *reinterpret_cast<const u32x4*>(vs + blk * (256 * BS) +
+                                                                    (c * (BS / 8) + value_octet<BS>(c, o)) * 16);
+                    acc[t] = mac32<ET>(__builtin_bit_cast(vec, v), pv, acc[t]);
+                }
+            }
+        }
+        bad_now = bad;
+        if constexpr (kv_bits(DT) != 16)
+            if (kt + 1 < kt1) codes.put(s_tile[buf ^ 1], threadIdx.x);
+        tile_arrived();
+    }
+    {
+        const uint32_t u = __float_as_uint(l_run);
+        const u32x2 w = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        l_run = __uint_as_float(w[0]) + __uint_as_float(w[1]);
+    }
+    const int64_t at = (int64_t)(t0 + tok) * Hq + h * a.G + g;
+    if (a.n_split > 1) {
+        if (!live) return;
+        const int64_t part = (int64_t)split * a.max_tokens * Hq + at;
+        if (half == 0) a.ws_ml[part] = make_float2(m_run, l_run);
+        if (m_run == -INFINITY) return;
+        float* o = a.ws_o + part * kHeadDim + 4 * half;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                *reinterpret_cast<f32x4*>(o + 32 * t + 8 * b) = f32x4{acc[t][4 * b], acc[t][4 * b + 1], acc[t][4 * b + 2], acc[t][4 * b + 3]};
+        return;
+    }
+    const float inv = m_run == -INFINITY ? 0.f : 1.f / l_run;
+    if (live && a.lse && half == 0)
+        a.lse[at] = m_run == -INFINITY ? -INFINITY : (m_run + log2f(l_run)) * 0.69314718055994531f;
+    uint16_t* o = a.out + (int64_t)(t0 + tok) * a.out_stride + (size_t)(h * a.G + g) * kHeadDim;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int b = 0; b < 4; b += 2) {
+            // channels 8 b + 4 half .. and 8 (b + 1) + 4 half ..: half 0 takes all 8 of the first, half 1 of the second
+            u32x4 w;
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const uint32_t x = pack2<ET>(acc[t][4 * b + 2 * n] * inv, acc[t][4 * b + 2 * n + 1] * inv);
+                const uint32_t y = pack2<ET>(acc[t][4 * b + 4 + 2 * n] * inv, acc[t][4 * b + 5 + 2 * n] * inv);
+                const u32x2 r = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+                w[n] = r[0];
+                w[2 + n] = r[1];
+            }
+            if (live) *reinterpret_cast<u32x4*>(o + 32 * t + 8 * (b + half)) = w;
+        }
+}
+
+// Joins the splits of a row: a wave per two rows, a lane four channels.
+template <int ET>
+__global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
+    const int Hq = a.Hkv * a.G;
+    const int64_t rows = (int64_t)a.max_tokens * Hq;
+    const int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int c = (threadIdx.x & 31) * 4;
+    const int last = a.tok_off[a.B];
+    if (at >= (int64_t)last * Hq || last > a.max_tokens) return;
+    float mx = -INFINITY;
+    for (int s = 0; s < a.n_split; ++s) mx = fmaxf(mx, a.ws_ml[s * rows + at].x);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    float l = 0.f;
+    if (mx != -INFINITY) {
+        for (int s = 0; s < a.n_split; ++s) {
+            const float2 ml = a.ws_ml[s * rows + at];
+            if (ml.x == -INFINITY) continue;
+            const float w = __builtin_amdgcn_exp2f(ml.x - mx);
+            const f32x4 x = *reinterpret_cast<const f32x4*>(a.ws_o + (s * rows + at) * kHeadDim + c);
+            l += ml.y * w;
+            o += x * w;
+        }
+        o *= 1.f / l;
+    }
+    uint16_t* dst = a.out + at / Hq * a.out_stride + at % Hq * kHeadDim + c;
+    *reinterpret_cast<u32x2*>(dst) = u32x2{pack2<ET>(o[0], o[1]), pack2<ET>(o[2], o[3])};
+    if (a.lse && c == 0) a.lse[at] = mx == -INFINITY ? -INFINITY : (mx + log2f(l)) * 0.69314718055994531f;
+}
+
+struct PromptPlan {
+    int n_tiles, n_split;
+};
+
+constexpr int kGroups = 512;  // workgroups aimed at where few rows are split over the context: two a CU
+constexpr int kLeastTiles = 4;  // tiles of keys of a split
+
+static int64_t key_tiles(const pulse_shape& s, int32_t max_blocks) {
+    return ((int64_t)max_blocks * s.block_size + kKeys - 1) / kKeys;
+}
+
+static PromptPlan prompt_plan(const pulse_shape& s, int32_t B, int64_t max_tokens, int32_t max_blocks) {
+    PromptPlan p;
+    const int64_t G = s.num_q_heads / s.num_kv_heads, rows = kWaves * kRowsPerWave;
+    p.n_tiles = (int)(max_tokens * G / rows + B);
+    const int64_t units = std::max<int64_t>((max_tokens * G + rows - 1) / rows, B) * s.num_kv_heads;
+    p.n_split = (int)std::max<int64_t>(1, std::min(kGroups / units, key_tiles(s, max_blocks) / kLeastTiles));
+    return p;
+}
+
+static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Partials of the splits of this call and every smaller one: fewer rows may have more splits, but no more than kGroups
+// workgroups' rows, nor than the context has splits.
+size_t prompt_ws_bytes(const pulse_shape& s, int32_t B, int64_t max_tokens, int32_t max_blocks) {
+    const int64_t most = key_tiles(s, max_blocks) / kLeastTiles;
+    if (most <= 1) return 256;
+    const size_t rows = (size_t)std::min<int64_t>((int64_t)kGroups * kWaves * kRowsPerWave, most * max_tokens * s.num_q_heads);
+    return up256(rows * kHeadDim * sizeof(float)) + up256(rows * sizeof(float2));
+}
+
+template <int DT, int BS>
+static void launch_prompt_t(const PromptArgs& a, hipStream_t st) {
+    const dim3 grid((unsigned)((int64_t)a.Hkv * a.n_tiles * a.n_split));
+    hipLaunchKernelGGL((prompt_kernel<DT, BS, kWaves>), grid, dim3(kWaves * kWave), 0, st, a);
+}
+
+template <int DT>
+static void launch_prompt_bs(int32_t bs, const PromptArgs& a, hipStream_t st) {
+    if (bs == 16) launch_prompt_t<DT, 16>(a, st);
+    else if (bs == 32) launch_prompt_t<DT, 32>(a, st);
+    else launch_prompt_t<DT, 64>(a, st);
+}
+
+hipError_t launch_prompt_attn(const pulse_shape& s, const void* q, int64_t q_stride, const int32_t* tok_off,
+                              int64_t max_tokens, const int32_t* ctx_len, int32_t B, const void* pool, int32_t n_slots,
+                              const int32_t* table, int32_t max_blocks, float sm_scale, void* out, int64_t out_stride,
+                              float* lse, int32_t* status, void* ws, hipStream_t st) {
+    if (B == 0 || max_tokens == 0) return hipSuccess;
+    const PromptPlan p = prompt_plan(s, B, max_tokens, max_blocks);
+    const int32_t G = s.num_q_heads / s.num_kv_heads;
+    PromptArgs a{(const uint16_t*)q, q_stride, tok_off, ctx_len, B, (int32_t)max_tokens, (const uint8_t*)pool, n_slots, table,
+                 max_blocks, s.num_kv_heads, G, (((uint64_t)1 << 32) + G - 1) / G,
+                 sm_scale * 1.4426950408889634f, (uint16_t*)out, out_stride, lse, (float*)ws, nullptr, p.n_tiles, p.n_split,
+                 status};
+    if (p.n_split > 1)
+        a.ws_ml = ws_at<float2>(ws, up256((size_t)p.n_split * max_tokens * s.num_q_heads * kHeadDim * sizeof(float)));
+    switch (s.dtype) {
+        case PULSE_BF16: launch_prompt_bs<PULSE_BF16>(s.block_size, a, st); break;
+        case PULSE_F16: launch_prompt_bs<PULSE_F16>(s.block_size, a, st); break;
+        case PULSE_BF16_KV8: launch_prompt_bs<PULSE_BF16_KV8>(s.block_size, a, st); break;
+        case PULSE_F16_KV8: launch_prompt_bs<PULSE_F16_KV8>(s.block_size, a, st); break;
+        case PULSE_BF16_KV4: launch_prompt_bs<PULSE_BF16_KV4>(s.block_size, a, st); break;
+        case PULSE_F16_KV4: launch_prompt_bs<PULSE_F16_KV4>(s.block_size, a, st); break;
+        default: return hipErrorInvalidValue;
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.n_split == 1) return e;
+    const unsigned groups = (unsigned)((max_tokens * s.num_q_heads + 7) / 8);
+    if (elem_type(s.dtype) == PULSE_BF16) hipLaunchKernelGGL(prompt_join_kernel<PULSE_BF16>, dim3(groups), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(prompt_join_kernel<PULSE_F16>, dim3(groups), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace pulse

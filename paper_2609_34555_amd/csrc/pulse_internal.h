@@ -326,6 +326,14 @@ hipError_t launch_load_kv(const pulse_shape& s, const void* pool, int32_t n_slot
                           int32_t rows, void* k, int64_t k_stride, void* v, int64_t v_stride, int32_t* status,
                           hipStream_t st);
 
+// Attention of new tokens over the slot pool (prompt.hip).
+constexpr int64_t kMaxPromptRows = 1 << 28;  // new tokens times query heads per KV head
+size_t prompt_ws_bytes(const pulse_shape& s, int32_t B, int64_t max_tokens, int32_t max_blocks);
+hipError_t launch_prompt_attn(const pulse_shape& s, const void* q, int64_t q_stride, const int32_t* tok_off,
+                              int64_t max_tokens, const int32_t* ctx_len, int32_t B, const void* pool, int32_t n_slots,
+                              const int32_t* table, int32_t max_blocks, float sm_scale, void* out, int64_t out_stride,
+                              float* lse, int32_t* status, void* ws, hipStream_t st);
+
 // Host-side argument check: return `code` from the calling entry point.
 #define PULSE_REQUIRE(cond, code)   \
     do {                            \

@@ -44,6 +44,7 @@ EXPORTED = (
     "pulse_mam", "pulse_pick_solo_heads", "pulse_irq_create", "pulse_irq_destroy", "pulse_irq_step",
     "pulse_probe_hbm_read", "pulse_probe_hbm_sink_bytes", "pulse_release_recalled", "pulse_attention_workgroups",
     "pulse_tables_workspace_bytes", "pulse_build_tables", "pulse_qk_norm_rope", "pulse_append_kv", "pulse_load_kv",
+    "pulse_prompt_workspace_bytes", "pulse_prompt_attn",
 )
 
 
@@ -196,6 +197,9 @@ def signatures():
                                               _P]),
         "pulse_append_kv": (ctypes.c_int, [SP, _P, I64, _P, I64, _P, I32, _P, I32, _P, _P]),
         "pulse_load_kv": (ctypes.c_int, [SP, _P, I32, _P, I32, _P, I64, _P, I64, _P, _P]),
+        "pulse_prompt_workspace_bytes": (SZ, [SP, I32, I64, I32]),
+        "pulse_prompt_attn": (ctypes.c_int, [SP, _P, I64, _P, I64, _P, I32, _P, I32, _P, I32, F, _P, I64, _P, _P, _P, SZ,
+                                             _P]),
         "pulse_events_create": (ctypes.c_int, [I32, _P]),
         "pulse_events_destroy": (ctypes.c_int, [I32, _P]),
         "pulse_event_elapsed_ms": (ctypes.c_int, [_P, _P, ctypes.POINTER(ctypes.c_float)]),
@@ -348,6 +352,18 @@ def pulse_load_kv(shape, slot_pool, n_slots, slot_map, n_rows, k, k_stride, v, v
     st = lib().pulse_load_kv(ctypes.byref(shape), _ptr(slot_pool), n_slots, _ptr(slot_map), n_rows, _ptr(k), k_stride,
                              _ptr(v), v_stride, _ptr(dev_status), _stream(stream))
     return _check(st, "pulse_load_kv", check)
+
+
+def pulse_prompt_workspace_bytes(shape: pulse_shape, B: int, max_tokens: int, max_blocks: int) -> int:
+    return lib().pulse_prompt_workspace_bytes(ctypes.byref(shape), B, max_tokens, max_blocks)
+
+
+def pulse_prompt_attn(shape, q, q_stride, tok_off, max_tokens, ctx_len, B, slot_pool, n_slots, block_table, max_blocks,
+                      sm_scale, out, out_stride, lse, dev_status, ws, ws_bytes, stream=None, check=True):
+    st = lib().pulse_prompt_attn(ctypes.byref(shape), _ptr(q), q_stride, _ptr(tok_off), max_tokens, _ptr(ctx_len), B,
+                                 _ptr(slot_pool), n_slots, _ptr(block_table), max_blocks, float(sm_scale), _ptr(out),
+                                 out_stride, _ptr(lse), _ptr(dev_status), _ptr(ws), ws_bytes, _stream(stream))
+    return _check(st, "pulse_prompt_attn", check)
 
 
 def pulse_pick_solo_heads(mam, check=True):
