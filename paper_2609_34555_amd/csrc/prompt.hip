@@ -486,7 +486,7 @@ struct PromptPlan {
     int n_tiles, n_split;
 };
 
-constexpr int kGroups = 512;  // workgroups aimed at where few rows are split over the context: two a CU
+constexpr int kSplitGroups = 512;  // workgroups aimed at where few rows are split over the context: two a CU
 constexpr int kLeastTiles = 4;  // tiles of keys of a split
 
 static int64_t key_tiles(const pulse_shape& s, int32_t max_blocks) {
@@ -498,18 +498,18 @@ static PromptPlan prompt_plan(const pulse_shape& s, int32_t B, int64_t max_token
     const int64_t G = s.num_q_heads / s.num_kv_heads, rows = kWaves * kRowsPerWave;
     p.n_tiles = (int)(max_tokens * G / rows + B);
     const int64_t units = std::max<int64_t>((max_tokens * G + rows - 1) / rows, B) * s.num_kv_heads;
-    p.n_split = (int)std::max<int64_t>(1, std::min(kGroups / units, key_tiles(s, max_blocks) / kLeastTiles));
+    p.n_split = (int)std::max<int64_t>(1, std::min(kSplitGroups / units, key_tiles(s, max_blocks) / kLeastTiles));
     return p;
 }
 
 static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Partials of the splits of this call and every smaller one: fewer rows may have more splits, but no more than kGroups
+// Partials of the splits of this call and every smaller one: fewer rows may have more splits, but no more than kSplitGroups
 // workgroups' rows, nor than the context has splits.
 size_t prompt_ws_bytes(const pulse_shape& s, int32_t B, int64_t max_tokens, int32_t max_blocks) {
     const int64_t most = key_tiles(s, max_blocks) / kLeastTiles;
     if (most <= 1) return 256;
-    const size_t rows = (size_t)std::min<int64_t>((int64_t)kGroups * kWaves * kRowsPerWave, most * max_tokens * s.num_q_heads);
+    const size_t rows = (size_t)std::min<int64_t>((int64_t)kSplitGroups * kWaves * kRowsPerWave, most * max_tokens * s.num_q_heads);
     return up256(rows * kHeadDim * sizeof(float)) + up256(rows * sizeof(float2));
 }
 
