@@ -666,6 +666,61 @@ PULSE_API pulse_status pulse_prompt_attn(const pulse_shape* shape, const void* q
                                          int32_t max_blocks, float sm_scale, void* out, int64_t out_stride, float* lse,
                                          int32_t* dev_status, void* ws, size_t ws_bytes, pulse_stream_t stream);
 
+/*
+ * Blocks as pages: requests that share them, blocks given back, a pool made
+ * smaller.  The table and the free list are those of pulse_recall_gather and
+ * pulse_build_tables.  `shared` (device int32 [n_slots], zero at the start)
+ * counts of every slot the table entries that name it beyond the first, so a slot
+ * that is taken from the free list has 0 and only these calls change it.  Every
+ * length, entry, count and slot is checked before anything is written: on an
+ * error (PULSE_ERR_BAD_INDEX unless said otherwise) nothing changes.  Not to be
+ * called between a recall and its release, which undoes the last allocation.  ws:
+ * pulse_pages_workspace_bytes() bytes of device memory, which serve any of the
+ * three with the same or smaller B, max_blocks and n_slots.  B <= 4096,
+ * B * max_blocks and n_slots <= 2^30 (else PULSE_ERR_UNSUPPORTED).  Any dtype.
+ *
+ * pulse_fork_blocks: for i < n <= B request dst[i] gets the first fork_len[i]
+ *   tokens of request src[i].  Its row of the table has to be empty (all -1); it
+ *   gets the source's entries of whole blocks, which both then share (a block
+ *   that is not resident stays so), and where the length ends inside a block,
+ *   that block, which has to be resident, is copied to the next slot of the free
+ *   list (in the order of i), so that either request may append to its own.
+ *   src, dst, fork_len   device int32 [n]; no request twice in dst, none in both
+ *   PULSE_ERR_POOL_EXHAUSTED if the free list has too few slots.
+ * pulse_free_blocks: request r keeps the blocks of its first keep_len[r] tokens
+ *   (0: none; INT32_MAX: all).  The entries behind them become -1, and slots
+ *   that no entry names any more go back to the free list: with k of them
+ *   *free_head becomes h = *free_head - k, and free_slots[h .. h + k) are they, in the
+ *   (request, block) order of their last entries.  An error if k exceeds
+ *   *free_head, if a slot is freed more often than it is named, or if a kept
+ *   length ends inside a block that is shared (the next token would be written
+ *   into it).
+ *   shared   may be NULL for a pool without forks
+ * pulse_compact_blocks: live blocks in slots from n_keep on move to free slots
+ *   below it, so that the pool may be cut to n_keep slots: the k-th of them in
+ *   ascending order takes the k-th slot of the free list that is below n_keep.
+ *   Entries and counts follow; the free list keeps the other slots below n_keep,
+ *   in their order, at its end: free_slots[*free_head .. n_free).  Slots that
+ *   neither the table nor the list names stay as they are.
+ *   PULSE_ERR_POOL_EXHAUSTED if too few slots below n_keep are free; a slot twice
+ *   in the list, or in the list and the table, is an error.
+ *   shared   may be NULL for a pool without forks
+ */
+PULSE_API size_t pulse_pages_workspace_bytes(const pulse_shape* shape, int32_t B, int32_t max_blocks, int32_t n_slots);
+PULSE_API pulse_status pulse_fork_blocks(const pulse_shape* shape, const int32_t* src, const int32_t* dst,
+                                         const int32_t* fork_len, int32_t n, int32_t* block_table, int32_t B,
+                                         int32_t max_blocks, int32_t* shared, const int32_t* free_slots,
+                                         int32_t* free_head, int32_t n_free, void* slot_pool, int32_t n_slots,
+                                         int32_t* dev_status, void* ws, size_t ws_bytes, pulse_stream_t stream);
+PULSE_API pulse_status pulse_free_blocks(const pulse_shape* shape, const int32_t* keep_len, int32_t B,
+                                         int32_t* block_table, int32_t max_blocks, int32_t* shared, int32_t* free_slots,
+                                         int32_t* free_head, int32_t n_free, int32_t n_slots, int32_t* dev_status,
+                                         void* ws, size_t ws_bytes, pulse_stream_t stream);
+PULSE_API pulse_status pulse_compact_blocks(const pulse_shape* shape, int32_t* block_table, int32_t B,
+                                            int32_t max_blocks, int32_t n_keep, int32_t* shared, int32_t* free_slots,
+                                            int32_t* free_head, int32_t n_free, void* slot_pool, int32_t n_slots,
+                                            int32_t* dev_status, void* ws, size_t ws_bytes, pulse_stream_t stream);
+
 /* ---- Interruptible layer-wise scheduling (IRQ, Sec. 4.2) ---- */
 
 /*

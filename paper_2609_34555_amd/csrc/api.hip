@@ -595,6 +595,71 @@ pulse_status pulse_prompt_attn(const pulse_shape* shape, const void* q, int64_t 
                                          (hipStream_t)stream));
 }
 
+// Entries of a table and slots are numbered in 32 bits, with room for a workgroup's last stretch.
+static bool pages_fit(int32_t B, int32_t max_blocks, int32_t n_slots) {
+    return B <= kMaxBatch && (int64_t)B * max_blocks <= (1 << 30) && n_slots <= (1 << 30);
+}
+
+size_t pulse_pages_workspace_bytes(const pulse_shape* shape, int32_t B, int32_t max_blocks, int32_t n_slots) {
+    if (!kv_shape_supported(shape) || B < 0 || max_blocks < 1 || n_slots < 1 || !pages_fit(B, max_blocks, n_slots)) return 0;
+    return pages_ws_bytes(B, max_blocks, n_slots);
+}
+
+static pulse_status check_pages_args(const pulse_shape* shape, int32_t B, int32_t max_blocks, int32_t n_free,
+                                     int32_t n_slots) {
+    PULSE_REQUIRE(shape, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(kv_shape_supported(shape), PULSE_ERR_UNSUPPORTED);
+    PULSE_REQUIRE(B >= 0 && max_blocks >= 1 && n_free >= 0 && n_slots >= 1, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(pages_fit(B, max_blocks, n_slots), PULSE_ERR_UNSUPPORTED);
+    return PULSE_OK;
+}
+
+pulse_status pulse_fork_blocks(const pulse_shape* shape, const int32_t* src, const int32_t* dst, const int32_t* fork_len,
+                               int32_t n, int32_t* block_table, int32_t B, int32_t max_blocks, int32_t* shared,
+                               const int32_t* free_slots, int32_t* free_head, int32_t n_free, void* slot_pool,
+                               int32_t n_slots, int32_t* dev_status, void* ws, size_t ws_bytes, pulse_stream_t stream) {
+    const pulse_status st = check_pages_args(shape, B, max_blocks, n_free, n_slots);
+    if (st != PULSE_OK) return st;
+    PULSE_REQUIRE(n >= 0 && n <= B, PULSE_ERR_INVALID_ARG);
+    if (n == 0) return PULSE_OK;
+    PULSE_REQUIRE(src && dst && fork_len && block_table && shared && free_head && slot_pool && dev_status,
+                  PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(free_slots || n_free == 0, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(reinterpret_cast<uintptr_t>(slot_pool) % 16 == 0, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(ws && ws_bytes >= pages_ws_bytes(B, max_blocks, n_slots), PULSE_ERR_WORKSPACE);
+    return hip_status(launch_fork_blocks(src, dst, fork_len, n, shape->block_size, block_table, B, max_blocks, shared,
+                                         free_slots, free_head, n_free, slot_pool, n_slots, pulse_block_bytes(shape),
+                                         dev_status, ws, (hipStream_t)stream));
+}
+
+pulse_status pulse_free_blocks(const pulse_shape* shape, const int32_t* keep_len, int32_t B, int32_t* block_table,
+                               int32_t max_blocks, int32_t* shared, int32_t* free_slots, int32_t* free_head,
+                               int32_t n_free, int32_t n_slots, int32_t* dev_status, void* ws, size_t ws_bytes,
+                               pulse_stream_t stream) {
+    const pulse_status st = check_pages_args(shape, B, max_blocks, n_free, n_slots);
+    if (st != PULSE_OK || B == 0) return st;
+    PULSE_REQUIRE(keep_len && block_table && free_head && dev_status && (free_slots || n_free == 0), PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(ws && ws_bytes >= pages_ws_bytes(B, max_blocks, n_slots), PULSE_ERR_WORKSPACE);
+    return hip_status(launch_free_blocks(keep_len, B, shape->block_size, block_table, max_blocks, shared, free_slots,
+                                         free_head, n_free, n_slots, dev_status, ws, (hipStream_t)stream));
+}
+
+pulse_status pulse_compact_blocks(const pulse_shape* shape, int32_t* block_table, int32_t B, int32_t max_blocks,
+                                  int32_t n_keep, int32_t* shared, int32_t* free_slots, int32_t* free_head,
+                                  int32_t n_free, void* slot_pool, int32_t n_slots, int32_t* dev_status, void* ws,
+                                  size_t ws_bytes, pulse_stream_t stream) {
+    const pulse_status st = check_pages_args(shape, B, max_blocks, n_free, n_slots);
+    if (st != PULSE_OK) return st;
+    PULSE_REQUIRE(n_keep >= 0 && n_keep <= n_slots, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE((block_table || B == 0) && free_head && slot_pool && dev_status && (free_slots || n_free == 0),
+                  PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(reinterpret_cast<uintptr_t>(slot_pool) % 16 == 0, PULSE_ERR_INVALID_ARG);
+    PULSE_REQUIRE(ws && ws_bytes >= pages_ws_bytes(B, max_blocks, n_slots), PULSE_ERR_WORKSPACE);
+    return hip_status(launch_compact_blocks(block_table, B, max_blocks, n_keep, shared, free_slots, free_head, n_free,
+                                            slot_pool, n_slots, pulse_block_bytes(shape), dev_status, ws,
+                                            (hipStream_t)stream));
+}
+
 pulse_status pulse_probe_hbm_read(const void* src, size_t bytes, void* sink, void* start_event, void* stop_event,
                                   pulse_stream_t stream) {
     PULSE_REQUIRE(bytes % 16 == 0 && (src || bytes == 0) && sink, PULSE_ERR_INVALID_ARG);

@@ -334,6 +334,19 @@ hipError_t launch_prompt_attn(const pulse_shape& s, const void* q, int64_t q_str
                               const int32_t* table, int32_t max_blocks, float sm_scale, void* out, int64_t out_stride,
                               float* lse, int32_t* status, void* ws, hipStream_t st);
 
+// Forks, frees and compaction of the pool's blocks (pages.hip).
+size_t pages_ws_bytes(int32_t B, int32_t max_blocks, int32_t n_slots);
+hipError_t launch_free_blocks(const int32_t* keep, int32_t B, int32_t bs, int32_t* table, int32_t max_blocks, int32_t* shared,
+                              int32_t* free_slots, int32_t* free_head, int32_t n_free, int32_t n_slots, int32_t* status,
+                              void* ws, hipStream_t st);
+hipError_t launch_fork_blocks(const int32_t* src, const int32_t* dst, const int32_t* len, int32_t n, int32_t bs,
+                              int32_t* table, int32_t B, int32_t max_blocks, int32_t* shared, const int32_t* free_slots,
+                              int32_t* free_head, int32_t n_free, void* pool, int32_t n_slots, size_t unit_bytes,
+                              int32_t* status, void* ws, hipStream_t st);
+hipError_t launch_compact_blocks(int32_t* table, int32_t B, int32_t max_blocks, int32_t n_keep, int32_t* shared,
+                                 int32_t* free_slots, int32_t* free_head, int32_t n_free, void* pool, int32_t n_slots,
+                                 size_t unit_bytes, int32_t* status, void* ws, hipStream_t st);
+
 // Host-side argument check: return `code` from the calling entry point.
 #define PULSE_REQUIRE(cond, code)   \
     do {                            \

@@ -44,7 +44,8 @@ EXPORTED = (
     "pulse_mam", "pulse_pick_solo_heads", "pulse_irq_create", "pulse_irq_destroy", "pulse_irq_step",
     "pulse_probe_hbm_read", "pulse_probe_hbm_sink_bytes", "pulse_release_recalled", "pulse_attention_workgroups",
     "pulse_tables_workspace_bytes", "pulse_build_tables", "pulse_qk_norm_rope", "pulse_append_kv", "pulse_load_kv",
-    "pulse_prompt_workspace_bytes", "pulse_prompt_attn",
+    "pulse_prompt_workspace_bytes", "pulse_prompt_attn", "pulse_pages_workspace_bytes", "pulse_fork_blocks",
+    "pulse_free_blocks", "pulse_compact_blocks",
 )
 
 
@@ -200,6 +201,10 @@ def signatures():
         "pulse_prompt_workspace_bytes": (SZ, [SP, I32, I64, I32]),
         "pulse_prompt_attn": (ctypes.c_int, [SP, _P, I64, _P, I64, _P, I32, _P, I32, _P, I32, F, _P, I64, _P, _P, _P, SZ,
                                              _P]),
+        "pulse_pages_workspace_bytes": (SZ, [SP, I32, I32, I32]),
+        "pulse_fork_blocks": (ctypes.c_int, [SP, _P, _P, _P, I32, _P, I32, I32, _P, _P, _P, I32, _P, I32, _P, _P, SZ, _P]),
+        "pulse_free_blocks": (ctypes.c_int, [SP, _P, I32, _P, I32, _P, _P, _P, I32, I32, _P, _P, SZ, _P]),
+        "pulse_compact_blocks": (ctypes.c_int, [SP, _P, I32, I32, I32, _P, _P, _P, I32, _P, I32, _P, _P, SZ, _P]),
         "pulse_events_create": (ctypes.c_int, [I32, _P]),
         "pulse_events_destroy": (ctypes.c_int, [I32, _P]),
         "pulse_event_elapsed_ms": (ctypes.c_int, [_P, _P, ctypes.POINTER(ctypes.c_float)]),
@@ -364,6 +369,34 @@ def pulse_prompt_attn(shape, q, q_stride, tok_off, max_tokens, ctx_len, B, slot_
                                  _ptr(slot_pool), n_slots, _ptr(block_table), max_blocks, float(sm_scale), _ptr(out),
                                  out_stride, _ptr(lse), _ptr(dev_status), _ptr(ws), ws_bytes, _stream(stream))
     return _check(st, "pulse_prompt_attn", check)
+
+
+def pulse_pages_workspace_bytes(shape: pulse_shape, B: int, max_blocks: int, n_slots: int) -> int:
+    return lib().pulse_pages_workspace_bytes(ctypes.byref(shape), B, max_blocks, n_slots)
+
+
+def pulse_fork_blocks(shape, src, dst, fork_len, n, block_table, B, max_blocks, shared, free_slots, free_head, n_free,
+                      slot_pool, n_slots, dev_status, ws, ws_bytes, stream=None, check=True):
+    st = lib().pulse_fork_blocks(ctypes.byref(shape), _ptr(src), _ptr(dst), _ptr(fork_len), n, _ptr(block_table), B,
+                                 max_blocks, _ptr(shared), _ptr(free_slots), _ptr(free_head), n_free, _ptr(slot_pool),
+                                 n_slots, _ptr(dev_status), _ptr(ws), ws_bytes, _stream(stream))
+    return _check(st, "pulse_fork_blocks", check)
+
+
+def pulse_free_blocks(shape, keep_len, B, block_table, max_blocks, shared, free_slots, free_head, n_free, n_slots,
+                      dev_status, ws, ws_bytes, stream=None, check=True):
+    st = lib().pulse_free_blocks(ctypes.byref(shape), _ptr(keep_len), B, _ptr(block_table), max_blocks, _ptr(shared),
+                                 _ptr(free_slots), _ptr(free_head), n_free, n_slots, _ptr(dev_status), _ptr(ws), ws_bytes,
+                                 _stream(stream))
+    return _check(st, "pulse_free_blocks", check)
+
+
+def pulse_compact_blocks(shape, block_table, B, max_blocks, n_keep, shared, free_slots, free_head, n_free, slot_pool,
+                         n_slots, dev_status, ws, ws_bytes, stream=None, check=True):
+    st = lib().pulse_compact_blocks(ctypes.byref(shape), _ptr(block_table), B, max_blocks, n_keep, _ptr(shared),
+                                    _ptr(free_slots), _ptr(free_head), n_free, _ptr(slot_pool), n_slots,
+                                    _ptr(dev_status), _ptr(ws), ws_bytes, _stream(stream))
+    return _check(st, "pulse_compact_blocks", check)
 
 
 def pulse_pick_solo_heads(mam, check=True):
