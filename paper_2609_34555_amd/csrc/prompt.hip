@@ -16,6 +16,7 @@
 // rounded to the 16-bit type for the second product (half a step of it, at random, beside half a step of the output's own
 // rounding to the same type); their sum is that of the values before rounding.
 #include <algorithm>
+#include <type_traits>
 
 #include "kv4.h"
 #include "kv8.h"
@@ -58,7 +59,7 @@ template <int BS>
 __device__ inline int value_octet(int c, int o) {
     if constexpr (BS == 16) return o ^ ((c >> 2 ^ c >> 3) & 1);
     else if constexpr (BS == 32) return o ^ ((c >> 1 ^ (c >> 3 & 1)) & 3);
-    else return o ^ ((c ^ c >> 3) & 7);
+    else return o ^ ((c ^ (c >> 3 & 1)) & 7);  // (bits of c below 32 alone: lanes read channels 32 apart at one distance)
 }
 
 struct PromptArgs {
@@ -98,114 +99,139 @@ __device__ inline Place find_place(const int32_t* __restrict__ tok_off, int32_t 
     return Place{lo, at - (int)((int64_t)tok_off[lo] * G / rows + lo)};
 }
 
-// Tile `t` of the cache of KV head h into LDS, 16-bit blocks: 1 KiB a wave and instruction, straight from memory.
-template <int BS, int W>
-__device__ inline void stage16(const PromptArgs& a, const int (&slot)[kKeys / BS], int h, uint8_t* lds, int wave, int lane) {
-    const size_t E = (size_t)2 * a.Hkv * BS * kHeadDim * 2;
-    constexpr int kParts = kTileBytes / 1024;
-    constexpr int kBlockParts = kParts / (kKeys / BS);  // of a block's keys, and of its values
-#pragma unroll
-    for (int i = 0; i < kParts / W; ++i) {
-        const int part = i * W + wave, blk = part / kBlockParts, in = part % kBlockParts;
-        const int s = __builtin_amdgcn_readfirstlane(slot[blk]);
-        const uint8_t* k = a.pool + (size_t)s * E + (size_t)h * BS * kHeadDim * 2;
-        const uint8_t* v = k + (size_t)a.Hkv * BS * kHeadDim * 2;
-        const int key = in * 4 + (lane >> 4);  // within the block
-        const uint8_t* ks = k + key * 256 + key_piece(key % 32, lane & 15) * 16;
-        constexpr int kOct = BS / 8;
-        const int c = in * (64 / kOct) + lane / kOct;
-        const uint8_t* vs = v + (c * kOct + value_octet<BS>(c, lane % kOct)) * 16;
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)ks,
-                                         (__attribute__((address_space(3))) void*)(lds + part * 1024), 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)vs,
-                                         (__attribute__((address_space(3))) void*)(lds + kTileBytes + part * 1024), 16, 0, 0);
+// Slots of a tile's blocks.  (Four by name, of which the first kKeys / BS count: an array would not stay in registers.)
+struct Slots {
+    int s0, s1, s2, s3;
+    uint32_t bad;  // blocks without a slot
+    __device__ inline int operator[](int i) const {  // of a wave-uniform i
+        return i == 0 ? s0 : i == 1 ? s1 : i == 2 ? s2 : s3;
     }
-}
+};
 
-// The same tile of 8-bit or 4-bit blocks: fetch() loads codes and scales, a 16-byte piece at a time, into registers; put()
-// decodes them, exactly, into the 16-bit type and writes what stage16 would have written.  Decoding costs a workgroup
+// The 16 KiB of a tile's keys, or of its values, into LDS from 16-bit blocks: 1 KiB a wave and instruction, straight from
+// memory.  A lane's place within a block is the same for every tile.
+template <int BS, int W>
+struct Stage16 {
+    static constexpr int kParts = kTileBytes / 1024;
+    static constexpr int kBlockParts = kParts / (kKeys / BS);  // of a block
+    static constexpr int kPlaces = kBlockParts > W ? kBlockParts / W : 1;
+    uint32_t k_at[kPlaces], v_at[kPlaces];
+    uint32_t E;
+
+    __device__ inline Stage16(const PromptArgs& a, int h, int wave, int lane) {
+        E = (uint32_t)a.Hkv * BS * kHeadDim * 4;
+        constexpr int kOct = BS / 8;
+#pragma unroll
+        for (int i = 0; i < kPlaces; ++i) {
+            const int in = (i * W + wave) % kBlockParts;
+            const int key = in * 4 + (lane >> 4);
+            k_at[i] = (uint32_t)h * BS * kHeadDim * 2 + key * 256 + key_piece(key % 32, lane & 15) * 16;
+            const int c = in * (64 / kOct) + lane / kOct;
+            v_at[i] = (uint32_t)(a.Hkv + h) * BS * kHeadDim * 2 + (c * kOct + value_octet<BS>(c, lane % kOct)) * 16;
+        }
+    }
+    template <bool K>
+    __device__ inline void tile(const PromptArgs& a, const Slots& slot, uint8_t* lds, int wave) const {
+#pragma unroll
+        for (int i = 0; i < kParts / W; ++i) {
+            const int part = i * W + wave;
+            const int s = slot[part / kBlockParts];
+            const uint8_t* src = a.pool + (uint64_t)(uint32_t)s * E;
+            __builtin_amdgcn_global_load_lds(
+                (const __attribute__((address_space(1))) void*)(src + (K ? k_at : v_at)[i % kPlaces]),
+                (__attribute__((address_space(3))) void*)(lds + part * 1024), 16, 0, 0);
+        }
+    }
+};
+
+// The same from 8-bit or 4-bit blocks: fetch() loads codes and scales, a 16-byte piece at a time, into registers; put()
+// decodes them, exactly, into the 16-bit type and writes what Stage16 would have written.  Decoding costs a workgroup
 // once what W waves then use.
 template <int DT, int BS, int W>
-struct Codes {
+struct StageCodes {
     static constexpr int ET = elem_type(DT);
     static constexpr int kThreads = W * kWave;
     static constexpr bool k4 = is_kv4(DT);
-    static constexpr int kUnits = kKeys * kHeadDim / (k4 ? 32 : 16);  // pieces of keys, and of values
+    static constexpr int kUnits = kKeys * kHeadDim / (k4 ? 32 : 16);  // pieces of a tile
     static constexpr int kEach = (kUnits + kThreads - 1) / kThreads;
     static constexpr int kPer = k4 ? 4 : 8;  // pieces of a key
     u32x4 k[kEach], v[kEach];
-    uint32_t ks[kEach];  // 8 bits: exponent byte of the piece's block (keys low, values high, of their blocks); 4: its scale
-    u32x2 vs[kEach][2];  // 4 bits: scale bytes of 8 tokens, of the piece's two channel groups
+    uint32_t ks[kEach], vs[kEach];  // scale byte of a piece's keys, and (8 bits) values
+    u32x2 vs4[kEach][2];            // 4 bits: scale bytes of 8 tokens, of the piece's two channel groups
+    const uint8_t* head;
+    uint64_t U;
 
-    // Piece u of keys: key u / kPer, of values: octet u / (kUnits / 8).  A wave's pieces lie in one block.
-    __device__ inline void fetch(const PromptArgs& a, const int (&slot)[kKeys / BS], int h, int tid) {
-        const size_t U = k4 ? (size_t)a.Hkv * kv4_head_bytes(BS) : (size_t)kv8_block_bytes(a.Hkv, BS);
+    __device__ inline StageCodes(const PromptArgs& a, int h, int, int) {
+        U = k4 ? (uint64_t)a.Hkv * kv4_head_bytes(BS) : (uint64_t)kv8_block_bytes(a.Hkv, BS);
+        head = a.pool + (size_t)h * (k4 ? kv4_head_bytes(BS) : kv8_head_bytes(BS));
+    }
+
+    // Piece u of keys: of key u / kPer; of values: of octet u / (kUnits / 8).  A wave's pieces lie in one block.
+    template <bool K>
+    __device__ inline void fetch(const PromptArgs& a, const Slots& slot, int h, int tid) {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const int u = i * kThreads + tid;
             if (kUnits % kThreads && u >= kUnits) break;
             const int key = u / kPer, oct = u / (kUnits / 8);
-            const uint8_t* kb = a.pool + (size_t)__builtin_amdgcn_readfirstlane(slot[key / BS]) * U;
-            const uint8_t* vb = a.pool + (size_t)__builtin_amdgcn_readfirstlane(slot[oct * 8 / BS]) * U;
-            if constexpr (k4) {
-                kb += (size_t)h * kv4_head_bytes(BS);
-                vb += (size_t)h * kv4_head_bytes(BS);
-                k[i] = *reinterpret_cast<const u32x4*>(kb + key % BS * 64 + u % 4 * 16);
-                ks[i] = kb[kv4_key_scales(BS) + key % BS * kGroups + u % 4];
-                const int at = u % 32;  // channels at / 2 + 16 * (4 * (at % 2) + 0 .. 3)
-                v[i] = *reinterpret_cast<const u32x4*>(vb + kv4_values(BS) + oct % (BS / 8) * 512 + at * 16);
+            const uint64_t at = (uint64_t)(uint32_t)slot[__builtin_amdgcn_readfirstlane((K ? key : oct * 8) / BS)] * U;
+            const uint8_t* b = head + at;
+            if constexpr (k4 && K) {
+                k[i] = *reinterpret_cast<const u32x4*>(b + key % BS * 64 + u % 4 * 16);
+                ks[i] = b[kv4_key_scales(BS) + key % BS * kv4_scales_per_token() + u % 4];
+            } else if constexpr (k4) {
+                const int p = u % 32;  // channels p / 2 + 16 * (4 * (p % 2) + 0 .. 3)
+                v[i] = *reinterpret_cast<const u32x4*>(b + kv4_values(BS) + oct % (BS / 8) * 512 + p * 16);
 #pragma unroll
                 for (int n = 0; n < 2; ++n)
-                    vs[i][n] = *reinterpret_cast<const u32x2*>(vb + kv4_value_scales(BS) + (2 * (at % 2) + n) * BS +
-                                                               oct % (BS / 8) * 8);
+                    vs4[i][n] = *reinterpret_cast<const u32x2*>(b + kv4_value_scales(BS) + (2 * (p % 2) + n) * BS +
+                                                                oct % (BS / 8) * 8);
             } else {
-                const size_t head = (size_t)h * kv8_head_bytes(BS), scale = (size_t)kv8_scales(a.Hkv, BS) + 2 * h;
-                k[i] = *reinterpret_cast<const u32x4*>(kb + head + key % BS * kHeadDim + u % 8 * 16);
-                const int at = u % 64;  // channels at / 4 + 16 * (2 * (at % 4) + 0 .. 1)
-                v[i] = *reinterpret_cast<const u32x4*>(vb + head + kv8_values(BS) + oct % (BS / 8) * 1024 + at * 16);
-                ks[i] = kb[scale] | (uint32_t)vb[scale + 1] << 8;
+                const uint8_t scale = a.pool[at + kv8_scales(a.Hkv, BS) + 2 * h + (K ? 0 : 1)];
+                if constexpr (K) {
+                    k[i] = *reinterpret_cast<const u32x4*>(b + key % BS * kHeadDim + u % 8 * 16);
+                    ks[i] = scale;
+                } else {  // channels u % 64 / 4 + 16 * (2 * (u % 4) + 0 .. 1)
+                    v[i] = *reinterpret_cast<const u32x4*>(b + kv8_values(BS) + oct % (BS / 8) * 1024 + u % 64 * 16);
+                    vs[i] = scale;
+                }
             }
         }
     }
 
+    template <bool K>
     __device__ inline void put(uint8_t* lds, int tid) const {
-        uint8_t* vals = lds + kTileBytes;
         constexpr int kOct = BS / 8;
-        auto value_at = [&](int oct, int c) {
-            return reinterpret_cast<u32x4*>(vals + oct / kOct * (256 * BS) + (c * kOct + value_octet<BS>(c, oct % kOct)) * 16);
-        };
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const int u = i * kThreads + tid;
             if (kUnits % kThreads && u >= kUnits) break;
             const int key = u / kPer, oct = u / (kUnits / 8);
-            if constexpr (k4) {
-                const int at = u % 32;
-                const float scale = kv4_scale(ks[i]);
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    *reinterpret_cast<u32x4*>(lds + key * 256 + key_piece(key % 32, 4 * (u % 4) + n) * 16) =
-                        __builtin_bit_cast(u32x4, kv4_decode8<ET>(k[i][n], scale));
-                    // 8 tokens, a scale each
-                    const u32x2 sb = vs[i][n / 2];
-                    u32x4 w;
+            for (int n = 0; n < 32 / kPer / 2; ++n) {
+                u32x4 w;
+                if constexpr (K) {
+                    if constexpr (k4) w = __builtin_bit_cast(u32x4, kv4_decode8<ET>(k[i][n], kv4_scale(ks[i])));
+                    else w = __builtin_bit_cast(u32x4, kv8_decode8<ET>(u32x2{k[i][2 * n], k[i][2 * n + 1]},
+                                                                       kv8_pow2((int)ks[i] - 127)));
+                    *reinterpret_cast<u32x4*>(lds + key * 256 + key_piece(key % 32, u % kPer * (16 / kPer) + n) * 16) = w;
+                } else {
+                    int c;
+                    if constexpr (k4) {
+                        c = u % 32 / 2 + 16 * (4 * (u % 2) + n);
+                        const u32x2 sb = vs4[i][n / 2];  // a scale for each of the 8 tokens
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        const float s0 = kv4_scale(sb[t / 2] >> (16 * (t % 2)) & 255u);
-                        const float s1 = kv4_scale(sb[t / 2] >> (16 * (t % 2) + 8) & 255u);
-                        w[t] = (decode_pair(v[i][n], t, s0) & 0xFFFFu) | (decode_pair(v[i][n], t, s1) & 0xFFFF0000u);
+                        for (int t = 0; t < 4; ++t) {
+                            const float s0 = kv4_scale(sb[t / 2] >> (16 * (t % 2)) & 255u);
+                            const float s1 = kv4_scale(sb[t / 2] >> (16 * (t % 2) + 8) & 255u);
+                            w[t] = (decode_pair(v[i][n], t, s0) & 0xFFFFu) | (decode_pair(v[i][n], t, s1) & 0xFFFF0000u);
+                        }
+                    } else {
+                        c = u % 64 / 4 + 16 * (2 * (u % 4) + n);
+                        w = __builtin_bit_cast(u32x4, kv8_decode8<ET>(u32x2{v[i][2 * n], v[i][2 * n + 1]},
+                                                                      kv8_pow2((int)vs[i] - 127)));
                     }
-                    *value_at(oct, at / 2 + 16 * (4 * (at % 2) + n)) = w;
-                }
-            } else {
-                const int at = u % 64;
-                const float kf = kv8_pow2((int)(ks[i] & 255) - 127), vf = kv8_pow2((int)(ks[i] >> 8) - 127);
-#pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    *reinterpret_cast<u32x4*>(lds + key * 256 + key_piece(key % 32, 2 * (u % 8) + n) * 16) =
-                        __builtin_bit_cast(u32x4, kv8_decode8<ET>(u32x2{k[i][2 * n], k[i][2 * n + 1]}, kf));
-                    *value_at(oct, at / 4 + 16 * (2 * (at % 4) + n)) =
-                        __builtin_bit_cast(u32x4, kv8_decode8<ET>(u32x2{v[i][2 * n], v[i][2 * n + 1]}, vf));
+                    *reinterpret_cast<u32x4*>(lds + oct / kOct * (256 * BS) + (c * kOct + value_octet<BS>(c, oct % kOct)) * 16) = w;
                 }
             }
         }
@@ -216,6 +242,7 @@ struct Codes {
         return t == 0 ? kv4_decode<ET, 0>(w, scale) : t == 1 ? kv4_decode<ET, 1>(w, scale)
              : t == 2 ? kv4_decode<ET, 2>(w, scale) : kv4_decode<ET, 3>(w, scale);
     }
+    __device__ static constexpr int kv4_scales_per_token() { return kHeadDim / kGroup; }
 };
 
 // This wave's pieces are in LDS, and so are the others', which are done with the other tile.
@@ -232,7 +259,7 @@ __global__ __launch_bounds__(W * kWave, 2) void prompt_kernel(PromptArgs a) {
     using vec = typename Mfma<ET>::vec;
     constexpr int kRows = W * kRowsPerWave;
     constexpr int kBlocks = kKeys / BS;
-    __shared__ __align__(1024) uint8_t s_tile[2][2 * kTileBytes];
+    __shared__ __align__(1024) uint8_t s_keys[2][kTileBytes], s_vals[2][kTileBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, half = lane >> 5;
     const int h = blockIdx.x % a.Hkv;
@@ -286,52 +313,161 @@ __global__ __launch_bounds__(W * kWave, 2) void prompt_kernel(PromptArgs a) {
     f32x16 acc[4] = {};
     float m_run = -INFINITY, l_run = 0.f;
 
-    // slots of a tile's blocks, read one tile ahead; a block without one is looked at as slot 0 and counts nothing
+    // Slots of a tile's blocks, looked up ahead; a block without one is looked at as slot 0 and counts nothing.
     const auto* row = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(a.table + (size_t)pl.r * a.max_blocks);
     const int n_blk = ok ? (ctx + BS - 1) / BS : 0;
-    int next[kBlocks];
     auto look_up = [&](int kt) {
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b) next[b] = row[min(kt * kBlocks + b, n_blk - 1)];
+        const int j = kt * kBlocks, last = n_blk - 1;
+        Slots x = {};
+        if (j + kBlocks <= n_blk) {
+            x.s0 = row[j];
+            if (kBlocks > 1) x.s1 = row[j + 1];
+            if (kBlocks > 2) x.s2 = row[j + 2], x.s3 = row[j + 3];
+        } else {
+            x.s0 = row[min(j, last)];
+            if (kBlocks > 1) x.s1 = row[min(j + 1, last)];
+            if (kBlocks > 2) x.s2 = row[min(j + 2, last)], x.s3 = row[min(j + 3, last)];
+        }
+        return x;
     };
-    Codes<DT, BS, W> codes;
-    uint32_t bad = 0;  // blocks without a slot of the tile staged last
-    auto stage = [&](int kt, int buf) {
-        bad = 0;
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
-            if ((uint32_t)next[b] >= (uint32_t)a.n_slots) {
-                bad |= 1u << b;
-                next[b] = 0;
+    auto checked = [&](Slots x) {
+        auto one = [&](int& s, uint32_t bit) {
+            if ((uint32_t)s >= (uint32_t)a.n_slots) {
+                x.bad |= bit;
+                s = 0;
             }
-        if constexpr (kv_bits(DT) == 16) stage16<BS, W>(a, next, h, s_tile[buf], wave, lane);
-        else codes.fetch(a, next, h, threadIdx.x);
-        if (bad && threadIdx.x == 0) report(a.status, PULSE_ERR_BAD_INDEX);
-        if (kt + 1 < kt1) look_up(kt + 1);
+        };
+        x.bad = 0;
+        one(x.s0, 1);
+        if (kBlocks > 1) one(x.s1, 2);
+        if (kBlocks > 2) one(x.s2, 4), one(x.s3, 8);
+        if (x.bad && threadIdx.x == 0) report(a.status, PULSE_ERR_BAD_INDEX);
+        return x;
     };
-    uint32_t bad_now = 0;
+    constexpr bool kCodes = kv_bits(DT) != 16;
+    std::conditional_t<kCodes, StageCodes<DT, BS, W>, Stage16<BS, W>> stage(a, h, wave, lane);
+    auto load_keys = [&](const Slots& x, int buf) {
+        if constexpr (kCodes) stage.template fetch<true>(a, x, h, threadIdx.x);
+        else stage.template tile<true>(a, x, s_keys[buf], wave);
+    };
+    auto load_vals = [&](const Slots& x, int buf) {
+        if constexpr (kCodes) stage.template fetch<false>(a, x, h, threadIdx.x);
+        else stage.template tile<false>(a, x, s_vals[buf], wave);
+    };
+
+    // Operands of four products from LDS: keys, a quarter of a tile (32 keys, 64 channels); values, 16 keys.
+    const uint32_t k_lds = key_of_row(col) * 256 + key_piece(key_of_row(col), half) * 16;
+    auto read_keys = [&](const uint8_t* keys, int q, u32x4 (&f)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            f[i] = *reinterpret_cast<const u32x4*>(keys + q / 2 * (32 * 256) + (k_lds ^ (q % 2 * 4 + i) * 32));
+    };
+    auto read_vals = [&](const uint8_t* vals, int st, u32x4 (&f)[4]) {
+        const int oct = 2 * st + half, blk = oct / (BS / 8), o = oct % (BS / 8);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            f[i] = *reinterpret_cast<const u32x4*>(vals + blk * (256 * BS) +
+                                                   ((32 * i + col) * (BS / 8) + value_octet<BS>(col, o)) * 16);
+    };
+    auto logits = [&](int q, const u32x4 (&f)[4], f32x16& s) {
+        if (q % 2 == 0) s = f32x16{};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s = mac32<ET>(__builtin_bit_cast(vec, f[i]), qb[q % 2 * 4 + i], s);
+    };
+    auto accumulate = [&](const u32x4 (&f)[4], vec pv) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = mac32<ET>(__builtin_bit_cast(vec, f[i]), pv, acc[i]);
+    };
+    // Probabilities of 16 keys, as an operand.
+    float m_use = 0.f;
+    auto probs = [&](const f32x16& s, int st) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[i] = __builtin_amdgcn_exp2f(fmaf(s[st % 2 * 8 + i], scale, -m_use));
+            l_run += x[i];
+        }
+        return __builtin_bit_cast(vec, u32x4{pack2<ET>(x[0], x[1]), pack2<ET>(x[2], x[3]), pack2<ET>(x[4], x[5]),
+                                             pack2<ET>(x[6], x[7])});
+    };
+    // One tile's probabilities and values, and the next one's logits, which take the registers of the logits before them:
+    // groups of four products, each beside the reads of the next group's operands and a part of the exponentials.
+    auto step = [&](auto has_next, f32x16 (&s)[2], const uint8_t* keys, const uint8_t* vals) {
+        constexpr bool kNext = decltype(has_next)::value;
+        u32x4 f[2][4];
+        if constexpr (kNext) read_keys(keys, 0, f[0]);
+        else read_vals(vals, 0, f[0]);
+        vec pv[4];
+        pv[0] = probs(s[0], 0);
+        pv[1] = probs(s[0], 1);
+        if constexpr (kNext) {
+            read_keys(keys, 1, f[1]);
+            logits(0, f[0], s[0]);
+            pv[2] = probs(s[1], 2);
+            read_vals(vals, 0, f[0]);
+            logits(1, f[1], s[0]);
+            pv[3] = probs(s[1], 3);
+        } else {
+            pv[2] = probs(s[1], 2);
+            pv[3] = probs(s[1], 3);
+        }
+        read_vals(vals, 1, f[1]);
+        accumulate(f[0], pv[0]);
+        if constexpr (kNext) read_keys(keys, 2, f[0]);
+        else read_vals(vals, 2, f[0]);
+        accumulate(f[1], pv[1]);
+        if constexpr (kNext) {
+            read_keys(keys, 3, f[1]);
+            logits(2, f[0], s[1]);
+            read_vals(vals, 2, f[0]);
+            logits(3, f[1], s[1]);
+        }
+        read_vals(vals, 3, f[1]);
+        accumulate(f[0], pv[2]);
+        accumulate(f[1], pv[3]);
+    };
+
+    // The keys of a tile are in LDS one tile earlier than its values.
+    Slots now, next, ahead;  // tiles kt, kt + 1, kt + 2
+    f32x16 s[2];
+    now.bad = next.bad = 0;
     if (kt0 < kt1) {
-        look_up(kt0);
-        stage(kt0, 0);
-        bad_now = bad;
-        if constexpr (kv_bits(DT) != 16) codes.put(s_tile[0], threadIdx.x);
+        now = checked(look_up(kt0));
+        load_keys(now, 0);
+        load_vals(now, 0);
+        if constexpr (kCodes) {
+            stage.template put<true>(s_keys[0], threadIdx.x);
+            stage.template put<false>(s_vals[0], threadIdx.x);
+        }
+        if (kt0 + 1 < kt1) {
+            next = checked(look_up(kt0 + 1));
+            load_keys(next, 1);
+            if constexpr (kCodes) stage.template put<true>(s_keys[1], threadIdx.x);
+        }
+        if (kt0 + 2 < kt1) ahead = look_up(kt0 + 2);
+        tile_arrived();
+        if (kt0 * kKeys < wave_keys) {
+            u32x4 f[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                read_keys(s_keys[0], q, f);
+                logits(q, f, s[q / 2]);
+            }
+        }
+        __syncthreads();
     }
-    tile_arrived();
-    int buf = 0;
-#pragma unroll 1
-    for (int kt = kt0; kt < kt1; ++kt, buf ^= 1) {
-        if (kt + 1 < kt1) stage(kt + 1, buf ^ 1);
+    // What a tile needs before its step: values behind the context taken out, logits masked, maxima looked at.  False where
+    // the wave has no row that attends to it.
+    auto prepare = [&](int kt, uint8_t* vals) {
         const int k0 = kt * kKeys;
-        uint8_t* ks = s_tile[buf];
-        uint8_t* vs = s_tile[buf] + kTileBytes;
-        if (k0 + kKeys > ctx || bad_now) {
+        if (k0 + kKeys > ctx || now.bad) {
             // behind a context's end lies what an earlier owner of the slot left, NaN perhaps, which a probability of 0
             // would not take out of the product; and a block without a slot was read from another's
             for (int i = threadIdx.x; i < kTileBytes / 16; i += W * kWave) {
                 constexpr int kOct = BS / 8;
                 const int c = i / kOct % kHeadDim, o = i % kOct, blk = i / (kOct * kHeadDim);
-                const int end = bad_now >> blk & 1 ? 0 : ctx - k0 - blk * BS - 8 * value_octet<BS>(c, o);
-                u32x4* at = reinterpret_cast<u32x4*>(vs) + i;
+                const int end = now.bad >> blk & 1 ? 0 : ctx - k0 - blk * BS - 8 * value_octet<BS>(c, o);
+                u32x4* at = reinterpret_cast<u32x4*>(vals) + i;
                 if (end < 8) {
                     u32x4 v = *at;
 #pragma unroll
@@ -342,76 +478,60 @@ __global__ __launch_bounds__(W * kWave, 2) void prompt_kernel(PromptArgs a) {
             }
             __syncthreads();
         }
-        if (k0 < wave_keys) {
-            f32x16 s[2] = {};
-            const int key = key_of_row(col);
+        if (k0 >= wave_keys) return false;
+        if (k0 + kKeys > wave_all) {
+            const int left = p + 1 - k0 - 8 * half;  // keys of this half's numbering that the row attends to
 #pragma unroll
-            for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    const vec kv = __builtin_bit_cast(vec, *reinterpret_cast<const u32x4*>(
-                                                               ks + (32 * sub + key) * 256 + key_piece(key, 2 * c + half) * 16));
-                    s[sub] = mac32<ET>(kv, qb[c], s[sub]);
-                }
-            float x[32];
-#pragma unroll
-            for (int i = 0; i < 32; ++i) x[i] = s[i / 16][i % 16];
-            if (k0 + kKeys > wave_all) {
-                const int left = p + 1 - k0 - 8 * half;  // keys of this half's numbering that the row attends to
-#pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (32 * (i / 16) + 16 * (i % 16 / 8) + i % 8 >= left) x[i] = -INFINITY;
-            }
-            if (bad_now) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    const int k = 32 * (i / 16) + 16 * (i % 16 / 8) + i % 8 + 8 * half;
-                    if (bad_now >> (k / BS) & 1) x[i] = -INFINITY;
-                }
-            }
-            float cm = x[0];
-#pragma unroll
-            for (int i = 1; i < 32; ++i) cm = __builtin_elementwise_maximum(cm, x[i]);
-            {
-                const uint32_t u = __float_as_uint(cm);
-                const u32x2 w = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-                cm = __builtin_elementwise_maximum(__uint_as_float(w[0]), __uint_as_float(w[1]));
-            }
-            const float m_new = __builtin_elementwise_maximum(m_run, cm * scale);
-            const float m_use = m_new == -INFINITY ? 0.f : m_new;
-            const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
-            m_run = m_new;
-            float psum = 0.f;
+            for (int i = 0; i < 32; ++i)
+                if (32 * (i / 16) + 16 * (i % 16 / 8) + i % 8 >= left) s[i / 16][i % 16] = -INFINITY;
+        }
+        if (now.bad) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
-                x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], scale, -m_use));
-                psum += x[i];
-            }
-            l_run = l_run * alpha + psum;
-            if (__ballot(alpha != 1.f)) {
-#pragma unroll
-                for (int t = 0; t < 4; ++t) acc[t] *= alpha;
-            }
-#pragma unroll
-            for (int st = 0; st < 4; ++st) {
-                const u32x4 pw = {pack2<ET>(x[8 * st], x[8 * st + 1]), pack2<ET>(x[8 * st + 2], x[8 * st + 3]),
-                                  pack2<ET>(x[8 * st + 4], x[8 * st + 5]), pack2<ET>(x[8 * st + 6], x[8 * st + 7])};
-                const vec pv = __builtin_bit_cast(vec, pw);
-                const int oct = 2 * st + half, blk = oct / (BS / 8), o = oct % (BS / 8);
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int c = 32 * t + col;
-                    const u32x4 v = *reinterpret_cast<const u32x4*>(vs + blk * (256 * BS) +
-                                                                    (c * (BS / 8) + value_octet<BS>(c, o)) * 16);
-                    acc[t] = mac32<ET>(__builtin_bit_cast(vec, v), pv, acc[t]);
-                }
+                const int k = 32 * (i / 16) + 16 * (i % 16 / 8) + i % 8 + 8 * half;
+                if (now.bad >> (k / BS) & 1) s[i / 16][i % 16] = -INFINITY;
             }
         }
-        bad_now = bad;
-        if constexpr (kv_bits(DT) != 16)
-            if (kt + 1 < kt1) codes.put(s_tile[buf ^ 1], threadIdx.x);
+        float cm = s[0][0];
+#pragma unroll
+        for (int i = 1; i < 32; ++i) cm = __builtin_elementwise_maximum(cm, s[i / 16][i % 16]);
+        {
+            const uint32_t u = __float_as_uint(cm);
+            const u32x2 w = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+            cm = __builtin_elementwise_maximum(__uint_as_float(w[0]), __uint_as_float(w[1])) * scale;
+        }
+        // The maximum that is subtracted follows the rows' own only when one of the wave's has left it 2^8 behind:
+        // until then probabilities and sums grow by up to that factor and keep their relative accuracy.
+        if (__ballot(!(cm <= m_run + 8.f))) {
+            const float m_new = __builtin_elementwise_maximum(m_run, cm);
+            const float alpha = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
+            m_run = m_new;
+            l_run *= alpha;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) acc[t] *= alpha;
+        }
+        m_use = m_run == -INFINITY ? 0.f : m_run;
+        return true;
+    };
+    int buf = 0;
+#pragma unroll 1
+    for (int kt = kt0; kt + 1 < kt1; ++kt, buf ^= 1) {
+        load_vals(next, buf ^ 1);
+        if (kt + 2 < kt1) {
+            ahead = checked(ahead);
+            load_keys(ahead, buf);
+        }
+        if (prepare(kt, s_vals[buf])) step(std::true_type(), s, s_keys[buf ^ 1], s_vals[buf]);
+        if constexpr (kCodes) {
+            stage.template put<false>(s_vals[buf ^ 1], threadIdx.x);
+            if (kt + 2 < kt1) stage.template put<true>(s_keys[buf], threadIdx.x);
+        }
+        now = next;
+        next = ahead;
+        if (kt + 3 < kt1) ahead = look_up(kt + 3);
         tile_arrived();
     }
+    if (kt0 < kt1 && prepare(kt1 - 1, s_vals[buf])) step(std::false_type(), s, nullptr, s_vals[buf]);
     {
         const uint32_t u = __float_as_uint(l_run);
         const u32x2 w = __builtin_amdgcn_permlane32_swap(u, u, false, false);
