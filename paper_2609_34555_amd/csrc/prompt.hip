@@ -135,7 +135,8 @@ struct Stage16 {
 #pragma unroll
         for (int i = 0; i < kParts / W; ++i) {
             const int part = i * W + wave;
-            const int s = slot[part / kBlockParts];
+            // (of W waves that share a block the index is a constant)
+            const int s = slot[kBlockParts >= W ? i * W / kBlockParts : part / kBlockParts];
             const uint8_t* src = a.pool + (uint64_t)(uint32_t)s * E;
             __builtin_amdgcn_global_load_lds(
                 (const __attribute__((address_space(1))) void*)(src + (K ? k_at : v_at)[i % kPlaces]),
@@ -316,32 +317,39 @@ __global__ __launch_bounds__(W * kWave, 2) void prompt_kernel(PromptArgs a) {
     // Slots of a tile's blocks, looked up ahead; a block without one is looked at as slot 0 and counts nothing.
     const auto* row = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(a.table + (size_t)pl.r * a.max_blocks);
     const int n_blk = ok ? (ctx + BS - 1) / BS : 0;
+    typedef __attribute__((ext_vector_type(kBlocks == 1 ? 2 : kBlocks), aligned(4))) int32_t Row;
     auto look_up = [&](int kt) {
         const int j = kt * kBlocks, last = n_blk - 1;
         Slots x = {};
-        if (j + kBlocks <= n_blk) {
-            x.s0 = row[j];
-            if (kBlocks > 1) x.s1 = row[j + 1];
-            if (kBlocks > 2) x.s2 = row[j + 2], x.s3 = row[j + 3];
-        } else {
+        if (kBlocks == 1) {
             x.s0 = row[min(j, last)];
-            if (kBlocks > 1) x.s1 = row[min(j + 1, last)];
+        } else if (j + kBlocks <= n_blk) {
+            const Row y = *(const __attribute__((address_space(4))) Row*)(row + j);
+            x.s0 = y[0], x.s1 = y[1];
+            if constexpr (kBlocks > 2) x.s2 = y[2], x.s3 = y[3];
+        } else {
+            x.s0 = row[min(j, last)], x.s1 = row[min(j + 1, last)];
             if (kBlocks > 2) x.s2 = row[min(j + 2, last)], x.s3 = row[min(j + 3, last)];
         }
         return x;
     };
     auto checked = [&](Slots x) {
-        auto one = [&](int& s, uint32_t bit) {
-            if ((uint32_t)s >= (uint32_t)a.n_slots) {
-                x.bad |= bit;
-                s = 0;
-            }
-        };
         x.bad = 0;
-        one(x.s0, 1);
-        if (kBlocks > 1) one(x.s1, 2);
-        if (kBlocks > 2) one(x.s2, 4), one(x.s3, 8);
-        if (x.bad && threadIdx.x == 0) report(a.status, PULSE_ERR_BAD_INDEX);
+        const uint32_t n = (uint32_t)a.n_slots;
+        uint32_t top = max((uint32_t)x.s0, (uint32_t)x.s1);
+        if (kBlocks > 2) top = max(top, max((uint32_t)x.s2, (uint32_t)x.s3));
+        if (top >= n) {
+            auto one = [&](int& s, uint32_t bit) {
+                if ((uint32_t)s >= n) {
+                    x.bad |= bit;
+                    s = 0;
+                }
+            };
+            one(x.s0, 1);
+            if (kBlocks > 1) one(x.s1, 2);
+            if (kBlocks > 2) one(x.s2, 4), one(x.s3, 8);
+            if (threadIdx.x == 0) report(a.status, PULSE_ERR_BAD_INDEX);
+        }
         return x;
     };
     constexpr bool kCodes = kv_bits(DT) != 16;
@@ -380,12 +388,13 @@ __global__ __launch_bounds__(W * kWave, 2) void prompt_kernel(PromptArgs a) {
     };
     // Probabilities of 16 keys, as an operand.
     float m_use = 0.f;
+    float sum = 0.f;  // of a tile
     auto probs = [&](const f32x16& s, int st) {
         float x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             x[i] = __builtin_amdgcn_exp2f(fmaf(s[st % 2 * 8 + i], scale, -m_use));
-            l_run += x[i];
+            sum += x[i];
         }
         return __builtin_bit_cast(vec, u32x4{pack2<ET>(x[0], x[1]), pack2<ET>(x[2], x[3]), pack2<ET>(x[4], x[5]),
                                              pack2<ET>(x[6], x[7])});
@@ -394,6 +403,7 @@ __global__ __launch_bounds__(W * kWave, 2) void prompt_kernel(PromptArgs a) {
     // groups of four products, each beside the reads of the next group's operands and a part of the exponentials.
     auto step = [&](auto has_next, f32x16 (&s)[2], const uint8_t* keys, const uint8_t* vals) {
         constexpr bool kNext = decltype(has_next)::value;
+        sum = 0.f;
         u32x4 f[2][4];
         if constexpr (kNext) read_keys(keys, 0, f[0]);
         else read_vals(vals, 0, f[0]);
@@ -425,6 +435,7 @@ __global__ __launch_bounds__(W * kWave, 2) void prompt_kernel(PromptArgs a) {
         read_vals(vals, 3, f[1]);
         accumulate(f[0], pv[2]);
         accumulate(f[1], pv[3]);
+        l_run += sum;
     };
 
     // The keys of a tile are in LDS one tile earlier than its values.
