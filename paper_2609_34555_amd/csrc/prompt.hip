@@ -27,7 +27,7 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 constexpr int kKeys = 64;                     // keys of a tile
 constexpr int kRowsPerWave = 32;
-constexpr int kWaves = 4;                     // of a workgroup
+constexpr int kWaves = 4;                     // of a workgroup; twice as many for long prompts
 constexpr int kTileBytes = kKeys * kHeadDim * 2;  // of keys, and of values, in LDS
 
 template <int ET>
@@ -60,6 +60,13 @@ __device__ inline int value_octet(int c, int o) {
     if constexpr (BS == 16) return o ^ ((c >> 2 ^ c >> 3) & 1);
     else if constexpr (BS == 32) return o ^ ((c >> 1 ^ (c >> 3 & 1)) & 3);
     else return o ^ ((c ^ (c >> 3 & 1)) & 7);  // (bits of c below 32 alone: lanes read channels 32 apart at one distance)
+}
+
+// Codes of byte t of w times `scale`, as two 16-bit values.
+template <int ET>
+__device__ inline uint32_t kv4_pair(uint32_t w, int t, float scale) {
+    return t == 0 ? kv4_decode<ET, 0>(w, scale) : t == 1 ? kv4_decode<ET, 1>(w, scale)
+         : t == 2 ? kv4_decode<ET, 2>(w, scale) : kv4_decode<ET, 3>(w, scale);
 }
 
 struct PromptArgs {
@@ -107,6 +114,33 @@ struct Slots {
         return i == 0 ? s0 : i == 1 ? s1 : i == 2 ? s2 : s3;
     }
 };
+
+// What a workgroup of `rows` rows has to know of its request.  Workgroup 0 looks at every request's lengths.
+struct Request {
+    bool any, ok;  // whether it has a row; whether its lengths are right (else no token is attended to)
+    int t0, ctx, base;  // its first row, its tokens, the tokens before its first new one
+    int64_t n_rows, row0;
+};
+__device__ inline Request look_at(const PromptArgs& a, const Place& pl, int rows, int bs, int threads) {
+    Request q;
+    q.t0 = a.tok_off[pl.r];
+    const int t1 = a.tok_off[pl.r + 1];
+    q.ctx = a.ctx_len[pl.r];
+    if (blockIdx.x == 0) {
+        for (int r = threadIdx.x; r < a.B; r += threads) {
+            const int64_t x = a.tok_off[r], y = a.tok_off[r + 1], c = a.ctx_len[r];
+            if (x < 0 || y < x || y > a.max_tokens || c < y - x || c > (int64_t)a.max_blocks * bs)
+                report(a.status, PULSE_ERR_BAD_INDEX);
+        }
+    }
+    const int fresh = t1 - q.t0;
+    q.n_rows = (int64_t)fresh * a.G;
+    q.row0 = (int64_t)pl.tile * rows;
+    q.any = !(q.t0 < 0 || t1 < q.t0 || t1 > a.max_tokens) && !(pl.tile < 0 || q.row0 >= q.n_rows);
+    q.ok = q.ctx >= fresh && q.ctx <= (int64_t)a.max_blocks * bs;
+    q.base = q.ctx - fresh;
+    return q;
+}
 
 // The 16 KiB of a tile's keys, or of its values, into LDS from 16-bit blocks: 1 KiB a wave and instruction, straight from
 // memory.  A lane's place within a block is the same for every tile.
@@ -225,7 +259,7 @@ struct StageCodes {
                         for (int t = 0; t < 4; ++t) {
                             const float s0 = kv4_scale(sb[t / 2] >> (16 * (t % 2)) & 255u);
                             const float s1 = kv4_scale(sb[t / 2] >> (16 * (t % 2) + 8) & 255u);
-                            w[t] = (decode_pair(v[i][n], t, s0) & 0xFFFFu) | (decode_pair(v[i][n], t, s1) & 0xFFFF0000u);
+                            w[t] = (kv4_pair<ET>(v[i][n], t, s0) & 0xFFFFu) | (kv4_pair<ET>(v[i][n], t, s1) & 0xFFFF0000u);
                         }
                     } else {
                         c = u % 64 / 4 + 16 * (2 * (u % 4) + n);
@@ -238,11 +272,6 @@ struct StageCodes {
         }
     }
 
-    // Codes of byte t of w times `scale`.
-    __device__ static inline uint32_t decode_pair(uint32_t w, int t, float scale) {
-        return t == 0 ? kv4_decode<ET, 0>(w, scale) : t == 1 ? kv4_decode<ET, 1>(w, scale)
-             : t == 2 ? kv4_decode<ET, 2>(w, scale) : kv4_decode<ET, 3>(w, scale);
-    }
     __device__ static constexpr int kv4_scales_per_token() { return kHeadDim / kGroup; }
 };
 
@@ -267,21 +296,11 @@ __global__ __launch_bounds__(W * kWave, 2) void prompt_kernel(PromptArgs a) {
     const int rest = blockIdx.x / a.Hkv;
     const int split = rest % a.n_split;
     const Place pl = find_place(a.tok_off, a.B, a.G, kRows, a.n_tiles - 1 - rest / a.n_split);
-    const int t0 = a.tok_off[pl.r], t1 = a.tok_off[pl.r + 1], ctx = a.ctx_len[pl.r];
-    if (blockIdx.x == 0) {  // every request's lengths
-        for (int r = threadIdx.x; r < a.B; r += W * kWave) {
-            const int64_t x = a.tok_off[r], y = a.tok_off[r + 1], c = a.ctx_len[r];
-            if (x < 0 || y < x || y > a.max_tokens || c < y - x || c > (int64_t)a.max_blocks * BS)
-                report(a.status, PULSE_ERR_BAD_INDEX);
-        }
-    }
-    if (t0 < 0 || t1 < t0 || t1 > a.max_tokens) return;
-    const int fresh = t1 - t0;
-    const int64_t n_rows = (int64_t)fresh * a.G;
-    const int64_t row0 = (int64_t)pl.tile * kRows;
-    if (pl.tile < 0 || row0 >= n_rows) return;
-    const bool ok = ctx >= fresh && ctx <= (int64_t)a.max_blocks * BS;  // else no token is attended to
-    const int base = ctx - fresh;
+    const Request rq = look_at(a, pl, kRows, BS, W * kWave);
+    if (!rq.any) return;
+    const bool ok = rq.ok;
+    const int t0 = rq.t0, ctx = rq.ctx, base = rq.base;
+    const int64_t n_rows = rq.n_rows, row0 = rq.row0;
     // this lane's row
     const int64_t m = row0 + wave * kRowsPerWave + col;
     const bool live = m < n_rows;
@@ -584,6 +603,277 @@ __global__ __launch_bounds__(W * kWave, 2) void prompt_kernel(PromptArgs a) {
         }
 }
 
+// The same for few rows of long contexts (drafted tokens to be verified): a workgroup takes 32 rows, whose keys its waves
+// share out, 32 keys at a time straight from memory into the operands, a step ahead; nothing waits for another wave until
+// the waves' results are joined in LDS.  A lane's operands are whole 16-byte loads in every form of the cache if product c
+// takes channels 64 * half + 8 c .. + 7 of a key, and row m of tile t of the values is channel
+// 64 * (m / 16) + 16 * t + m % 16.
+template <int DT, int BS>
+struct FewLoads {
+    static constexpr int ET = elem_type(DT);
+    static constexpr int kBits = kv_bits(DT);
+    static constexpr int kPer = BS >= 32 ? 1 : 2;  // blocks of a step
+    using vec = typename Mfma<ET>::vec;
+    u32x4 k[kBits / 2];          // 64 channels of a key
+    u32x4 v[2][kBits / 4];       // 8 tokens of 4 channels, of two octets
+    uint32_t ks, vs[2];          // 8 bits: scale bytes of the key's block and of the octets'; 4: two scales of the key
+    u32x2 vs4[2][2];             // 4 bits: scales of 8 tokens, of two channel groups
+
+    __device__ inline void load(const PromptArgs& a, const int (&slot)[2], int in_block, int h, int col, int half) {
+        const int key = key_of_row(col);
+        const uint64_t U = kBits == 16 ? (uint64_t)a.Hkv * BS * kHeadDim * 4
+                         : kBits == 8 ? (uint64_t)kv8_block_bytes(a.Hkv, BS) : (uint64_t)a.Hkv * kv4_head_bytes(BS);
+        const uint8_t* b0 = a.pool + (uint64_t)(uint32_t)slot[0] * U;
+        const uint8_t* b1 = kPer == 2 ? a.pool + (uint64_t)(uint32_t)slot[1] * U : b0;
+        const uint8_t* kb = key >= 16 ? b1 : b0;
+        const int row = (kPer == 2 ? key % 16 : key) + in_block;
+        if constexpr (kBits == 16) {
+            kb += ((size_t)h * BS + row) * 256 + half * 128;
+        } else if constexpr (kBits == 8) {
+            ks = kb[kv8_scales(a.Hkv, BS) + 2 * h];
+            kb += (size_t)h * kv8_head_bytes(BS) + row * 128 + half * 64;
+        } else {
+            kb += (size_t)h * kv4_head_bytes(BS);
+            ks = *reinterpret_cast<const uint16_t*>(kb + kv4_key_scales(BS) + row * 4 + half * 2);
+            kb += row * 64 + half * 32;
+        }
+#pragma unroll
+        for (int i = 0; i < kBits / 2; ++i) k[i] = reinterpret_cast<const u32x4*>(kb)[i];
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+            const uint8_t* vb = st ? b1 : b0;
+            const int oct = ((kPer == 2 ? 0 : 16 * st) + in_block) / 8 + half;
+            if constexpr (kBits == 16) {
+                vb += (size_t)(a.Hkv + h) * BS * 256 + oct * 16;
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    v[st][t] = *reinterpret_cast<const u32x4*>(vb + (64 * (col >> 4) + 16 * t + (col & 15)) * BS * 2);
+            } else if constexpr (kBits == 8) {
+                vs[st] = vb[kv8_scales(a.Hkv, BS) + 2 * h + 1];
+                vb += (size_t)h * kv8_head_bytes(BS) + kv8_values(BS) + oct * 1024 + (col & 15) * 64 + (col >> 4) * 32;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) v[st][i] = reinterpret_cast<const u32x4*>(vb)[i];
+            } else {
+                vb += (size_t)h * kv4_head_bytes(BS);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    vs4[st][i] = *reinterpret_cast<const u32x2*>(vb + kv4_value_scales(BS) + (2 * (col >> 4) + i) * BS + oct * 8);
+                v[st][0] = *reinterpret_cast<const u32x4*>(vb + kv4_values(BS) + oct * 512 + (col & 15) * 32 + (col >> 4) * 16);
+            }
+        }
+    }
+    __device__ inline vec key(int c) const {
+        if constexpr (kBits == 16) return __builtin_bit_cast(vec, k[c]);
+        else if constexpr (kBits == 8)
+            return kv8_decode8<ET>(u32x2{k[c / 2][c % 2 * 2], k[c / 2][c % 2 * 2 + 1]}, kv8_pow2((int)ks - 127));
+        else return kv4_decode8<ET>(k[c / 4][c % 4], kv4_scale(ks >> (8 * (c / 4)) & 255u));
+    }
+    __device__ inline u32x4 value(int st, int t) const {
+        u32x4 w;
+        if constexpr (kBits == 16) {
+            w = v[st][t];
+        } else if constexpr (kBits == 8) {
+            w = __builtin_bit_cast(u32x4, kv8_decode8<ET>(u32x2{v[st][t / 2][t % 2 * 2], v[st][t / 2][t % 2 * 2 + 1]},
+                                                          kv8_pow2((int)vs[st] - 127)));
+        } else {
+            const u32x2 sb = vs4[st][t / 2];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                const float s0 = kv4_scale(sb[n / 2] >> (16 * (n % 2)) & 255u);
+                const float s1 = kv4_scale(sb[n / 2] >> (16 * (n % 2) + 8) & 255u);
+                w[n] = (kv4_pair<ET>(v[st][0][t], n, s0) & 0xFFFFu) | (kv4_pair<ET>(v[st][0][t], n, s1) & 0xFFFF0000u);
+            }
+        }
+        return w;
+    }
+};
+
+// grid as prompt_kernel's, with 32 rows a workgroup.
+template <int DT, int BS>
+__global__ __launch_bounds__(kWaves * kWave, 2) void prompt_few_kernel(PromptArgs a) {
+    constexpr int ET = elem_type(DT);
+    constexpr int W = kWaves, kRows = 32, kStep = 32;
+    constexpr int kPer = FewLoads<DT, BS>::kPer;
+    using vec = typename Mfma<ET>::vec;
+    __shared__ __align__(16) float s_o[W][kRows][kHeadDim];
+    __shared__ float2 s_ml[W][kRows];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const int h = blockIdx.x % a.Hkv;
+    const int rest = blockIdx.x / a.Hkv;
+    const int split = rest % a.n_split;
+    const Place pl = find_place(a.tok_off, a.B, a.G, kRows, a.n_tiles - 1 - rest / a.n_split);
+    const Request q = look_at(a, pl, kRows, BS, W * kWave);
+    if (!q.any) return;
+    const int64_t m = q.row0 + col;
+    const bool live = m < q.n_rows;
+    const int mi = (int)(live ? m : q.n_rows - 1);
+    const int tok = (int)((uint64_t)mi * a.g_magic >> 32), g = mi - tok * a.G;
+    const int p = q.base + tok;
+    const int Hq = a.Hkv * a.G;
+    const int64_t last_row = min(q.row0 + kRows - 1, q.n_rows - 1);
+    const int keys = q.ok ? q.base + (int)((uint64_t)last_row * a.g_magic >> 32) + 1 : 0;
+    const int all = q.base + (int)((uint64_t)q.row0 * a.g_magic >> 32) + 1;  // keys that every row attends to
+    // this wave's steps: a share of the split's, which is a share of the context
+    const int n_steps = (keys + kStep - 1) / kStep, shares = a.n_split * W, share = split * W + wave;
+    const int i0 = (int)((int64_t)n_steps * share / shares), i1 = (int)((int64_t)n_steps * (share + 1) / shares);
+
+    const auto* row = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(a.table + (size_t)pl.r * a.max_blocks);
+    const int last_blk = (q.ctx + BS - 1) / BS - 1;
+    int slot[2] = {0, 0}, ahead[2] = {0, 0};
+    uint32_t bad = 0, bad_next = 0;
+    auto look_up = [&](int i) {
+        ahead[0] = row[min(BS == 64 ? i / 2 : i * kPer, last_blk)];
+        if (kPer == 2) ahead[1] = row[min(i * kPer + 1, last_blk)];
+    };
+    auto take = [&]() {  // the slots that were looked up; a block without one is read as slot 0 and counts nothing
+        bad_next = 0;
+#pragma unroll
+        for (int b = 0; b < kPer; ++b) {
+            slot[b] = ahead[b];
+            if ((uint32_t)slot[b] >= (uint32_t)a.n_slots) {
+                bad_next |= 1u << b;
+                slot[b] = 0;
+                if (lane == 0) report(a.status, PULSE_ERR_BAD_INDEX);
+            }
+        }
+    };
+
+    f32x16 acc[4] = {};
+    float m_run = -INFINITY, l_run = 0.f;
+    const float scale = fmaxf(fabsf(a.scale_log2), 1e-30f);
+    vec qb[8];
+    FewLoads<DT, BS> x;
+    if (i0 < i1) {
+        look_up(i0);
+        take();
+        x.load(a, slot, BS == 64 ? i0 % 2 * 32 : 0, h, col, half);
+        bad = bad_next;
+        if (i0 + 1 < i1) look_up(i0 + 1);
+        const uint16_t* qr = a.q + (int64_t)(q.t0 + tok) * a.q_stride + (size_t)(h * a.G + g) * kHeadDim + half * 64;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) qb[c] = load_vec<ET>(qr + 8 * c);
+        if (a.scale_log2 < 0.f) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) qb[c] = -qb[c];
+        }
+    }
+#pragma unroll 1
+    for (int i = i0; i < i1; ++i) {
+        const int k0 = i * kStep;
+        f32x16 s = {};
+#pragma unroll
+        for (int c = 0; c < 8; ++c) s = mac32<ET>(x.key(c), qb[c], s);
+        FewLoads<DT, BS> now = x;
+        const uint32_t bad_now = bad;
+        if (i + 1 < i1) {
+            take();
+            x.load(a, slot, BS == 64 ? (i + 1) % 2 * 32 : 0, h, col, half);
+            bad = bad_next;
+            if (i + 2 < i1) look_up(i + 2);
+        }
+        if (k0 + kStep > all || bad_now) {
+            const int left = p + 1 - k0 - 8 * half;
+#pragma unroll
+            for (int n = 0; n < 16; ++n) {
+                const int k = 16 * (n / 8) + n % 8;
+                if (k >= left || (bad_now >> (kPer == 2 ? n / 8 : 0) & 1)) s[n] = -INFINITY;
+            }
+        }
+        float cm = s[0];
+#pragma unroll
+        for (int n = 1; n < 16; ++n) cm = __builtin_elementwise_maximum(cm, s[n]);
+        const uint32_t u = __float_as_uint(cm);
+        const u32x2 w = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        cm = __builtin_elementwise_maximum(__uint_as_float(w[0]), __uint_as_float(w[1])) * scale;
+        if (__ballot(!(cm <= m_run + 8.f))) {  // (as in prompt_kernel)
+            const float m_new = __builtin_elementwise_maximum(m_run, cm);
+            const float alpha = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
+            m_run = m_new;
+            l_run *= alpha;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) acc[t] *= alpha;
+        }
+        const float m_use = m_run == -INFINITY ? 0.f : m_run;
+        float sum = 0.f;
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+            float y[8];
+#pragma unroll
+            for (int n = 0; n < 8; ++n) {
+                y[n] = __builtin_amdgcn_exp2f(fmaf(s[8 * st + n], scale, -m_use));
+                sum += y[n];
+            }
+            const vec pv = __builtin_bit_cast(vec, u32x4{pack2<ET>(y[0], y[1]), pack2<ET>(y[2], y[3]),
+                                                         pack2<ET>(y[4], y[5]), pack2<ET>(y[6], y[7])});
+            u32x4 v[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) v[t] = now.value(st, t);
+            if (k0 + kStep > q.ctx || bad_now) {  // tokens that are not the context's: anything may lie there
+                const int left = bad_now >> (kPer == 2 ? st : 0) & 1 ? 0 : q.ctx - k0 - 16 * st - 8 * half;
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    const uint32_t keep = (2 * n < left ? 0xFFFFu : 0u) | (2 * n + 1 < left ? 0xFFFF0000u : 0u);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) v[t][n] &= keep;
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < 4; ++t) acc[t] = mac32<ET>(__builtin_bit_cast(vec, v[t]), pv, acc[t]);
+        }
+        l_run += sum;
+    }
+    {
+        const uint32_t u = __float_as_uint(l_run);
+        const u32x2 w = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        l_run = __uint_as_float(w[0]) + __uint_as_float(w[1]);
+    }
+    // the waves' results side by side (4 channels of a row at a place that depends on the row), then joined
+    if (half == 0) s_ml[wave][col] = make_float2(m_run, l_run);
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int c4 = 16 * (b / 2) + 4 * t + 2 * (b % 2) + half;  // (channel / 4)
+            *reinterpret_cast<f32x4*>(&s_o[wave][col][4 * (c4 ^ col)]) =
+                f32x4{acc[t][4 * b], acc[t][4 * b + 1], acc[t][4 * b + 2], acc[t][4 * b + 3]};
+        }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < kRows * kHeadDim / 4 / (W * kWave); ++n) {
+        const int at = n * W * kWave + threadIdx.x, r = at / 32, c4 = at % 32;
+        const int64_t mr = q.row0 + r;
+        if (mr >= q.n_rows) break;
+        float top = s_ml[0][r].x;
+#pragma unroll
+        for (int w = 1; w < W; ++w) top = __builtin_elementwise_maximum(top, s_ml[w][r].x);
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        float l = 0.f;
+        if (top != -INFINITY) {
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float2 ml = s_ml[w][r];
+                const float f = __builtin_amdgcn_exp2f(ml.x - top);
+                l += ml.y * f;
+                o += *reinterpret_cast<const f32x4*>(&s_o[w][r][4 * (c4 ^ r)]) * f;
+            }
+        }
+        const int tr = (int)((uint64_t)mr * a.g_magic >> 32), head = h * a.G + (int)mr - tr * a.G;
+        const int64_t out_row = q.t0 + tr, slot_row = out_row * Hq + head;
+        if (a.n_split > 1) {
+            const int64_t part = (int64_t)split * a.max_tokens * Hq + slot_row;
+            if (c4 == 0) a.ws_ml[part] = make_float2(top, l);
+            *reinterpret_cast<f32x4*>(a.ws_o + part * kHeadDim + 4 * c4) = o;
+        } else {
+            if (top != -INFINITY) o *= 1.f / l;
+            *reinterpret_cast<u32x2*>(a.out + out_row * a.out_stride + (size_t)head * kHeadDim + 4 * c4) =
+                u32x2{pack2<ET>(o[0], o[1]), pack2<ET>(o[2], o[3])};
+            if (a.lse && c4 == 0)
+                a.lse[slot_row] = top == -INFINITY ? -INFINITY : (top + log2f(l)) * 0.69314718055994531f;
+        }
+    }
+}
+
 // Joins the splits of a row: a wave per two rows, a lane four channels.
 template <int ET>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
@@ -614,11 +904,21 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
 }
 
 struct PromptPlan {
+    int rows;  // of a workgroup: 32 (prompt_few_kernel), 128 or 256
     int n_tiles, n_split;
 };
 
 constexpr int kSplitGroups = 512;  // workgroups aimed at where few rows are split over the context: two a CU
-constexpr int kLeastTiles = 4;  // tiles of keys of a split
+constexpr int kLeastTiles = 4;     // tiles of keys of a split
+constexpr int kFewRows = 32;
+// Workgroups of eight waves, which stage and decode a tile for twice the rows, from two rounds of them and 2048 new tokens
+// of a request on: below, the rows behind the diagonal that the larger tile multiplies in vain cost more.  In us, four
+// waves and eight, 32 query heads over 8 KV heads, 16-bit and 8-bit cache:
+//   1 x 2048   51.9  64.4   63.3  68.2      8 x 1024    96.7 111.0   108.5 110.8
+//   1 x 4096  149.7 138.6  163.4 149.6      1 x 8192   535.5 523.3   592.7 552.9
+// The 4-bit cache, 4096 tokens at the end of 32768: 2097 and 1900.
+constexpr int kLongPrompt = 2048;
+constexpr int kLongGroups = 512;
 
 static int64_t key_tiles(const pulse_shape& s, int32_t max_blocks) {
     return ((int64_t)max_blocks * s.block_size + kKeys - 1) / kKeys;
@@ -626,9 +926,14 @@ static int64_t key_tiles(const pulse_shape& s, int32_t max_blocks) {
 
 static PromptPlan prompt_plan(const pulse_shape& s, int32_t B, int64_t max_tokens, int32_t max_blocks) {
     PromptPlan p;
-    const int64_t G = s.num_q_heads / s.num_kv_heads, rows = kWaves * kRowsPerWave;
-    p.n_tiles = (int)(max_tokens * G / rows + B);
-    const int64_t units = std::max<int64_t>((max_tokens * G + rows - 1) / rows, B) * s.num_kv_heads;
+    const int64_t G = s.num_q_heads / s.num_kv_heads;
+    const int64_t all = max_tokens * G;
+    p.rows = kWaves * kRowsPerWave;
+    if (all <= (int64_t)kFewRows * B) p.rows = 32;
+    else if (max_tokens >= (int64_t)kLongPrompt * B && all * s.num_kv_heads >= (int64_t)kLongGroups * 2 * p.rows) p.rows *= 2;
+    const int64_t rows = p.rows;
+    p.n_tiles = (int)(all / rows + B);
+    const int64_t units = std::max<int64_t>((all + rows - 1) / rows, B) * s.num_kv_heads;
     p.n_split = (int)std::max<int64_t>(1, std::min(kSplitGroups / units, key_tiles(s, max_blocks) / kLeastTiles));
     return p;
 }
@@ -636,7 +941,7 @@ static PromptPlan prompt_plan(const pulse_shape& s, int32_t B, int64_t max_token
 static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Partials of the splits of this call and every smaller one: fewer rows may have more splits, but no more than kSplitGroups
-// workgroups' rows, nor than the context has splits.
+// workgroups' rows, nor than the context has splits (calls of 256 rows a workgroup have no splits).
 size_t prompt_ws_bytes(const pulse_shape& s, int32_t B, int64_t max_tokens, int32_t max_blocks) {
     const int64_t most = key_tiles(s, max_blocks) / kLeastTiles;
     if (most <= 1) return 256;
@@ -645,16 +950,18 @@ size_t prompt_ws_bytes(const pulse_shape& s, int32_t B, int64_t max_tokens, int3
 }
 
 template <int DT, int BS>
-static void launch_prompt_t(const PromptArgs& a, hipStream_t st) {
+static void launch_prompt_t(const PromptArgs& a, int rows, hipStream_t st) {
     const dim3 grid((unsigned)((int64_t)a.Hkv * a.n_tiles * a.n_split));
-    hipLaunchKernelGGL((prompt_kernel<DT, BS, kWaves>), grid, dim3(kWaves * kWave), 0, st, a);
+    if (rows == 32) hipLaunchKernelGGL((prompt_few_kernel<DT, BS>), grid, dim3(kWaves * kWave), 0, st, a);
+    else if (rows == kWaves * kRowsPerWave) hipLaunchKernelGGL((prompt_kernel<DT, BS, kWaves>), grid, dim3(kWaves * kWave), 0, st, a);
+    else hipLaunchKernelGGL((prompt_kernel<DT, BS, 2 * kWaves>), grid, dim3(2 * kWaves * kWave), 0, st, a);
 }
 
 template <int DT>
-static void launch_prompt_bs(int32_t bs, const PromptArgs& a, hipStream_t st) {
-    if (bs == 16) launch_prompt_t<DT, 16>(a, st);
-    else if (bs == 32) launch_prompt_t<DT, 32>(a, st);
-    else launch_prompt_t<DT, 64>(a, st);
+static void launch_prompt_bs(int32_t bs, const PromptArgs& a, int rows, hipStream_t st) {
+    if (bs == 16) launch_prompt_t<DT, 16>(a, rows, st);
+    else if (bs == 32) launch_prompt_t<DT, 32>(a, rows, st);
+    else launch_prompt_t<DT, 64>(a, rows, st);
 }
 
 hipError_t launch_prompt_attn(const pulse_shape& s, const void* q, int64_t q_stride, const int32_t* tok_off,
@@ -671,12 +978,12 @@ hipError_t launch_prompt_attn(const pulse_shape& s, const void* q, int64_t q_str
     if (p.n_split > 1)
         a.ws_ml = ws_at<float2>(ws, up256((size_t)p.n_split * max_tokens * s.num_q_heads * kHeadDim * sizeof(float)));
     switch (s.dtype) {
-        case PULSE_BF16: launch_prompt_bs<PULSE_BF16>(s.block_size, a, st); break;
-        case PULSE_F16: launch_prompt_bs<PULSE_F16>(s.block_size, a, st); break;
-        case PULSE_BF16_KV8: launch_prompt_bs<PULSE_BF16_KV8>(s.block_size, a, st); break;
-        case PULSE_F16_KV8: launch_prompt_bs<PULSE_F16_KV8>(s.block_size, a, st); break;
-        case PULSE_BF16_KV4: launch_prompt_bs<PULSE_BF16_KV4>(s.block_size, a, st); break;
-        case PULSE_F16_KV4: launch_prompt_bs<PULSE_F16_KV4>(s.block_size, a, st); break;
+        case PULSE_BF16: launch_prompt_bs<PULSE_BF16>(s.block_size, a, p.rows, st); break;
+        case PULSE_F16: launch_prompt_bs<PULSE_F16>(s.block_size, a, p.rows, st); break;
+        case PULSE_BF16_KV8: launch_prompt_bs<PULSE_BF16_KV8>(s.block_size, a, p.rows, st); break;
+        case PULSE_F16_KV8: launch_prompt_bs<PULSE_F16_KV8>(s.block_size, a, p.rows, st); break;
+        case PULSE_BF16_KV4: launch_prompt_bs<PULSE_BF16_KV4>(s.block_size, a, p.rows, st); break;
+        case PULSE_F16_KV4: launch_prompt_bs<PULSE_F16_KV4>(s.block_size, a, p.rows, st); break;
         default: return hipErrorInvalidValue;
     }
     hipError_t e = hipGetLastError();

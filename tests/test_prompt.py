@@ -181,6 +181,20 @@ def test_new_tokens(case, bits):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("ctx,new,hq,hkv,bs,dt,bits", [
+    ([4200], None, 32, 8, 16, "bf16", 16), ([2300, 2100], None, 64, 16, 32, "f16", 8), ([2900], [2700], 48, 8, 64, "bf16", 4),
+    ([4111], None, 32, 2, 16, "f16", 4), ([2500, 1900], None, 32, 8, 64, "bf16", 16), ([2431, 1900], None, 36, 12, 32, "bf16", 8)])
+def test_long_prompts(ctx, new, hq, hkv, bs, dt, bits):
+    """Prompts long and wide enough for the workgroups of 256 rows."""
+    say(f"\n[gpu] prompt {bits} bits ctx={ctx} hq={hq} hkv={hkv} bs={bs} {dt}")
+    c = Case(ctx, new or ctx, hq, hkv, bs, dt, bits, sum(ctx))
+    out, lse = c.run()
+    c.check(out, lse)
+    again = c.run(fill=0)
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("bits,scale", [(16, 0.0), (8, -0.1), (16, -0.2), (4, 1.0)])
 def test_any_scale(bits, scale):
     c = Case([100, 300], [100, 40], 8, 2, 16, "bf16", bits, 5)
