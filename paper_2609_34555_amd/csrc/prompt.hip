@@ -874,33 +874,82 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void prompt_few_kernel(PromptArg
     }
 }
 
-// Joins the splits of a row: a wave per two rows, a lane four channels.
-template <int ET>
+// Joins the splits of the rows: 32 threads, four channels each, take a row and `STRIDE`th splits of it, four of which are
+// loaded before any is used; a workgroup holds eight rows, or (many splits: STRIDE 8) eight shares of one row, which it adds
+// up in LDS.  (Loaded
+// one after another, 64 splits took 45 us more: 5 tokens at the end of 64K, 4 bits, 69 and 24 us.)
+constexpr int kManySplits = 8;  // above it, a workgroup a row
+
+template <int ET, int STRIDE>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
+    __shared__ f32x4 s_o[8][32];
+    __shared__ float2 s_ml[8];
     const int Hq = a.Hkv * a.G;
     const int64_t rows = (int64_t)a.max_tokens * Hq;
-    const int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int c = (threadIdx.x & 31) * 4;
+    const int part = threadIdx.x >> 5, c4 = threadIdx.x & 31;
+    const int64_t at = STRIDE == 1 ? (int64_t)blockIdx.x * 8 + part : (int64_t)blockIdx.x;
     const int last = a.tok_off[a.B];
-    if (at >= (int64_t)last * Hq || last > a.max_tokens) return;
-    float mx = -INFINITY;
-    for (int s = 0; s < a.n_split; ++s) mx = fmaxf(mx, a.ws_ml[s * rows + at].x);
+    const bool any = at < (int64_t)last * Hq && last <= a.max_tokens;
+    if (STRIDE > 1 && !any) return;
+    float top = -INFINITY, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    float l = 0.f;
-    if (mx != -INFINITY) {
-        for (int s = 0; s < a.n_split; ++s) {
-            const float2 ml = a.ws_ml[s * rows + at];
-            if (ml.x == -INFINITY) continue;
-            const float w = __builtin_amdgcn_exp2f(ml.x - mx);
-            const f32x4 x = *reinterpret_cast<const f32x4*>(a.ws_o + (s * rows + at) * kHeadDim + c);
-            l += ml.y * w;
-            o += x * w;
+    for (int s0 = STRIDE == 1 ? 0 : part; any && s0 < a.n_split; s0 += 4 * STRIDE) {
+        float2 ml[4];
+        f32x4 x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int s = min(s0 + i * STRIDE, a.n_split - 1);
+            ml[i] = a.ws_ml[s * rows + at];
+            x[i] = *reinterpret_cast<const f32x4*>(a.ws_o + (s * rows + at) * kHeadDim + 4 * c4);
         }
-        o *= 1.f / l;
+        float m = top;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (s0 + i * STRIDE < a.n_split) m = __builtin_elementwise_maximum(m, ml[i].x);
+        if (m == -INFINITY) continue;
+        const float f = __builtin_amdgcn_exp2f(top - m);
+        top = m;
+        l *= f;
+        o *= f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (s0 + i * STRIDE >= a.n_split || ml[i].x == -INFINITY) continue;  // (such a split's sums are not written)
+            const float w = __builtin_amdgcn_exp2f(ml[i].x - m);
+            l += ml[i].y * w;
+            o += x[i] * w;
+        }
     }
-    uint16_t* dst = a.out + at / Hq * a.out_stride + at % Hq * kHeadDim + c;
+    if (STRIDE > 1) {
+        s_o[part][c4] = o;
+        if (c4 == 0) s_ml[part] = make_float2(top, l);
+        __syncthreads();
+        if (part) return;
+        float m = top;
+        for (int i = 1; i < 8; ++i) m = __builtin_elementwise_maximum(m, s_ml[i].x);
+        l = 0.f;
+        o = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; m != -INFINITY && i < 8; ++i) {
+            const float2 ml = s_ml[i];
+            const float w = __builtin_amdgcn_exp2f(ml.x - m);
+            l += ml.y * w;
+            o += s_o[i][c4] * w;
+        }
+        top = m;
+    }
+    if (!any) return;
+    if (top != -INFINITY) o *= 1.f / l;
+    uint16_t* dst = a.out + at / Hq * a.out_stride + at % Hq * kHeadDim + 4 * c4;
     *reinterpret_cast<u32x2*>(dst) = u32x2{pack2<ET>(o[0], o[1]), pack2<ET>(o[2], o[3])};
-    if (a.lse && c == 0) a.lse[at] = mx == -INFINITY ? -INFINITY : (mx + log2f(l)) * 0.69314718055994531f;
+    if (a.lse && c4 == 0) a.lse[at] = top == -INFINITY ? -INFINITY : (top + log2f(l)) * 0.69314718055994531f;
+}
+
+template <int ET>
+static void launch_join(const PromptArgs& a, hipStream_t st) {
+    const int64_t rows = (int64_t)a.max_tokens * a.Hkv * a.G;
+    if (a.n_split > kManySplits)
+        hipLaunchKernelGGL((prompt_join_kernel<ET, 8>), dim3((unsigned)rows), dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL((prompt_join_kernel<ET, 1>), dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, a);
 }
 
 struct PromptPlan {
@@ -910,7 +959,9 @@ struct PromptPlan {
 
 constexpr int kSplitGroups = 512;  // workgroups aimed at where few rows are split over the context: two a CU
 constexpr int kLeastTiles = 4;     // tiles of keys of a split
-constexpr int kFewRows = 32;
+// Rows of a request, on average, up to which prompt_few_kernel takes them, 32 to a workgroup: beyond 32 every workgroup
+// reads the keys again, which costs the 16-bit cache more than the decoding of codes that 128 rows share saves the others.
+static int64_t few_rows(const pulse_shape& s) { return kv_bits(s.dtype) == 16 ? 32 : 64; }
 // Workgroups of eight waves, which stage and decode a tile for twice the rows, from two rounds of them and 2048 new tokens
 // of a request on: below, the rows behind the diagonal that the larger tile multiplies in vain cost more.  In us, four
 // waves and eight, 32 query heads over 8 KV heads, 16-bit and 8-bit cache:
@@ -929,7 +980,7 @@ static PromptPlan prompt_plan(const pulse_shape& s, int32_t B, int64_t max_token
     const int64_t G = s.num_q_heads / s.num_kv_heads;
     const int64_t all = max_tokens * G;
     p.rows = kWaves * kRowsPerWave;
-    if (all <= (int64_t)kFewRows * B) p.rows = 32;
+    if (all <= few_rows(s) * B) p.rows = 32;
     else if (max_tokens >= (int64_t)kLongPrompt * B && all * s.num_kv_heads >= (int64_t)kLongGroups * 2 * p.rows) p.rows *= 2;
     const int64_t rows = p.rows;
     p.n_tiles = (int)(all / rows + B);
@@ -988,9 +1039,8 @@ hipError_t launch_prompt_attn(const pulse_shape& s, const void* q, int64_t q_str
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.n_split == 1) return e;
-    const unsigned groups = (unsigned)((max_tokens * s.num_q_heads + 7) / 8);
-    if (elem_type(s.dtype) == PULSE_BF16) hipLaunchKernelGGL(prompt_join_kernel<PULSE_BF16>, dim3(groups), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(prompt_join_kernel<PULSE_F16>, dim3(groups), dim3(256), 0, st, a);
+    if (elem_type(s.dtype) == PULSE_BF16) launch_join<PULSE_BF16>(a, st);
+    else launch_join<PULSE_F16>(a, st);
     return hipGetLastError();
 }
 
