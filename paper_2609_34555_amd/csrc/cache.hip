@@ -403,7 +403,7 @@ __device__ inline Scale8 scale8(uint32_t top, uint32_t old_byte, bool anew) {
     return Scale8{(uint32_t)(e + 127), kv8_pow2(-e), anew || e == old ? 1.f : kv8_pow2(max(old - e, -126))};
 }
 
-// grid = (Hkv, groups of `per` rows): a workgroup takes one head of the runs that begin in its `per` rows (1 or BS).
+// grid = (Hkv, groups of `per` rows): a workgroup takes one head of the runs that begin in its `per` rows (up to BS).
 template <int DT, int BS>
 __global__ __launch_bounds__(BS / 16 * kWave) void append8_kernel(CacheArgs a, int32_t per) {
     constexpr int kWaves = BS / 16;
@@ -413,7 +413,7 @@ __global__ __launch_bounds__(BS / 16 * kWave) void append8_kernel(CacheArgs a, i
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l = lane & 15, grp = lane >> 4, h = blockIdx.x;
     for (int64_t r0 = blockIdx.y * (int64_t)per; r0 < a.rows; r0 += gridDim.y * (int64_t)per) {
-        // slots of the row before, of the group's rows and of those that its last run may go on to: two places a lane
+        // slots of the row before, of the group's rows and of those that its last run may go on to
         int64_t m[2], slot[2], prev[2];
         uint64_t on[2], same[2];
 #pragma unroll
@@ -436,12 +436,11 @@ __global__ __launch_bounds__(BS / 16 * kWave) void append8_kernel(CacheArgs a, i
 #pragma unroll
         for (int i = 0; i < 2; ++i) same[i] = __ballot(slot[i] >= 0 && slot[i] == prev[i]);
         for (int at = 1; at <= per; ++at) {
-            const int w = at >> 6, b = at & 63;
-            if (!(on[w] >> b & 1) || (same[w] >> b & 1)) continue;
+            if (!(on[0] >> at & 1) || (same[0] >> at & 1)) continue;  // (at <= 32)
             // rows of the run: those behind its first that are in the same slot, at most a block's
             int n = 1;
-            while (n < BS && at + n < 128 && (same[(at + n) >> 6] >> ((at + n) & 63) & 1)) ++n;
-            const int64_t blk = __shfl(w ? slot[1] : slot[0], b);
+            while (n < BS && ((at + n < 64 ? same[0] : same[1]) >> ((at + n) & 63) & 1)) ++n;
+            const int64_t blk = __shfl(slot[0], at);
             const int64_t first = r0 - 1 + at;
             if (lane < BS) s_row[wave][lane] = -1;
             wave_lds_order();
@@ -547,9 +546,16 @@ __global__ __launch_bounds__(BS / 16 * kWave) void append8_kernel(CacheArgs a, i
     }
 }
 
+// Rows times heads up to which a workgroup looks at one row, at eight, and above at a block's (32 at most, which two places
+// a lane hold with a block behind them).  In us with the reading of what was written, one row and eight: 1 x 1000 rows x 8
+// heads 17.2 and 11.1, 1024 requests of one row 28.5 and 43.4; eight and a block: 18K rows 52.0 and 44.4, 8 x 300 rows 15.0
+// and 16.7.
+constexpr int64_t kRunRows8 = 4096, kRunRows8Most = 65536;
+
 template <int DT, int BS>
 static void launch_append8_t(const CacheArgs& a, hipStream_t st) {
-    const int32_t per = (int64_t)a.rows * a.Hkv > kRunRows ? BS / 2 : 1;
+    const int64_t units = (int64_t)a.rows * a.Hkv;
+    const int32_t per = units > kRunRows8Most ? (BS < 32 ? BS : 32) : units > kRunRows8 ? 8 : 1;
     const int64_t groups = ((int64_t)a.rows + per - 1) / per;
     const dim3 grid((unsigned)a.Hkv, (unsigned)(groups < kCacheGrid ? groups : kCacheGrid));
     hipLaunchKernelGGL((append8_kernel<DT, BS>), grid, dim3(BS / 16 * kWave), 0, st, a, per);

@@ -17,9 +17,14 @@ namespace pulse {
 constexpr int kPageThreads = 256;
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / kWave;
-constexpr int kTile = 1024;           // entries of a workgroup in the passes over tables
+constexpr int kTile = 256;            // entries of a workgroup in the passes over tables
 constexpr int kChunk = 16384;         // bytes of a block that a workgroup copies at a time
-constexpr int64_t kOneGroup = 65536;  // table entries up to which one workgroup makes every pass
+// Table entries up to which one workgroup makes every pass of a free, and table and list entries up to which it plans a
+// compaction.  In us, a pass of a free (three small copies and a fork with it), one workgroup and a launch for each of its
+// four passes: 635 entries 27 and 34, 3K 28.8 and 34, 6K 37.3 and 37.2, 8K 43 and 38, 33K 121 and 38; a compaction of
+// 6K entries and a list of 8K 63.4 and 70.5.
+constexpr int kOneFree = 4096;
+constexpr int kOneGroup = 8192;
 constexpr int kCopyGroups = 2048;
 
 // Values that other workgroups, or other waves, wrote in this launch or an atomic changed: past the vector cache.
@@ -77,22 +82,29 @@ struct FreeArgs {
 // N entries, 64 from one to the next, loaded before any of them is looked at.
 template <int N>
 struct Entries {
-    int e[N], slot[N], keep[N];
+    int e[N], j[N], slot[N], keep[N];
     bool in[N];
     __device__ Entries(const FreeArgs& a, int first, int end) {
+        int r = first / a.mb, at = first - r * a.mb;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             in[i] = first + 64 * i < end;
-            e[i] = in[i] ? first + 64 * i : end - 1;
+            e[i] = in[i] ? first + 64 * i : 0;
+            j[i] = in[i] ? at : 0;
             slot[i] = a.table[e[i]];
-            keep[i] = a.keep[e[i] / a.mb];
+            keep[i] = a.keep[in[i] ? r : 0];
+            at += 64;
+            if (at >= a.mb) {
+                const int rows = at / a.mb;
+                r += rows;
+                at -= rows * a.mb;
+            }
         }
     }
 };
 
 // Slot of an entry if it is freed, -1 if not, -2 if something is wrong with it.
-__device__ inline int freed_slot(const FreeArgs& a, int e, int s, int keep) {
-    const int j = e % a.mb;
+__device__ inline int freed_slot(const FreeArgs& a, int j, int s, int keep) {
     if (keep < 0) return -2;
     if (j * (int64_t)a.bs >= keep) return s == -1 ? -1 : (s < 0 || s >= a.n_slots) ? -2 : s;
     // a kept block that tokens are taken out of is appended to next, which no other request may see
@@ -122,49 +134,41 @@ __device__ inline void free_apply(const FreeArgs& a, int e, int s, bool returns,
     a.table[e] = -1;
 }
 
-// All passes in one workgroup: a wave takes a stretch of the entries, four times 64 at a time.
+// Stores and atomics of this wave have reached L2, where the workgroup's other waves look.
+__device__ inline void reached_l2() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
+// All passes in one workgroup, N times 64 entries a wave, which stay in registers.
+template <int N>
 __global__ __launch_bounds__(kPlanThreads) void free_small_kernel(FreeArgs a) {
-    __shared__ uint64_t s_ret[kOneGroup / 64 + 4];
     __shared__ int s_wave[kPlanWaves];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = a.B * a.mb;
-    const int each = ((n + 63) / 64 + 4 * kPlanWaves - 1) / (4 * kPlanWaves) * 4;  // words of 64 of a wave
-    const int first = min(n, wave * each * 64), end = min(n, first + each * 64);
     const int head = *a.free_head;
+    const Entries<N> x(a, wave * 64 * N + lane, n);
     bool wrong = head < 0 || head > a.n_free;
-    for (int e = first; e < end; e += 256) {
-        const Entries<4> x(a, e + lane, end);
+    int s[N];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int s = freed_slot(a, x.e[i], x.slot[i], x.keep[i]);
-            wrong |= x.in[i] && s == -2;
-            if (x.in[i] && s >= 0) free_reset(a, s);
-        }
+    for (int i = 0; i < N; ++i) {
+        s[i] = x.in[i] ? freed_slot(a, x.j[i], x.slot[i], x.keep[i]) : -1;
+        wrong |= s[i] == -2;
+        if (s[i] >= 0) free_reset(a, s[i]);
     }
-    __threadfence();
-    __syncthreads();
-    for (int e = first; e < end; e += 256) {
-        const Entries<4> x(a, e + lane, end);
+    reached_l2();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int s = freed_slot(a, x.e[i], x.slot[i], x.keep[i]);
-            if (x.in[i] && s >= 0) free_count(a, x.e[i], s);
-        }
-    }
-    __threadfence();
-    __syncthreads();
+    for (int i = 0; i < N; ++i)
+        if (s[i] >= 0) free_count(a, x.e[i], s[i]);
+    reached_l2();
+    uint64_t ret[N];
     int mine = 0;
-    for (int e = first; e < end; e += 256) {
-        const Entries<4> x(a, e + lane, end);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int s = freed_slot(a, x.e[i], x.slot[i], x.keep[i]);
-            bool returns = false;
-            if (x.in[i] && s >= 0) returns = free_returns(a, x.e[i], s, wrong);
-            const uint64_t b = __ballot(returns);
-            if (lane == 0) s_ret[e / 64 + i] = b;
-            mine += __popcll(b);
-        }
+    for (int i = 0; i < N; ++i) {
+        bool returns = false;
+        if (s[i] >= 0) returns = free_returns(a, x.e[i], s[i], wrong);
+        ret[i] = __ballot(returns);
+        mine += __popcll(ret[i]);
     }
     if (lane == 0) s_wave[wave] = mine;
     wrong = __syncthreads_or(wrong);
@@ -178,15 +182,10 @@ __global__ __launch_bounds__(kPlanThreads) void free_small_kernel(FreeArgs a) {
         return;
     }
     int at = head - total + before;
-    for (int e = first; e < end; e += 256) {
-        const Entries<4> x(a, e + lane, end);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint64_t b = s_ret[e / 64 + i];
-            const int s = freed_slot(a, x.e[i], x.slot[i], x.keep[i]);
-            if (x.in[i] && s >= 0) free_apply(a, x.e[i], s, b >> lane & 1, at + __popcll(b & ((1ull << lane) - 1)));
-            at += __popcll(b);
-        }
+    for (int i = 0; i < N; ++i) {
+        if (s[i] >= 0) free_apply(a, x.e[i], s[i], ret[i] >> lane & 1, at + __popcll(ret[i] & ((1ull << lane) - 1)));
+        at += __popcll(ret[i]);
     }
     if (threadIdx.x == 0) *a.free_head = head - total;
 }
@@ -204,7 +203,7 @@ __global__ __launch_bounds__(kPageThreads) void free_kernel(FreeArgs a) {
     bool wrong = false;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-        s[i] = freed_slot(a, x.e[i], x.slot[i], x.keep[i]);
+        s[i] = freed_slot(a, x.j[i], x.slot[i], x.keep[i]);
         if (!x.in[i]) s[i] = -1;
         wrong |= s[i] == -2;
         if (PASS == 0 && s[i] >= 0) free_reset(a, s[i]);
@@ -438,41 +437,27 @@ __device__ inline int ranked(int n, int* s_wave, V value, K keep, E emit) {
     return total;
 }
 
-// The moves: which slots, and where to.  ONE: this workgroup also makes the marks, in LDS.
-template <bool ONE>
+__device__ inline void write_plan(const CompactArgs& a, bool wrong, int moves, int low, int head) {
+    a.plan[0] = wrong ? 0 : moves;
+    a.plan[1] = wrong ? 0 : low;
+    a.plan[2] = wrong ? PULSE_ERR_BAD_INDEX : moves > low ? PULSE_ERR_POOL_EXHAUSTED : 0;
+    a.plan[3] = wrong ? 0 : head;
+}
+
+// The moves from the marks: which slots, and where to.
 __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(CompactArgs a) {
-    extern __shared__ uint32_t s_bits[];
     __shared__ int s_wave[kPlanWaves];
     const int words = (a.n_slots + 31) / 32;
-    uint32_t* live = ONE ? s_bits : a.live;
-    uint32_t* listed = ONE ? s_bits + words : a.listed;
     const int head = *a.free_head;
-    bool wrong = head < 0 || head > a.n_free;
-    if (ONE) {
-        for (int w = threadIdx.x; w < 2 * words; w += kPlanThreads) s_bits[w] = 0;
-        __syncthreads();
-#pragma unroll 4
-        for (int e = threadIdx.x; e < (int)a.entries; e += kPlanThreads) wrong |= mark_entry(a, live, e);
-        if (!wrong) {
-#pragma unroll 4
-            for (int i = head + threadIdx.x; i < a.n_free; i += kPlanThreads) wrong |= mark_listed(a, listed, i);
-        }
-        __syncthreads();
-    } else {
-        wrong |= a.plan[4] != 0;
-    }
-    for (int w = threadIdx.x; w < words; w += kPlanThreads) wrong |= (live[w] & listed[w]) != 0;
+    bool wrong = a.plan[4] != 0;
+    for (int w = threadIdx.x; w < words; w += kPlanThreads) wrong |= (a.live[w] & a.listed[w]) != 0;
     if (__syncthreads_or(wrong)) {
-        if (threadIdx.x == 0) {
-            a.plan[0] = a.plan[1] = 0;
-            a.plan[2] = PULSE_ERR_BAD_INDEX;
-            a.plan[3] = 0;
-        }
+        if (threadIdx.x == 0) write_plan(a, true, 0, 0, 0);
         return;
     }
     const int first = a.n_keep / 32 * 32;  // of the word with the first slot that is to be left
     const int moves = ranked(
-        32 * words - first, s_wave, [&](int i) { return (int)live[(first + i) >> 5]; },
+        32 * words - first, s_wave, [&](int i) { return (int)a.live[(first + i) >> 5]; },
         [&](int i, int bits) { return first + i >= a.n_keep && (bits >> (i & 31) & 1); },
         [&](int i, int, int k) {
             a.high[k] = first + i;
@@ -481,11 +466,90 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(CompactArgs 
     const int low = ranked(
         a.n_free - head, s_wave, [&](int i) { return a.free_slots[head + i]; },
         [&](int, int s) { return s < a.n_keep; }, [&](int, int s, int k) { a.low[k] = s; });
-    if (threadIdx.x == 0) {
-        a.plan[0] = moves;
-        a.plan[1] = low;
-        a.plan[2] = moves > low ? PULSE_ERR_POOL_EXHAUSTED : 0;
-        a.plan[3] = head;
+    if (threadIdx.x == 0) write_plan(a, false, moves, low, head);
+}
+
+// Marks and moves in one workgroup: table and list are loaded at once and stay in registers, the marks are bits in LDS.
+__global__ __launch_bounds__(kPlanThreads) void compact_small_kernel(CompactArgs a) {
+    constexpr int N = kOneGroup / kPlanThreads;
+    extern __shared__ uint32_t s_bits[];
+    __shared__ int s_wave[2][kPlanWaves];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int words = (a.n_slots + 31) / 32;
+    uint32_t* live = s_bits;
+    uint32_t* listed = s_bits + words;
+    const int head = *a.free_head;
+    int entry[N], slot[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int e = i * kPlanThreads + threadIdx.x, f = (wave * N + i) * 64 + lane;  // (a wave's list entries in a row)
+        entry[i] = e < (int)a.entries ? a.table[e] : -1;
+        slot[i] = f < a.n_free ? a.free_slots[f] : 0;
+    }
+    for (int w = threadIdx.x; w < 2 * words; w += kPlanThreads) s_bits[w] = 0;
+    __syncthreads();
+    bool wrong = head < 0 || head > a.n_free;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int f = (wave * N + i) * 64 + lane;
+        if (entry[i] != -1) {
+            if (entry[i] < 0 || entry[i] >= a.n_slots) wrong = true;
+            else atomicOr(live + (entry[i] >> 5), 1u << (entry[i] & 31));
+        }
+        if (f < head || f >= a.n_free) {
+            slot[i] = INT32_MAX;  // not in the list
+        } else if (slot[i] < 0 || slot[i] >= a.n_slots) {
+            wrong = true;
+        } else {
+            const uint32_t bit = 1u << (slot[i] & 31);
+            wrong |= (atomicOr(listed + (slot[i] >> 5), bit) & bit) != 0;
+        }
+    }
+    __syncthreads();
+    // live slots from n_keep on, a stretch of words a thread; free ones below it, a stretch of the list a wave
+    const int each = (words + kPlanThreads - 1) / kPlanThreads;
+    const int w0 = min(words, (int)threadIdx.x * each), w1 = min(words, w0 + each);
+    int high = 0;
+    auto bits_of = [&](int w) {
+        const uint32_t b = live[w];
+        return 32 * w >= a.n_keep ? b : 32 * w + 32 <= a.n_keep ? 0u : b & ~0u << (a.n_keep & 31);
+    };
+    for (int w = w0; w < w1; ++w) {
+        wrong |= (live[w] & listed[w]) != 0;
+        high += __popc(bits_of(w));
+    }
+    uint64_t below[N];
+    int low = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        below[i] = __ballot(slot[i] < a.n_keep);
+        low += __popcll(below[i]);
+    }
+    const int upto = (int)wave_scan((uint32_t)high, 0u, OpAdd());
+    if (lane == 63) s_wave[0][wave] = upto;
+    if (lane == 0) s_wave[1][wave] = low;
+    wrong = __syncthreads_or(wrong);
+    int h0 = upto - high, l0 = 0, moves = 0, lows = 0;
+    for (int i = 0; i < kPlanWaves; ++i) {
+        if (i < wave) {
+            h0 += s_wave[0][i];
+            l0 += s_wave[1][i];
+        }
+        moves += s_wave[0][i];
+        lows += s_wave[1][i];
+    }
+    if (threadIdx.x == 0) write_plan(a, wrong, moves, lows, head);
+    if (wrong) return;
+    for (int w = w0; w < w1; ++w)
+        for (uint32_t b = bits_of(w); b; b &= b - 1) {
+            const int x = 32 * w + __builtin_ctz(b);
+            a.high[h0] = x;
+            a.place[x] = h0++;
+        }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (slot[i] < a.n_keep) a.low[l0 + __popcll(below[i] & ((1ull << lane) - 1))] = slot[i];
+        l0 += __popcll(below[i]);
     }
 }
 
@@ -554,8 +618,10 @@ hipError_t launch_free_blocks(const int32_t* keep, int32_t B, int32_t bs, int32_
     const int64_t tiles = table_tiles(B, max_blocks);
     FreeArgs a{keep, B, bs, table, max_blocks, shared, free_slots, free_head, n_free, n_slots, status, w.slots[0], w.slots[1],
                w.tiles[0], w.tiles[1], w.few, (int32_t)tiles};
-    if ((int64_t)B * max_blocks <= kOneGroup) {
-        hipLaunchKernelGGL(free_small_kernel, dim3(1), dim3(kPlanThreads), 0, st, a);
+    const int64_t entries = (int64_t)B * max_blocks;
+    if (entries <= kOneFree) {
+        if (entries <= 2 * kPlanThreads) hipLaunchKernelGGL(free_small_kernel<2>, dim3(1), dim3(kPlanThreads), 0, st, a);
+        else hipLaunchKernelGGL(free_small_kernel<kOneFree / kPlanThreads>, dim3(1), dim3(kPlanThreads), 0, st, a);
         return hipGetLastError();
     }
     const dim3 grid((unsigned)tiles);
@@ -587,14 +653,14 @@ hipError_t launch_compact_blocks(int32_t* table, int32_t B, int32_t max_blocks, 
     const int words = (n_slots + 31) / 32;
     CompactArgs a{table, entries, n_keep, shared, free_slots, free_head, n_free, (uint8_t*)pool, n_slots, (int64_t)unit_bytes,
                   status, (uint32_t*)w.slots[0], (uint32_t*)w.slots[0] + words + 1, w.slots[1], w.slots[2], w.slots[3], w.few};
-    if (entries + n_free <= kOneGroup && 8 * (size_t)words <= 49152) {
-        hipLaunchKernelGGL(compact_plan_kernel<true>, dim3(1), dim3(kPlanThreads), 8 * (size_t)words, st, a);
+    if (entries <= kOneGroup && n_free <= kOneGroup && 8 * (size_t)words <= 49152) {
+        hipLaunchKernelGGL(compact_small_kernel, dim3(1), dim3(kPlanThreads), 8 * (size_t)words, st, a);
     } else {
         const int64_t most = entries > n_free ? entries : n_free;
         const unsigned groups = (unsigned)std::min<int64_t>(kCopyGroups, (most + kPageThreads - 1) / kPageThreads + 1);
         hipLaunchKernelGGL(compact_clear_kernel, dim3(groups), dim3(kPageThreads), 0, st, a);
         hipLaunchKernelGGL(compact_mark_kernel, dim3(groups), dim3(kPageThreads), 0, st, a);
-        hipLaunchKernelGGL(compact_plan_kernel<false>, dim3(1), dim3(kPlanThreads), 0, st, a);
+        hipLaunchKernelGGL(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a);
     }
     hipLaunchKernelGGL(compact_kernel, dim3(kCopyGroups), dim3(kPageThreads), 0, st, a);
     return hipGetLastError();
