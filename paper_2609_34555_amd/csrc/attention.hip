@@ -50,7 +50,7 @@ constexpr int kCombineThreads = kHeadDim;
 // of 64, whose shortest split is two steps, calls of few splits take 4, on
 // twice the CUs: 1.5K tokens 11.9 and 13.3, 8 of 2K (1024 splits) 14.0 and
 // 14.8, 16 of 4K 22.8 and 19.9.
-constexpr int kKv4Waves = 8;
+constexpr int kCodeWaves = 8;
 
 // Selected blocks up to which one workgroup takes a whole request and head of a 4-bit cache, so that no merge
 // launch follows: 2 to 4 steps of its waves, the more the more workgroups wait for the memory, the fewer the larger
@@ -59,24 +59,25 @@ constexpr int kKv4Waves = 8;
 //   9 requests, 8 heads of 8    13.4 12.3  12.4 12.3  13.8 13.7
 //   24 requests, 8 heads of 4   15.4 12.0  17.5 12.2  17.4 13.6
 //   8 requests, 1 head of 16    11.8 11.5  12.9 14.6  13.1 16.7
-static int32_t kv4_one_entries(const pulse_shape& s, int64_t units) {
+static int32_t one_group_entries(const pulse_shape& s, int64_t units) {
     const int steps = units > 64 ? 4 : s.num_q_heads > 8 * s.num_kv_heads ? 2 : 3;
-    return kKv4Waves * steps * kChunkTokens / s.block_size;
+    return kCodeWaves * steps * kChunkTokens / s.block_size;
 }
 
 int attn_waves(const pulse_shape& s, int32_t B, int32_t k_max) {
     if (s.num_q_heads / s.num_kv_heads <= 8) return 8;
-    if (!is_kv4(s.dtype)) return 4;
+    if (!in_codes(s.dtype)) return 4;
     const int64_t units = (int64_t)B * s.num_kv_heads;
-    const bool few = s.block_size > kChunkTokens && k_max > kv4_one_entries(s, units) &&
+    const bool few = s.block_size > kChunkTokens && k_max > one_group_entries(s, units) &&
                      units * k_max <= PULSE_ATTN_TARGET_WAVES / 2;
-    return few ? 4 : kKv4Waves;
+    return few ? 4 : kCodeWaves;
 }
 
 // Entries of one 32-token step, and of the shortest split.
 static int32_t split_step(int32_t bs) { return bs >= kChunkTokens ? 1 : kChunkTokens / bs; }
 // Two steps, one of a 4-bit cache (a quarter of the bytes, and twice the shortest split's work to share out: 64
-// requests of 80 tokens 10.1 and 9.0 us with two and one).
+// requests of 80 tokens 10.1 and 9.0 us with two and one; of an 8-bit one 32 requests of 1000 tokens, lognormal, 12.0 and
+// 13.0, 2 requests of 2000 10.9 and 9.7).
 static int32_t split_least(const pulse_shape& s) {
     const int t = (is_kv4(s.dtype) ? 1 : 2) * kChunkTokens;
     return s.block_size >= t ? 1 : t / s.block_size;
@@ -121,7 +122,7 @@ struct SplitArgs {
 //   5 requests, 3 KV heads, around 702 tokens                          11.3  12.1  10.9
 constexpr int kPlanRequests = 64;
 
-// With a 4-bit cache a step is short and a second workgroup on a CU costs more than half as much again, so its calls
+// With a 4-bit cache (and, by the same rules, an 8-bit one) a step is short and a second workgroup on a CU costs more than half as much again, so its calls
 // keep to one round more strictly.  Where all counts are k_max and the host's split takes more than a round, the
 // splits are `even`, the shortest that fit one round, unless the second workgroups are so light that even * W >
 // eps * (W + their waves).  Where the host's pieces do not fit, a plan may take up to `most` = 64 entries per wave.
@@ -132,8 +133,10 @@ constexpr int kPlanRequests = 64;
 //   11 x 4K         27.6 22.3    48 x 12K r      35.3 25.9    72 x 4K r       25.4 27.8
 //   17 x 1.5K       21.0 18.2    88 x 4K         32.8 24.6    112 x 4K r      39.6 34.7
 //   17 x 12K r      52.5 39.7    136 x 1.5K      25.2 19.9    136 x 1.5K r    47.7 27.4
-constexpr int kPlanRequestsKv4 = 256;
-constexpr int kPlanTokensKv4 = 2048;
+// An 8-bit cache, split like a 16-bit one and as it is, requests x tokens: 256 x 500 100 59, 128 x 1000 60 52, 4 x 32K over
+// one KV head of 16 28 21, 24 x 4K r 56 53; 16 x 2K r 23.2 23.8, 64 x 2000 51.6 52.3.
+constexpr int kPlanRequestsCodes = 256;
+constexpr int kPlanTokensCodes = 2048;
 // More requests and heads than a round has workgroups: from 4K tokens on the grid has two workgroups for each, for a
 // plan to share out.  Equal counts leave the second without work, and so do, where the last round is as good as full,
 // counts of three quarters of k_max on average.  In us, one workgroup each and this (8 KV heads; 2 from 132 requests):
@@ -674,6 +677,13 @@ __device__ inline void attend_split_kv4(const uint16_t* __restrict__ q, const ui
 // tokens of 8 channels; a block has one scale for its keys and one for its values, so both are decoded with it, exactly,
 // into the operands of the products: keys into the type of the queries, values into bf16, so that the probabilities can
 // be cut into three bf16 parts, all 24 bits of them (as in attend_split_kv4).
+//
+// Bound: HBM, 256 bytes per token and KV head, once enough steps are in flight: 32 requests of 4K tokens, 8 heads (268 MB)
+// 53 us (5.1 TB/s; 46 at what streaming reads reach); short calls are the launch, the look-ups and the waves' merge (7 us
+// for 400 tokens).  A step's loads are issued together and the other waves hide them: 120 VGPRs, so two workgroups a CU;
+// with the next step loaded ahead (180 VGPRs) the long calls are 0 to 1% faster and those of many workgroups slower
+// (128 requests of 1000 tokens 60 and 82 us, 256 of 500 100 and 144).  Values loaded behind the logits instead of with the
+// keys: equal.
 template <int DT, int BS>
 __device__ inline void attend_split_kv8(const uint16_t* __restrict__ q, const uint8_t* __restrict__ pool,
                                         int32_t n_slots, const int32_t* __restrict__ table, int32_t max_blocks,
@@ -742,13 +752,11 @@ __device__ inline void attend_split_kv8(const uint16_t* __restrict__ q, const ui
 #pragma unroll
         for (int n = 0; n < 4; ++n) vw[n] = reinterpret_cast<const u32x4*>(vb)[n];
     };
-    load_k(0);
-    load_v(0);
 #pragma unroll 1
     for (int i = 0; i < steps; ++i) {
-        u32x4 vn[4];
-#pragma unroll
-        for (int n = 0; n < 4; ++n) vn[n] = vw[n];
+        load_k(i);
+        load_v(i);
+        u32x4 (&vn)[4] = vw;
         const int e0 = i / kHalves * kPer;
         const float ks = kv8_pow2((int)(__shfl((int)my_scales, e0 + k_tok / BS) & 255) - 127);
         float vs = kv8_pow2((__shfl((int)my_scales, e0 + v_tok / BS) >> 8) - 127);
@@ -761,10 +769,6 @@ __device__ inline void attend_split_kv8(const uint16_t* __restrict__ q, const ui
                 const u32x2 w = {kw[sub][kc / 2][2 * (kc % 2)], kw[sub][kc / 2][2 * (kc % 2) + 1]};
                 s[sub] = MQ::mac(kv8_decode8<ET>(w, ks), qb[kc], s[sub]);
             }
-        if (i + 1 < steps) {
-            load_k(i + 1);
-            load_v(i + 1);
-        }
         float x[8];
 #pragma unroll
         for (int n = 0; n < 8; ++n) x[n] = s[n / 4][n % 4] * scale_log2;
@@ -855,7 +859,7 @@ __global__ __launch_bounds__(W * kWave) void attn_splitk_kernel(
     Piece p;
     p.r = sp.light_last ? blockIdx.y : blockIdx.z;
     p.wg = sp.light_last ? blockIdx.z : blockIdx.y;
-    p.eps = is_kv4(DT) ? sp.even : sp.eps;
+    p.eps = in_codes(DT) ? sp.even : sp.eps;
     int piece = p.r * sp.n_wg + p.wg;
     const bool planned = sp.planned;
     auto load_j = [&]() {
@@ -871,10 +875,10 @@ __global__ __launch_bounds__(W * kWave) void attn_splitk_kernel(
             lane == 0)
             report(status, PULSE_ERR_BAD_INDEX);
         p.cnt = k_max;
-        p.nwg = is_kv4(DT) ? sp.n_even : sp.n_wg;
+        p.nwg = in_codes(DT) ? sp.n_even : sp.n_wg;
         if (counts.equal(B, k_max, lane)) {
-            if (is_kv4(DT) && p.wg >= p.nwg) return;
-        } else if (is_kv4(DT) && (!sp.share || (sp.level && counts.level(B, k_max)))) {
+            if (in_codes(DT) && p.wg >= p.nwg) return;
+        } else if (in_codes(DT) && (!sp.share || (sp.level && counts.level(B, k_max)))) {
             own = true;
             if (sp.share) own_eps = sp.even;
         } else {
@@ -887,7 +891,7 @@ __global__ __launch_bounds__(W * kWave) void attn_splitk_kernel(
     }
     if (own) {
         p.cnt = sel_cnt[p.r];
-        if (is_kv4(DT) && p.eps != own_eps) {
+        if (in_codes(DT) && p.eps != own_eps) {
             p.eps = own_eps;
             j_lane = load_j();
         }
@@ -1058,8 +1062,8 @@ __global__ __launch_bounds__(kCombineThreads) void attn_combine_kernel(
 }
 
 // Whether requests and heads alone are more than a round of workgroups, and few enough for a plan.
-static bool kv4_over(const pulse_shape& s, int32_t B) {
-    return is_kv4(s.dtype) && B <= kPlanRequestsKv4 && B > PULSE_ATTN_TARGET_WAVES / (kKv4Waves * s.num_kv_heads);
+static bool over_a_round(const pulse_shape& s, int32_t B) {
+    return in_codes(s.dtype) && B <= kPlanRequestsCodes && B > PULSE_ATTN_TARGET_WAVES / (kCodeWaves * s.num_kv_heads);
 }
 
 AttnPlan attn_plan(const pulse_shape& s, int32_t B, int32_t k_max) {
@@ -1072,14 +1076,14 @@ AttnPlan attn_plan(const pulse_shape& s, int32_t B, int32_t k_max) {
     int64_t max_split = (k_max + min_entries - 1) / min_entries;
     if (want > max_split) want = max_split;
     if (want < 1) want = 1;
-    if (is_kv4(s.dtype)) {
+    if (in_codes(s.dtype)) {
         // All waves of a workgroup have work, however many requests there are: the CU's other workgroups do not make
         // up for idle waves.  1000 tokens of 8 heads, in us, one round of waves and this: 64 requests 20.8 and 22.6
         // (lognormal 41.3 and 34.7), 96 32.7 and 29.4, 128 49.8 and 36.5, 256 143 and 69.
-        want = std::max(want, std::min<int64_t>(max_split, kKv4Waves));
-        if (want > kKv4Waves && k_max <= kv4_one_entries(s, units)) want = kKv4Waves;
-        if (kv4_over(s, B) && (int64_t)k_max * s.block_size >= kOverTokens)
-            want = std::max<int64_t>(want, 2 * kKv4Waves);
+        want = std::max(want, std::min<int64_t>(max_split, kCodeWaves));
+        if (want > kCodeWaves && k_max <= one_group_entries(s, units)) want = kCodeWaves;
+        if (over_a_round(s, B) && (int64_t)k_max * s.block_size >= kOverTokens)
+            want = std::max<int64_t>(want, 2 * kCodeWaves);
     }
     int64_t eps = (k_max + want - 1) / want;
     eps = ((eps + step - 1) / step) * step;
@@ -1102,12 +1106,12 @@ int64_t attn_partials(const pulse_shape& s, int32_t B, int32_t k_max) {
 // each request and head more, or those of 64 entries, each request and head's last workgroup not full; and the second
 // workgroups of a plan beyond a round.
 int64_t attn_partials_most(const pulse_shape& s, int32_t B, int32_t k_max) {
-    const bool kv4 = is_kv4(s.dtype);
+    const bool kv4 = in_codes(s.dtype);
     const int64_t W = s.num_q_heads / s.num_kv_heads <= 8 || kv4 ? 8 : 4;
     const int64_t units = (int64_t)B * s.num_kv_heads, least = split_least(s);
     const int64_t shortest = units * (((k_max + least - 1) / least + 3) / 4);
     const int64_t splits = std::max(PULSE_ATTN_TARGET_WAVES + units, units * (((int64_t)k_max + 63) / 64));
-    const int64_t second = kv4 ? std::min<int64_t>(units, (int64_t)kPlanRequestsKv4 * s.num_kv_heads) : 0;
+    const int64_t second = kv4 ? std::min<int64_t>(units, (int64_t)kPlanRequestsCodes * s.num_kv_heads) : 0;
     return std::min(std::max(shortest, units), splits / W + units + second);
 }
 
@@ -1118,7 +1122,7 @@ static void launch_attn_t(dim3 grid, size_t lds, hipStream_t st, hipEvent_t done
                           const int32_t* sel_cnt, int32_t k_max, const int32_t* ctx_len, int32_t B, int32_t Hq,
                           int32_t Hkv, int32_t G, const SplitArgs& sp, float scale_log2, float* ws_o, float2* ws_ml,
                           float* out, float* lse, __bf16* x, int32_t* status) {
-    constexpr int kMany = is_kv4(DT) ? kPlanRequestsKv4 / kWave : 1;
+    constexpr int kMany = in_codes(DT) ? kPlanRequestsCodes / kWave : 1;
     const auto kernel =
         B <= kPlanRequests ? attn_splitk_kernel<DT, BS, W, GP, 1> : attn_splitk_kernel<DT, BS, W, GP, kMany>;
     launch_timed(kernel, grid, dim3(W * kWave), (uint32_t)lds, st, nullptr, done,
@@ -1148,12 +1152,12 @@ hipError_t launch_attention(const pulse_shape& s, const void* q, const void* poo
     sp.n_even = n_wg;
     sp.most = sp.eps;
     sp.level = false;
-    if (is_kv4(s.dtype)) {
+    if (in_codes(s.dtype)) {
         sp.most = 64;
-        const bool over = kv4_over(s, B);
+        const bool over = over_a_round(s, B);
         sp.level = over && 4 * (int64_t)((B + round - 1) / std::max(round, 1)) * round <= 5 * (int64_t)B;
         // workgroups of a request in one round
-        const int32_t each = over ? 1 : B <= kPlanRequestsKv4 ? round / B : 0;
+        const int32_t each = over ? 1 : B <= kPlanRequestsCodes ? round / B : 0;
         if (each >= 1 && n_wg > each) {
             const int64_t eps = ((int64_t)k_max + W * each - 1) / (W * each);
             const int32_t even = (int32_t)std::min<int64_t>((eps + sp.step - 1) / sp.step * sp.step, sp.most);
@@ -1164,9 +1168,9 @@ hipError_t launch_attention(const pulse_shape& s, const void* q, const void* poo
             }
         }
     }
-    sp.share = B <= kPlanRequests || (int64_t)k_max * s.block_size >= kPlanTokensKv4;
+    sp.share = B <= kPlanRequests || (int64_t)k_max * s.block_size >= kPlanTokensCodes;
     if (B <= kPlanRequests) sp.planned = sp.eps >= 2 * sp.least || all > round;
-    else sp.planned = is_kv4(s.dtype) && B <= kPlanRequestsKv4 && (sp.share || sp.even != sp.eps);
+    else sp.planned = in_codes(s.dtype) && B <= kPlanRequestsCodes && (sp.share || sp.even != sp.eps);
     sp.planned = sp.planned && n_wg > 1 && k_max <= (1 << 22);
     sp.light_last = (p.n_split % W != 0 || sp.even != sp.eps) && all > round && n_wg <= 65535;
     const dim3 grid = sp.light_last ? dim3((unsigned)Hkv, (unsigned)B, (unsigned)n_wg)
@@ -1185,24 +1189,28 @@ hipError_t launch_attention(const pulse_shape& s, const void* q, const void* poo
     else if (G <= 8) PULSE_ATTN(DT, BS, 8, 8); \
     else if (W == 8) PULSE_ATTN(DT, BS, 8, 16); \
     else PULSE_ATTN(DT, 64, 4, 16)
+#define PULSE_ATTN_KV8(DT, BS)                \
+    if (W == 8) PULSE_ATTN(DT, BS, 8, 16);    \
+    else PULSE_ATTN(DT, 64, 4, 16)
 #define PULSE_ATTN_BS(WHICH, DT)                   \
     if (s.block_size == 16) { WHICH(DT, 16); }      \
     else if (s.block_size == 32) { WHICH(DT, 32); } \
     else { WHICH(DT, 64); }
     if (s.dtype == PULSE_BF16) { PULSE_ATTN_BS(PULSE_ATTN_W, PULSE_BF16) }
     else if (s.dtype == PULSE_F16) { PULSE_ATTN_BS(PULSE_ATTN_W, PULSE_F16) }
-    else if (s.dtype == PULSE_BF16_KV8) { PULSE_ATTN_BS(PULSE_ATTN_W, PULSE_BF16_KV8) }
-    else if (s.dtype == PULSE_F16_KV8) { PULSE_ATTN_BS(PULSE_ATTN_W, PULSE_F16_KV8) }
+    else if (s.dtype == PULSE_BF16_KV8) { PULSE_ATTN_BS(PULSE_ATTN_KV8, PULSE_BF16_KV8) }
+    else if (s.dtype == PULSE_F16_KV8) { PULSE_ATTN_BS(PULSE_ATTN_KV8, PULSE_F16_KV8) }
     else if (s.dtype == PULSE_BF16_KV4) { PULSE_ATTN_BS(PULSE_ATTN_KV4, PULSE_BF16_KV4) }
     else { PULSE_ATTN_BS(PULSE_ATTN_KV4, PULSE_F16_KV4) }
 #undef PULSE_ATTN_BS
+#undef PULSE_ATTN_KV8
 #undef PULSE_ATTN_KV4
 #undef PULSE_ATTN_W
 #undef PULSE_ATTN
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (n_wg <= 1) return (done && split_done) ? hipEventRecord(done, st) : hipSuccess;
-    const auto combine = B <= kPlanRequests ? attn_combine_kernel<1> : attn_combine_kernel<kPlanRequestsKv4 / kWave>;
+    const auto combine = B <= kPlanRequests ? attn_combine_kernel<1> : attn_combine_kernel<kPlanRequestsCodes / kWave>;
     launch_timed(combine, dim3((unsigned)G, (unsigned)Hkv, (unsigned)B), dim3(kCombineThreads), 0u, st, nullptr, done,
                  (const float*)ws_o, (const float2*)ws_ml, sel_cnt, k_max, B, Hq, Hkv, G, sp, W, out, lse, x);
     return hipGetLastError();

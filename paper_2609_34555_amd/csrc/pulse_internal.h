@@ -33,8 +33,9 @@ __host__ __device__ constexpr int elem_type(int dtype) {
 }
 __host__ __device__ constexpr bool is_kv4(int dtype) { return dtype == PULSE_F16_KV4 || dtype == PULSE_BF16_KV4; }
 __host__ __device__ constexpr bool is_kv8(int dtype) { return dtype == PULSE_F16_KV8 || dtype == PULSE_BF16_KV8; }
-// Bits of a cached element.
+// Bits of a cached element; whether it is a code under a scale.
 __host__ __device__ constexpr int kv_bits(int dtype) { return is_kv4(dtype) ? 4 : is_kv8(dtype) ? 8 : 16; }
+__host__ __device__ constexpr bool in_codes(int dtype) { return kv_bits(dtype) != 16; }
 
 // ---- timed launches ---------------------------------------------------------
 
