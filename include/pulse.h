@@ -78,7 +78,8 @@
  * pulse_recall_gather, pulse_release_recalled, pulse_sparse_decode_attn,
  * pulse_attention_workgroups, pulse_decode_layer(_noalloc), the offload layers
  * (without an engine) and the normal layers of pulse_irq_step,
- * pulse_build_tables, pulse_qk_norm_rope, pulse_append_kv and pulse_load_kv.
+ * pulse_build_tables, pulse_qk_norm_rope, pulse_append_kv, pulse_load_kv,
+ * pulse_prompt_attn and the calls on pages.
  * The others return what they return for a dtype that they do not know.
  */
 #ifndef PULSE_H
@@ -637,7 +638,9 @@ PULSE_API pulse_status pulse_load_kv(const pulse_shape* shape, const void* slot_
  *   lse[row][hq] = log sum_t exp(logit_t)           (fp32, optional)
  * so the new tokens' own keys and values are in the cache before the call
  * (pulse_append_kv).  The cache may be in 16, 8 or 4 bits.  Products and sums in
- * fp32; probabilities are rounded to the 16-bit type before they meet V.
+ * fp32; probabilities are rounded to the 16-bit type before they meet V.  Keys of
+ * tokens behind p count nothing whatever they are, values as long as they are
+ * finite; what lies behind the context's end may be anything.
  *   q            device rows of 16-bit elements, row i at i * q_stride elements,
  *                its heads one after another (out: the same at out_stride)
  *   tok_off      device int32 [B+1];  ctx_len  device int32 [B]
@@ -656,7 +659,7 @@ PULSE_API pulse_status pulse_load_kv(const pulse_shape* shape, const void* slot_
  * repeats its bits.
  * out must overlap no input.  q, out and the pool are 16-byte aligned, strides
  * multiples of 8 that hold the heads (else PULSE_ERR_INVALID_ARG); B <= 4096 and
- * max_tokens * G < 2^28 (else PULSE_ERR_UNSUPPORTED).
+ * max_tokens * G < 2^28 and max_tokens * Hq < 2^31 (else PULSE_ERR_UNSUPPORTED).
  */
 PULSE_API size_t pulse_prompt_workspace_bytes(const pulse_shape* shape, int32_t B, int64_t max_tokens,
                                               int32_t max_blocks);

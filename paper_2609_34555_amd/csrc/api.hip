@@ -565,7 +565,7 @@ pulse_status pulse_load_kv(const pulse_shape* shape, const void* slot_pool, int3
 }
 
 static bool prompt_fits(const pulse_shape& s, int64_t max_tokens) {
-    return max_tokens * (s.num_q_heads / s.num_kv_heads) < kMaxPromptRows;
+    return max_tokens * (s.num_q_heads / s.num_kv_heads) < kMaxPromptRows && max_tokens * s.num_q_heads <= INT32_MAX;
 }
 
 size_t pulse_prompt_workspace_bytes(const pulse_shape* shape, int32_t B, int64_t max_tokens, int32_t max_blocks) {

@@ -959,9 +959,23 @@ struct PromptPlan {
 
 constexpr int kSplitGroups = 512;  // workgroups aimed at where few rows are split over the context: two a CU
 constexpr int kLeastTiles = 4;     // tiles of keys of a split
-// Rows of a request, on average, up to which prompt_few_kernel takes them, 32 to a workgroup: beyond 32 every workgroup
-// reads the keys again, which costs the 16-bit cache more than the decoding of codes that 128 rows share saves the others.
-static int64_t few_rows(const pulse_shape& s) { return kv_bits(s.dtype) == 16 ? 32 : 64; }
+// prompt_few_kernel takes 32 rows to a workgroup, so every 32 rows read the keys again.  It is for
+// - few rows of long contexts: up to 32 of a request on average, 64 over a cache of codes (beyond, that reading costs the
+//   16-bit cache more than the decoding of codes that 128 rows share saves the others), and
+// - few workgroups: up to 256, which leave CUs to share out the keys of a workgroup of 128, or 512 unless prompts are so
+//   short that a workgroup is mostly its start; over a cache of codes, whose decoding is then shared out too, 512 and 1152.
+// In us, 128 rows and 32, 16-bit and 8-bit cache, query heads / KV heads:
+//   1 x 256    32/8    9.7   8.3    11.4   7.7      1 x 512    32/8   18.7  14.8    21.3  11.8
+//   1 x 1024   32/8   29.3  31.8    32.3  26.3      1 x 1000   16/2   24.7  21.6    25.5  16.0
+//   1 x 3000   12/1   63.1  72.5    81.9  53.2      8 x 100    32/8    8.7  13.6     9.7  13.1
+//   16 x 5 of 32K     366   369     246   193       16 x 16 of 32K    378   565     303   273
+//   1 x 200    64/8    9.6  10.4 (16 bits, blocks of 32)
+static bool few_rows(const pulse_shape& s, int32_t B, int64_t max_tokens) {
+    const int64_t rows = max_tokens * (s.num_q_heads / s.num_kv_heads), groups = (rows + 31) / 32 * s.num_kv_heads;
+    const bool codes = in_codes(s.dtype);
+    const int64_t few = codes ? 512 : 256, some = codes ? 1152 : 512;
+    return rows <= (codes ? 64 : 32) * (int64_t)B || groups <= few || (groups <= some && max_tokens >= 256 * (int64_t)B);
+}
 // Workgroups of eight waves, which stage and decode a tile for twice the rows, from two rounds of them and 2048 new tokens
 // of a request on: below, the rows behind the diagonal that the larger tile multiplies in vain cost more.  In us, four
 // waves and eight, 32 query heads over 8 KV heads, 16-bit and 8-bit cache:
@@ -980,7 +994,7 @@ static PromptPlan prompt_plan(const pulse_shape& s, int32_t B, int64_t max_token
     const int64_t G = s.num_q_heads / s.num_kv_heads;
     const int64_t all = max_tokens * G;
     p.rows = kWaves * kRowsPerWave;
-    if (all <= few_rows(s) * B) p.rows = 32;
+    if (few_rows(s, B, max_tokens)) p.rows = 32;
     else if (max_tokens >= (int64_t)kLongPrompt * B && all * s.num_kv_heads >= (int64_t)kLongGroups * 2 * p.rows) p.rows *= 2;
     const int64_t rows = p.rows;
     p.n_tiles = (int)(all / rows + B);

@@ -161,6 +161,11 @@ CASES = [
     ([1800, 2048], [600, 500], 4, 1, 16, "bf16"),                # a part of a prompt
     ([60] * 70, None, 2, 2, 16, "bf16"),                          # many short ones
     ([40 + 3 * i for i in range(100)], [1 + i % 9 for i in range(100)], 5, 1, 32, "f16"),
+    # 32 rows a workgroup by the number of workgroups, a request of many rows among requests of few; more than that
+    ([700], None, 8, 2, 32, "f16"),
+    ([900, 30, 2000, 1], [200, 2, 3, 1], 8, 1, 16, "bf16"),
+    ([260, 300, 280], None, 32, 8, 16, "bf16"),
+    ([2000, 40, 1999], [64, 64 - 24, 64], 24, 8, 64, "f16"),
 ]
 
 
@@ -289,6 +294,67 @@ def test_large_logits_and_constant_rows(bits):
     c.check(out, lse)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("T", [96, 5])
+def test_captured_calls_replay_as_eager(T, bits):
+    """A padded step in a graph, replayed on other lengths, contexts and queries, with eager work between; few rows and a
+    split over the context (T = 5) and more."""
+    c = Case([1500, 700, 900], [T // 3, T // 3, T - 2 * (T // 3)], 8, 2, 16, "bf16", bits, 12, pad=4)
+    d, st = c.d, dev([0])
+    nb = P.pulse_prompt_workspace_bytes(c.sh, 3, c.T, c.mb)
+    bufs = [dict(out=torch.zeros((c.T, c.stride), device=DEV, dtype=c.dtype), lse=torch.zeros((c.T, c.hq), device=DEV),
+                 ws=torch.full((nb,), 255, dtype=torch.uint8, device=DEV)) for _ in range(2)]
+
+    def call(b):
+        P.pulse_prompt_attn(c.sh, d["q"], c.stride, d["off"], c.T, d["ctx"], 3, d["pool"], c.pool.shape[0], d["table"], c.mb,
+                            SCALE, b["out"], c.stride, b["lse"], st, b["ws"], nb)
+
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        call(bufs[0])
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        call(bufs[0])
+    for i, new in enumerate(([T, 0, 0], [1, 1, 1], [0, 2, T - 2], [T // 3] * 3)):
+        d["off"].copy_(dev(np.concatenate([[0], np.cumsum(new)])))
+        d["ctx"].copy_(dev([1500 - i, 700 - 7 * i, 900]))
+        d["q"].mul_(-1)
+        for b in bufs:
+            b["out"].fill_(3)
+            b["lse"].fill_(3)
+        g.replay()
+        call(bufs[1])
+        torch.cuda.synchronize()
+        assert torch.equal(bufs[0]["out"], bufs[1]["out"]) and torch.equal(bufs[0]["lse"], bufs[1]["lse"]), i
+        n = sum(new)
+        assert (bufs[0]["out"][n:] == 3).all() and (bufs[0]["out"][:n, : c.hq * D] != 3).any() and st.item() == 0
+
+
+@pytest.mark.gpu
+def test_two_calls_at_once():
+    """Calls on two streams with workspaces of their own give what they give alone."""
+    cases = [Case([5000, 3000], [7, 2], 16, 4, 64, "bf16", 8, 13), Case([300, 900], [300, 900], 8, 2, 16, "f16", 16, 14)]
+    alone = [c.run() for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    sizes = [P.pulse_prompt_workspace_bytes(c.sh, c.B, c.T, c.mb) for c in cases]
+    got = [dict(ws=torch.full((sizes[i % 2],), 255, dtype=torch.uint8, device=DEV), st=dev([0]),
+                out=torch.full_like(alone[i % 2][0], 3), lse=torch.full_like(alone[i % 2][1], 3)) for i in range(6)]
+    torch.cuda.synchronize()
+    for i, b in enumerate(got):
+        c = cases[i % 2]
+        P.pulse_prompt_attn(c.sh, c.d["q"], c.stride, c.d["off"], c.T, c.d["ctx"], c.B, c.d["pool"], c.pool.shape[0],
+                            c.d["table"], c.mb, SCALE, b["out"], c.stride, b["lse"], b["st"], b["ws"], sizes[i % 2],
+                            stream=streams[i % 2])
+    torch.cuda.synchronize()
+    for i, b in enumerate(got):
+        out, lse = alone[i % 2]
+        assert b["st"].item() == 0 and torch.equal(b["out"], out) and torch.equal(b["lse"], lse)
+
+
 def test_prompt_refusals():
     sh = P.make_shape(32, 8, D, 16, P.PULSE_BF16)
     a = dict(q=FAKE, q_stride=4096, tok_off=FAKE, max_tokens=100, ctx_len=FAKE, B=2, slot_pool=FAKE, n_slots=50,
@@ -308,6 +374,8 @@ def test_prompt_refusals():
         assert call(**kw) == P.PULSE_ERR_UNSUPPORTED, kw
     assert call(P.make_shape(32, 8, 64, 16, P.PULSE_BF16)) == P.PULSE_ERR_UNSUPPORTED
     assert call(P.make_shape(32, 8, D, 16, 7)) == P.PULSE_ERR_UNSUPPORTED
+    assert call(P.make_shape(64, 64, D, 16, P.PULSE_BF16), q_stride=8192, out_stride=8192,
+                max_tokens=1 << 25) == P.PULSE_ERR_UNSUPPORTED
     assert call(B=0, q=None) == P.PULSE_OK and call(max_tokens=0, q=None) == P.PULSE_OK
     assert P.pulse_prompt_workspace_bytes(sh, 2, 1 << 26, 8) == 0 and P.pulse_prompt_workspace_bytes(sh, -1, 5, 8) == 0
     assert P.pulse_prompt_workspace_bytes(sh, 2, 100, 8) > 0
