@@ -650,16 +650,16 @@ PULSE_API pulse_status pulse_load_kv(const pulse_shape* shape, const void* slot_
  *   ws           pulse_prompt_workspace_bytes() bytes of device memory; one of that
  *                size serves any call with the same or smaller B, max_tokens and
  *                max_blocks
- * PULSE_ERR_BAD_INDEX if a request's offsets are out of order or outside
- * [0, max_tokens] (its rows are then undefined), if ctx_len[r] is less than its
- * new tokens or more than max_blocks blocks (its rows get out = 0, lse = -inf), or
+ * PULSE_ERR_BAD_INDEX if offsets are out of order or outside [0, max_tokens] (the
+ * rows of any request are then undefined), if ctx_len[r] is less than r's new tokens or more than max_blocks blocks (its rows get out = 0, lse = -inf), or
  * if a block of the context has no slot (its tokens count nothing; a row without
  * any gets out = 0, lse = -inf).  The order of a row's sums depends on the shape, B,
  * max_tokens, max_blocks and the request's own lengths and offset; the same call
  * repeats its bits.
  * out must overlap no input.  q, out and the pool are 16-byte aligned, strides
- * multiples of 8 that hold the heads (else PULSE_ERR_INVALID_ARG); B <= 4096 and
- * max_tokens * G < 2^28 and max_tokens * Hq < 2^31 (else PULSE_ERR_UNSUPPORTED).
+ * multiples of 8 that hold the heads (else PULSE_ERR_INVALID_ARG); B <= 4096,
+ * Hkv <= 1024, max_tokens * G < 2^28 and max_tokens * Hq < 2^30 (else
+ * PULSE_ERR_UNSUPPORTED).
  */
 PULSE_API size_t pulse_prompt_workspace_bytes(const pulse_shape* shape, int32_t B, int64_t max_tokens,
                                               int32_t max_blocks);

@@ -564,8 +564,10 @@ pulse_status pulse_load_kv(const pulse_shape* shape, const void* slot_pool, int3
                                      dev_status, (hipStream_t)stream));
 }
 
+// Rows of a KV head, divided by G in 32 bits, and of all heads, whose workgroups a launch can hold.
 static bool prompt_fits(const pulse_shape& s, int64_t max_tokens) {
-    return max_tokens * (s.num_q_heads / s.num_kv_heads) < kMaxPromptRows && max_tokens * s.num_q_heads <= INT32_MAX;
+    return s.num_kv_heads <= 1024 && max_tokens * (s.num_q_heads / s.num_kv_heads) < kMaxPromptRows &&
+           max_tokens * s.num_q_heads < kMaxPromptRows * 4;
 }
 
 size_t pulse_prompt_workspace_bytes(const pulse_shape* shape, int32_t B, int64_t max_tokens, int32_t max_blocks) {

@@ -13,7 +13,7 @@
 // transposed.
 //
 // Precision: products of 16-bit factors, exact, summed in fp32; maxima, sums and rescaling in fp32.  Probabilities are
-// rounded to the 16-bit type for the second product (half a step of it, at random, beside half a step of the output's own
+// rounded to the 16-bit type for the second product (half a step of it at most, beside half a step of the output's own
 // rounding to the same type); their sum is that of the values before rounding.
 #include <algorithm>
 #include <type_traits>
@@ -29,6 +29,12 @@ constexpr int kKeys = 64;                     // keys of a tile
 constexpr int kRowsPerWave = 32;
 constexpr int kWaves = 4;                     // of a workgroup; twice as many for long prompts
 constexpr int kTileBytes = kKeys * kHeadDim * 2;  // of keys, and of values, in LDS
+
+// What is subtracted from logits (base 2) is their maximum less this.  In fp16, whose normal numbers end at 2^-14,
+// probabilities of up to 2^(7 + 8) (see `prepare`), so that those of 2^-21 and more keep all their bits, and what tens of
+// thousands of smaller ones lose together stays below 2^-16.
+template <int ET>
+constexpr float kLift = ET == PULSE_F16 ? 7.f : 0.f;
 
 template <int ET>
 __device__ inline f32x16 mac32(typename Mfma<ET>::vec a, typename Mfma<ET>::vec b, f32x16 c) {
@@ -79,6 +85,7 @@ struct PromptArgs {
     int32_t n_slots;
     const int32_t* table;
     int32_t max_blocks;
+    int32_t max_ctx;        // tokens of max_blocks blocks
     int32_t Hkv, G;
     uint64_t g_magic;       // m / G = m * g_magic >> 32 for rows m below 2^28
     float scale_log2;
@@ -121,7 +128,7 @@ struct Request {
     int t0, ctx, base;  // its first row, its tokens, the tokens before its first new one
     int64_t n_rows, row0;
 };
-__device__ inline Request look_at(const PromptArgs& a, const Place& pl, int rows, int bs, int threads) {
+__device__ inline Request look_at(const PromptArgs& a, const Place& pl, int rows, int threads) {
     Request q;
     q.t0 = a.tok_off[pl.r];
     const int t1 = a.tok_off[pl.r + 1];
@@ -129,7 +136,7 @@ __device__ inline Request look_at(const PromptArgs& a, const Place& pl, int rows
     if (blockIdx.x == 0) {
         for (int r = threadIdx.x; r < a.B; r += threads) {
             const int64_t x = a.tok_off[r], y = a.tok_off[r + 1], c = a.ctx_len[r];
-            if (x < 0 || y < x || y > a.max_tokens || c < y - x || c > (int64_t)a.max_blocks * bs)
+            if (x < 0 || y < x || y > a.max_tokens || c < y - x || c > a.max_ctx)
                 report(a.status, PULSE_ERR_BAD_INDEX);
         }
     }
@@ -137,7 +144,7 @@ __device__ inline Request look_at(const PromptArgs& a, const Place& pl, int rows
     q.n_rows = (int64_t)fresh * a.G;
     q.row0 = (int64_t)pl.tile * rows;
     q.any = !(q.t0 < 0 || t1 < q.t0 || t1 > a.max_tokens) && !(pl.tile < 0 || q.row0 >= q.n_rows);
-    q.ok = q.ctx >= fresh && q.ctx <= (int64_t)a.max_blocks * bs;
+    q.ok = q.ctx >= fresh && q.ctx <= a.max_ctx;
     q.base = q.ctx - fresh;
     return q;
 }
@@ -296,7 +303,7 @@ __global__ __launch_bounds__(W * kWave, 2) void prompt_kernel(PromptArgs a) {
     const int rest = blockIdx.x / a.Hkv;
     const int split = rest % a.n_split;
     const Place pl = find_place(a.tok_off, a.B, a.G, kRows, a.n_tiles - 1 - rest / a.n_split);
-    const Request rq = look_at(a, pl, kRows, BS, W * kWave);
+    const Request rq = look_at(a, pl, kRows, W * kWave);
     if (!rq.any) return;
     const bool ok = rq.ok;
     const int t0 = rq.t0, ctx = rq.ctx, base = rq.base;
@@ -528,7 +535,7 @@ __global__ __launch_bounds__(W * kWave, 2) void prompt_kernel(PromptArgs a) {
         {
             const uint32_t u = __float_as_uint(cm);
             const u32x2 w = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-            cm = __builtin_elementwise_maximum(__uint_as_float(w[0]), __uint_as_float(w[1])) * scale;
+            cm = fmaf(__builtin_elementwise_maximum(__uint_as_float(w[0]), __uint_as_float(w[1])), scale, -kLift<ET>);
         }
         // The maximum that is subtracted follows the rows' own only when one of the wave's has left it 2^8 behind:
         // until then probabilities and sums grow by up to that factor and keep their relative accuracy.
@@ -703,7 +710,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void prompt_few_kernel(PromptArg
     const int rest = blockIdx.x / a.Hkv;
     const int split = rest % a.n_split;
     const Place pl = find_place(a.tok_off, a.B, a.G, kRows, a.n_tiles - 1 - rest / a.n_split);
-    const Request q = look_at(a, pl, kRows, BS, W * kWave);
+    const Request q = look_at(a, pl, kRows, W * kWave);
     if (!q.any) return;
     const int64_t m = q.row0 + col;
     const bool live = m < q.n_rows;
@@ -785,7 +792,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void prompt_few_kernel(PromptArg
         for (int n = 1; n < 16; ++n) cm = __builtin_elementwise_maximum(cm, s[n]);
         const uint32_t u = __float_as_uint(cm);
         const u32x2 w = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-        cm = __builtin_elementwise_maximum(__uint_as_float(w[0]), __uint_as_float(w[1])) * scale;
+        cm = fmaf(__builtin_elementwise_maximum(__uint_as_float(w[0]), __uint_as_float(w[1])), scale, -kLift<ET>);
         if (__ballot(!(cm <= m_run + 8.f))) {  // (as in prompt_kernel)
             const float m_new = __builtin_elementwise_maximum(m_run, cm);
             const float alpha = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
@@ -876,8 +883,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void prompt_few_kernel(PromptArg
 
 // Joins the splits of the rows: 32 threads, four channels each, take a row and `STRIDE`th splits of it, four of which are
 // loaded before any is used; a workgroup holds eight rows, or (many splits: STRIDE 8) eight shares of one row, which it adds
-// up in LDS.  (Loaded
-// one after another, 64 splits took 45 us more: 5 tokens at the end of 64K, 4 bits, 69 and 24 us.)
+// up in LDS.  (Loaded one after another, 64 splits took 45 us more: 5 tokens at the end of 64K, 4 bits, 69 and 24 us.)
 constexpr int kManySplits = 8;  // above it, a workgroup a row
 
 template <int ET, int STRIDE>
@@ -888,8 +894,8 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
     const int64_t rows = (int64_t)a.max_tokens * Hq;
     const int part = threadIdx.x >> 5, c4 = threadIdx.x & 31;
     const int64_t at = STRIDE == 1 ? (int64_t)blockIdx.x * 8 + part : (int64_t)blockIdx.x;
-    const int last = a.tok_off[a.B];
-    const bool any = at < (int64_t)last * Hq && last <= a.max_tokens;
+    const int first = a.tok_off[0], last = a.tok_off[a.B];
+    const bool any = at >= (int64_t)first * Hq && at < (int64_t)last * Hq && last <= a.max_tokens;
     if (STRIDE > 1 && !any) return;
     float top = -INFINITY, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -1037,7 +1043,7 @@ hipError_t launch_prompt_attn(const pulse_shape& s, const void* q, int64_t q_str
     const PromptPlan p = prompt_plan(s, B, max_tokens, max_blocks);
     const int32_t G = s.num_q_heads / s.num_kv_heads;
     PromptArgs a{(const uint16_t*)q, q_stride, tok_off, ctx_len, B, (int32_t)max_tokens, (const uint8_t*)pool, n_slots, table,
-                 max_blocks, s.num_kv_heads, G, (((uint64_t)1 << 32) + G - 1) / G,
+                 max_blocks, (int32_t)std::min<int64_t>((int64_t)max_blocks * s.block_size, INT32_MAX - 127), s.num_kv_heads, G, (((uint64_t)1 << 32) + G - 1) / G,
                  sm_scale * 1.4426950408889634f, (uint16_t*)out, out_stride, lse, (float*)ws, nullptr, p.n_tiles, p.n_split,
                  status};
     if (p.n_split > 1)

@@ -118,12 +118,12 @@ class Case:
                     continue
                 # a logit is a sum of 128 fp32 products of exact factors, scaled (134 * 2^-24 of the sum of their sizes);
                 # the exponential adds 2^-23 of its value and 2^-24 of an argument of up to twice `reach`; a probability is
-                # rounded once to the 16-bit type (u; in fp16 2^-25 at least), summed over the tokens in fp32, and so is
+                # rounded once to the 16-bit type (u; in fp16 2^-25 of 2^7 at least), summed over the tokens in fp32, and so is
                 # the denominator; the result is rounded once more
                 n = len(m)
                 logit = reach * 134 * 2.0**-24 + 2.0**-23
                 rel = (2 * logit + u + (n + 16) * 2.0**-23)[:, None]
-                low = 2.0**-25 * v[:, m].abs().sum(1).repeat_interleave(self.hq // self.hkv, 0) if u < 2.0**-10 else 0
+                low = 2.0**-32 * v[:, m].abs().sum(1).repeat_interleave(self.hq // self.hkv, 0) if u < 2.0**-10 else 0
                 bound = (mass * rel + low) * (1 + u) + want.abs() * u + 2.0**-24
                 worst[0] = max(worst[0], ((got - want).abs() / bound).max().item())
                 worst[1] = max(worst[1], ((lse[row] - want_lse).abs()
@@ -295,6 +295,38 @@ def test_large_logits_and_constant_rows(bits):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("new", [3, 700])
+def test_many_small_probabilities(new):
+    """fp16: one token's probability is near 1 and its value 0; the result is the sum of the others', 2^-19.6 each."""
+    c = Case([3000], [new], 16, 1 if new == 3 else 4, 16, "f16", 16, 21, garbage=False)
+    k0 = torch.zeros((c.hkv, 1, D), dtype=torch.float64)
+    k0[..., 0] = 16
+    first = int(c.table[0, 0])
+    c.k[:], c.v[:] = 0, c.v.abs() + 0.5
+    c.k[first, :, 0], c.v[first, :, 0] = k0[:, 0], 0
+    c.pool, c.k, c.v = pack(torch.stack([c.k, c.v]).to(c.dtype), 16, c.bs)
+    c.q.zero_()
+    c.q.view(c.T, c.hq, D)[..., 0] = 19.6424 / (16 * SCALE * 1.4426950408889634)
+    c.d.update(q=c.q.to(DEV), pool=c.pool.to(DEV))
+    c.check(*c.run())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,bits", [(5, 16), (5, 8), (70, 4), (300, 16)])
+def test_rows_before_the_first_request_stay(T, bits):
+    """The first request's rows need not begin at 0: what is before them is left as it was, whatever the splits."""
+    c = Case([2000, 900], [T, T // 2], 8, 2, 16, "bf16", bits, 22)
+    want, want_lse = c.run()
+    lead = 3
+    q = torch.cat([torch.zeros((lead, c.stride), device=DEV, dtype=c.dtype), c.d["q"]])
+    for fill in (0, 255):
+        out, lse = c.run(q=q, off=c.d["off"] + lead, T=c.T + lead, fill=fill)
+        assert (out[:lead] == 3).all() and (lse[:lead] == 3).all()
+        u = torch.finfo(c.dtype).eps / 2  # (the plan may be another: each form rounds as in `check`)
+        assert ((out[lead:] - want).double().abs() <= 8 * u * want.double().abs() + 8 * u).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("bits", [16, 8, 4])
 @pytest.mark.parametrize("T", [96, 5])
 def test_captured_calls_replay_as_eager(T, bits):
@@ -375,7 +407,9 @@ def test_prompt_refusals():
     assert call(P.make_shape(32, 8, 64, 16, P.PULSE_BF16)) == P.PULSE_ERR_UNSUPPORTED
     assert call(P.make_shape(32, 8, D, 16, 7)) == P.PULSE_ERR_UNSUPPORTED
     assert call(P.make_shape(64, 64, D, 16, P.PULSE_BF16), q_stride=8192, out_stride=8192,
-                max_tokens=1 << 25) == P.PULSE_ERR_UNSUPPORTED
+                max_tokens=1 << 24) == P.PULSE_ERR_UNSUPPORTED
+    assert call(P.make_shape(2048, 2048, D, 16, P.PULSE_BF16), q_stride=1 << 18,
+                out_stride=1 << 18) == P.PULSE_ERR_UNSUPPORTED
     assert call(B=0, q=None) == P.PULSE_OK and call(max_tokens=0, q=None) == P.PULSE_OK
     assert P.pulse_prompt_workspace_bytes(sh, 2, 1 << 26, 8) == 0 and P.pulse_prompt_workspace_bytes(sh, -1, 5, 8) == 0
     assert P.pulse_prompt_workspace_bytes(sh, 2, 100, 8) > 0
