@@ -16,6 +16,7 @@
 // rounded to the 16-bit type for the second product (half a step of it at most, beside half a step of the output's own
 // rounding to the same type); their sum is that of the values before rounding.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "kv4.h"
@@ -965,22 +966,30 @@ struct PromptPlan {
 
 constexpr int kSplitGroups = 512;  // workgroups aimed at where few rows are split over the context: two a CU
 constexpr int kLeastTiles = 4;     // tiles of keys of a split
+constexpr int kCus = 256;
 // prompt_few_kernel takes 32 rows to a workgroup, so every 32 rows read the keys again.  It is for
 // - few rows of long contexts: up to 32 of a request on average, 64 over a cache of codes (beyond, that reading costs the
 //   16-bit cache more than the decoding of codes that 128 rows share saves the others), and
-// - few workgroups: up to 256, which leave CUs to share out the keys of a workgroup of 128, or 512 unless prompts are so
-//   short that a workgroup is mostly its start; over a cache of codes, whose decoding is then shared out too, 512 and 1152.
-// In us, 128 rows and 32, 16-bit and 8-bit cache, query heads / KV heads:
-//   1 x 256    32/8    9.7   8.3    11.4   7.7      1 x 512    32/8   18.7  14.8    21.3  11.8
-//   1 x 1024   32/8   29.3  31.8    32.3  26.3      1 x 1000   16/2   24.7  21.6    25.5  16.0
+// - few workgroups and tables of no more than 1280 tokens, 5120 over a cache of codes: up to 256, which leave CUs to share
+//   out the keys of a workgroup of 128, or 512 unless prompts are so short that a workgroup is mostly its start; over a
+//   cache of codes, whose decoding is then shared out too, 512 and 1152, and up to 128 also tables of 16K tokens.
+// In us, 128 rows and 32, 16-bit and 8-bit cache, new tokens (of a context), query heads / KV heads:
+//   1 x 256    32/8    9.6   8.2    11.3   7.5      1 x 512    32/8   18.7  14.7    21.0  11.6
+//   1 x 1024   32/8   25.8  31.8    32.5  26.2      1 x 1024   16/2   24.7  21.5    25.1  15.4
 //   1 x 3000   12/1   63.1  72.5    81.9  53.2      8 x 100    32/8    8.7  13.6     9.7  13.1
+//   1 x 512 of 2048   33.4  42.0    34.8  28.2      1 x 512 of 4096   49.4  79.3    52.8  50.6
+//   1 x 512 of 16K     149   294     162   187      1 x 256 of 16K      83   158      90   102
+//   1 x 64 of 16K      37    52      39    35      1 x 64 of 8000      28    33      30    24
 //   16 x 5 of 32K     366   369     246   193       16 x 16 of 32K    378   565     303   273
 //   1 x 200    64/8    9.6  10.4 (16 bits, blocks of 32)
-static bool few_rows(const pulse_shape& s, int32_t B, int64_t max_tokens) {
+static bool few_rows(const pulse_shape& s, int32_t B, int64_t max_tokens, int32_t max_blocks) {
     const int64_t rows = max_tokens * (s.num_q_heads / s.num_kv_heads), groups = (rows + 31) / 32 * s.num_kv_heads;
     const bool codes = in_codes(s.dtype);
-    const int64_t few = codes ? 512 : 256, some = codes ? 1152 : 512;
-    return rows <= (codes ? 64 : 32) * (int64_t)B || groups <= few || (groups <= some && max_tokens >= 256 * (int64_t)B);
+    if (rows <= (codes ? 64 : 32) * (int64_t)B) return true;
+    const int64_t tokens = (int64_t)max_blocks * s.block_size;
+    if (codes && groups <= 128 && tokens <= 16384) return true;
+    if (tokens > (codes ? 5120 : 1280)) return false;
+    return groups <= (codes ? 512 : 256) || (groups <= (codes ? 1152 : 512) && max_tokens >= 256 * (int64_t)B);
 }
 // Workgroups of eight waves, which stage and decode a tile for twice the rows, from two rounds of them and 2048 new tokens
 // of a request on: below, the rows behind the diagonal that the larger tile multiplies in vain cost more.  In us, four
@@ -995,17 +1004,31 @@ static int64_t key_tiles(const pulse_shape& s, int32_t max_blocks) {
     return ((int64_t)max_blocks * s.block_size + kKeys - 1) / kKeys;
 }
 
+// Splits that pay: n of them leave 1/n of the longest workgroup's time `us` (1.2 a tile of keys for 128 rows of it; for 32
+// 0.5, 0.3 over a cache of codes) and cost a launch (3) and partials that are written and read, 1 KiB a row and split at 7
+// TB/s.  A little more than a workgroup for each CU takes twice one's time.  In us, splits and times: 1024 tokens of 32
+// heads over 8 2 29.4, 1 25.2; 256 at the end of 2048 8 26.8, 5 26.4, 4 23.1, in 8 bits (32 rows) 2 25.2, 1 17.5; 1500 of
+// 12 heads over 1 1 33.7, 2 30.1, 3 27.6; 2 requests of 8 at the end of 1000, 16 heads over 2, 1 14.6, 4 10.7.
+static int64_t splits_worth(double us, int64_t rows, int64_t units, int64_t most) {
+    const double each = (double)rows * 1024 / 7e6;
+    int64_t n = (int64_t)std::min((double)most, std::sqrt(us / each));
+    if (n * units > kCus && 2 * n * units < 3 * kCus && 2 * units <= kCus) n = kCus / units;
+    return n < 2 || us - us / n < 3 + n * each ? 1 : n;
+}
+
 static PromptPlan prompt_plan(const pulse_shape& s, int32_t B, int64_t max_tokens, int32_t max_blocks) {
     PromptPlan p;
     const int64_t G = s.num_q_heads / s.num_kv_heads;
     const int64_t all = max_tokens * G;
     p.rows = kWaves * kRowsPerWave;
-    if (few_rows(s, B, max_tokens)) p.rows = 32;
+    if (few_rows(s, B, max_tokens, max_blocks)) p.rows = 32;
     else if (max_tokens >= (int64_t)kLongPrompt * B && all * s.num_kv_heads >= (int64_t)kLongGroups * 2 * p.rows) p.rows *= 2;
     const int64_t rows = p.rows;
     p.n_tiles = (int)(all / rows + B);
     const int64_t units = std::max<int64_t>((all + rows - 1) / rows, B) * s.num_kv_heads;
-    p.n_split = (int)std::max<int64_t>(1, std::min(kSplitGroups / units, key_tiles(s, max_blocks) / kLeastTiles));
+    const int64_t tiles = key_tiles(s, max_blocks);
+    p.n_split = (int)splits_worth((double)tiles * (rows > 32 ? 1.2 : in_codes(s.dtype) ? 0.3 : 0.5), max_tokens * s.num_q_heads, units,
+                                  std::min(kSplitGroups / units, tiles / kLeastTiles));
     return p;
 }
 
