@@ -8,6 +8,9 @@
 // Bound: tables, lists and counts are read once or twice from L2, a few microseconds of dependent round trips and
 // launches; copies run at the rate of HBM.  Nothing is written before everything is checked, which takes a pass (and,
 // beyond one workgroup, a launch) of its own.  No result depends on the order of atomics: counts, maxima and bits.
+// In the kernels, blocks of 64 KiB: 48 forks (as many blocks copied, 6 MB) 5.0 us of checks and 6.4, a free of 33K entries 3.7 +
+// 3.0 + 3.4 + 4.7 (one workgroup: 103), of 635 entries 4.0; a compaction of 6K entries plans in 6.5 and moves 131 MB read
+// and 131 written in 48.4 (5.4 TB/s).
 #include <algorithm>
 
 #include "pulse_internal.h"

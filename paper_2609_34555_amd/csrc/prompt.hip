@@ -10,7 +10,8 @@
 // are its operand of the second product: probabilities never leave its registers, and as the accumulators of O^T have
 // the same column, maxima, sums and rescaling are a lane's own but for one exchange between the wave's halves.  Keys lie
 // token by token and values channel by channel in the 16-bit cache, which is what either operand takes, so no tile is
-// transposed.
+// transposed.  The same sums for 32 rows, whose keys a workgroup's waves share out, are prompt_few_kernel; either may be
+// split over the context, and prompt_join_kernel adds up the splits.
 //
 // Precision: products of 16-bit factors, exact, summed in fp32; maxima, sums and rescaling in fp32.  Probabilities are
 // rounded to the 16-bit type for the second product (half a step of it at most, beside half a step of the output's own
@@ -289,6 +290,15 @@ __device__ inline void tile_arrived() {
     __syncthreads();
 }
 
+// Bound: the matrix units, 4 * 128 operations a row and key, and beside them the vector units (an exponential, a
+// maximum, a sum, half a conversion a row and key).  8 prompts of 501 to 16000 tokens, 32 heads over 8 (5.75 TFLOP): 5.25 to
+// 5.5 ms, 1.05 PFLOP/s, of 1.31 to 1.39 that a large product reaches; 4096 tokens at the end of 32K in 4 bits 1.9 ms, the
+// same rate.  Counted there: matrix units busy 52% of the cycles and vector units 40 to 47%, at a clock that the load holds
+// at 1.9 GHz, no LDS conflict, 96% of the reads from L2.  So a step issues a group of four products beside each part of the
+// exponentials and each read of operands (8.0 to 5.9 ms with the next tile's logits among them), the maximum is followed
+// late (`prepare`; 6.1 to 5.6 with it and no array indexed at run time), and two workgroups of four waves share a CU.  64
+// rows a wave, which would halve the LDS reads, do not fit the registers; priorities between waves and a fixed order of
+// instructions cost 2 to 4%.
 // grid = Hkv * n_tiles * n_split workgroups: neighbours take the KV heads of one tile (a head's tiles then mostly run on
 // one XCD, whose L2 holds its keys), splits next, and the last tiles, which attend to the most keys, begin first.
 template <int DT, int BS, int W>
@@ -616,6 +626,10 @@ __global__ __launch_bounds__(W * kWave, 2) void prompt_kernel(PromptArgs a) {
 // the waves' results are joined in LDS.  A lane's operands are whole 16-byte loads in every form of the cache if product c
 // takes channels 64 * half + 8 c .. + 7 of a key, and row m of tile t of the values is channel
 // 64 * (m / 16) + 16 * t + m % 16.
+//
+// Bound: HBM, the context's bytes once for every 32 rows.  16 requests of 5 tokens at the end of 32K, 8 bits, 32 heads over
+// 8 (866 MB): 165 us and 4.9 of the join, 5.2 TB/s of 5.8 that streaming reads reach; with tiles in LDS for 128 rows, most
+// of them empty, 233.
 template <int DT, int BS>
 struct FewLoads {
     static constexpr int ET = elem_type(DT);
