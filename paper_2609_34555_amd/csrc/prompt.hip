@@ -17,7 +17,6 @@
 // rounded to the 16-bit type for the second product (half a step of it at most, beside half a step of the output's own
 // rounding to the same type); their sum is that of the values before rounding.
 #include <algorithm>
-#include <cmath>
 #include <type_traits>
 
 #include "kv4.h"
@@ -96,7 +95,9 @@ struct PromptArgs {
     float* lse;
     float* ws_o;            // [n_split][max_tokens * Hq][128]
     float2* ws_ml;
+    int32_t* ws_n;          // [max_tokens * Hq] splits of a row, 1 where its result is written already
     int32_t n_tiles, n_split;
+    float tile_us, split_us;  // (splits_worth)
     int32_t* status;
 };
 
@@ -149,6 +150,18 @@ __device__ inline Request look_at(const PromptArgs& a, const Place& pl, int rows
     q.ok = q.ctx >= fresh && q.ctx <= a.max_ctx;
     q.base = q.ctx - fresh;
     return q;
+}
+
+// Splits that pay for a context: n of them leave 1/n of a workgroup's time, `tile_us` a tile of keys (1.2 for 128 rows; for
+// 32 0.5, 0.3 over a cache of codes), and cost partials that are written and read, `split_us` a split (1 KiB a row of the
+// call, 7 TB/s) and a launch.  Looked at for the whole table when a launch is planned, and for what a workgroup attends to
+// by itself: short contexts in a wide table, and the first tiles of a prompt, are not split (256 tokens in a table of 32K,
+// 16 bits: 19.0 us and 12.7, of 8.0 in a table that fits; where all contexts are long it costs the join half a microsecond).
+constexpr int kLeastTiles = 4;  // tiles of keys of a split
+__host__ __device__ inline int splits_worth(int tiles, float tile_us, float split_us, int most) {
+    const float us = (float)tiles * tile_us;
+    const int n = min(min((int)sqrtf(us / split_us), most), tiles / kLeastTiles);
+    return n < 2 || us - us / (float)n < 3.f + (float)n * split_us ? 1 : n;
 }
 
 // The 16 KiB of a tile's keys, or of its values, into LDS from 16-bit blocks: 1 KiB a wave and instruction, straight from
@@ -334,7 +347,9 @@ __global__ __launch_bounds__(W * kWave, 2) void prompt_kernel(PromptArgs a) {
     const int wave_keys = wave_row < n_rows && ok ? base + token_of(wave_row + kRowsPerWave - 1) + 1 : 0;
     const int wave_all = base + token_of(wave_row) + 1;
     const int n_kt = (wg_keys + kKeys - 1) / kKeys;
-    const int kt0 = (int)((int64_t)n_kt * split / a.n_split), kt1 = (int)((int64_t)n_kt * (split + 1) / a.n_split);
+    const int n_split = a.n_split > 1 ? splits_worth(n_kt, a.tile_us, a.split_us, a.n_split) : 1;
+    if (split >= n_split) return;
+    const int kt0 = (int)((int64_t)n_kt * split / n_split), kt1 = (int)((int64_t)n_kt * (split + 1) / n_split);
 
     vec qb[8];
     {
@@ -586,7 +601,8 @@ __global__ __launch_bounds__(W * kWave, 2) void prompt_kernel(PromptArgs a) {
         l_run = __uint_as_float(w[0]) + __uint_as_float(w[1]);
     }
     const int64_t at = (int64_t)(t0 + tok) * Hq + h * a.G + g;
-    if (a.n_split > 1) {
+    if (a.n_split > 1 && live && half == 0 && split == 0) a.ws_n[at] = n_split;
+    if (n_split > 1) {
         if (!live) return;
         const int64_t part = (int64_t)split * a.max_tokens * Hq + at;
         if (half == 0) a.ws_ml[part] = make_float2(m_run, l_run);
@@ -736,8 +752,10 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void prompt_few_kernel(PromptArg
     const int64_t last_row = min(q.row0 + kRows - 1, q.n_rows - 1);
     const int keys = q.ok ? q.base + (int)((uint64_t)last_row * a.g_magic >> 32) + 1 : 0;
     const int all = q.base + (int)((uint64_t)q.row0 * a.g_magic >> 32) + 1;  // keys that every row attends to
+    const int n_split = a.n_split > 1 ? splits_worth((keys + kKeys - 1) / kKeys, a.tile_us, a.split_us, a.n_split) : 1;
+    if (split >= n_split) return;
     // this wave's steps: a share of the split's, which is a share of the context
-    const int n_steps = (keys + kStep - 1) / kStep, shares = a.n_split * W, share = split * W + wave;
+    const int n_steps = (keys + kStep - 1) / kStep, shares = n_split * W, share = split * W + wave;
     const int i0 = (int)((int64_t)n_steps * share / shares), i1 = (int)((int64_t)n_steps * (share + 1) / shares);
 
     const auto* row = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(a.table + (size_t)pl.r * a.max_blocks);
@@ -882,7 +900,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void prompt_few_kernel(PromptArg
         }
         const int tr = (int)((uint64_t)mr * a.g_magic >> 32), head = h * a.G + (int)mr - tr * a.G;
         const int64_t out_row = q.t0 + tr, slot_row = out_row * Hq + head;
-        if (a.n_split > 1) {
+        if (a.n_split > 1 && split == 0 && c4 == 0) a.ws_n[slot_row] = n_split;
+        if (n_split > 1) {
             const int64_t part = (int64_t)split * a.max_tokens * Hq + slot_row;
             if (c4 == 0) a.ws_ml[part] = make_float2(top, l);
             *reinterpret_cast<f32x4*>(a.ws_o + part * kHeadDim + 4 * c4) = o;
@@ -911,22 +930,24 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
     const int64_t at = STRIDE == 1 ? (int64_t)blockIdx.x * 8 + part : (int64_t)blockIdx.x;
     const int first = a.tok_off[0], last = a.tok_off[a.B];
     const bool any = at >= (int64_t)first * Hq && at < (int64_t)last * Hq && last <= a.max_tokens;
-    if (STRIDE > 1 && !any) return;
+    // (rows of offsets that are wrong have any number here)
+    const int n_split = any ? min(max(a.ws_n[at], 1), a.n_split) : 1;
+    if (STRIDE > 1 && n_split == 1) return;
     float top = -INFINITY, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = STRIDE == 1 ? 0 : part; any && s0 < a.n_split; s0 += 4 * STRIDE) {
+    for (int s0 = STRIDE == 1 ? 0 : part; n_split > 1 && s0 < n_split; s0 += 4 * STRIDE) {
         float2 ml[4];
         f32x4 x[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int s = min(s0 + i * STRIDE, a.n_split - 1);
+            const int s = min(s0 + i * STRIDE, n_split - 1);
             ml[i] = a.ws_ml[s * rows + at];
             x[i] = *reinterpret_cast<const f32x4*>(a.ws_o + (s * rows + at) * kHeadDim + 4 * c4);
         }
         float m = top;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (s0 + i * STRIDE < a.n_split) m = __builtin_elementwise_maximum(m, ml[i].x);
+            if (s0 + i * STRIDE < n_split) m = __builtin_elementwise_maximum(m, ml[i].x);
         if (m == -INFINITY) continue;
         const float f = __builtin_amdgcn_exp2f(top - m);
         top = m;
@@ -934,7 +955,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
         o *= f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (s0 + i * STRIDE >= a.n_split || ml[i].x == -INFINITY) continue;  // (such a split's sums are not written)
+            if (s0 + i * STRIDE >= n_split || ml[i].x == -INFINITY) continue;  // (such a split's sums are not written)
             const float w = __builtin_amdgcn_exp2f(ml[i].x - m);
             l += ml[i].y * w;
             o += x[i] * w;
@@ -957,7 +978,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a) {
         }
         top = m;
     }
-    if (!any) return;
+    if (n_split == 1) return;
     if (top != -INFINITY) o *= 1.f / l;
     uint16_t* dst = a.out + at / Hq * a.out_stride + at % Hq * kHeadDim + 4 * c4;
     *reinterpret_cast<u32x2*>(dst) = u32x2{pack2<ET>(o[0], o[1]), pack2<ET>(o[2], o[3])};
@@ -976,10 +997,10 @@ static void launch_join(const PromptArgs& a, hipStream_t st) {
 struct PromptPlan {
     int rows;  // of a workgroup: 32 (prompt_few_kernel), 128 or 256
     int n_tiles, n_split;
+    float tile_us, split_us;
 };
 
 constexpr int kSplitGroups = 512;  // workgroups aimed at where few rows are split over the context: two a CU
-constexpr int kLeastTiles = 4;     // tiles of keys of a split
 constexpr int kCus = 256;
 // prompt_few_kernel takes 32 rows to a workgroup, so every 32 rows read the keys again.  It is for
 // - few rows of long contexts: up to 32 of a request on average, 64 over a cache of codes (beyond, that reading costs the
@@ -1018,18 +1039,6 @@ static int64_t key_tiles(const pulse_shape& s, int32_t max_blocks) {
     return ((int64_t)max_blocks * s.block_size + kKeys - 1) / kKeys;
 }
 
-// Splits that pay: n of them leave 1/n of the longest workgroup's time `us` (1.2 a tile of keys for 128 rows of it; for 32
-// 0.5, 0.3 over a cache of codes) and cost a launch (3) and partials that are written and read, 1 KiB a row and split at 7
-// TB/s.  A little more than a workgroup for each CU takes twice one's time.  In us, splits and times: 1024 tokens of 32
-// heads over 8 2 29.4, 1 25.2; 256 at the end of 2048 8 26.8, 5 26.4, 4 23.1, in 8 bits (32 rows) 2 25.2, 1 17.5; 1500 of
-// 12 heads over 1 1 33.7, 2 30.1, 3 27.6; 2 requests of 8 at the end of 1000, 16 heads over 2, 1 14.6, 4 10.7.
-static int64_t splits_worth(double us, int64_t rows, int64_t units, int64_t most) {
-    const double each = (double)rows * 1024 / 7e6;
-    int64_t n = (int64_t)std::min((double)most, std::sqrt(us / each));
-    if (n * units > kCus && 2 * n * units < 3 * kCus && 2 * units <= kCus) n = kCus / units;
-    return n < 2 || us - us / n < 3 + n * each ? 1 : n;
-}
-
 static PromptPlan prompt_plan(const pulse_shape& s, int32_t B, int64_t max_tokens, int32_t max_blocks) {
     PromptPlan p;
     const int64_t G = s.num_q_heads / s.num_kv_heads;
@@ -1041,20 +1050,27 @@ static PromptPlan prompt_plan(const pulse_shape& s, int32_t B, int64_t max_token
     p.n_tiles = (int)(all / rows + B);
     const int64_t units = std::max<int64_t>((all + rows - 1) / rows, B) * s.num_kv_heads;
     const int64_t tiles = key_tiles(s, max_blocks);
-    p.n_split = (int)splits_worth((double)tiles * (rows > 32 ? 1.2 : in_codes(s.dtype) ? 0.3 : 0.5), max_tokens * s.num_q_heads, units,
-                                  std::min(kSplitGroups / units, tiles / kLeastTiles));
+    const int64_t most = kSplitGroups / units;
+    p.tile_us = rows > 32 ? 1.2f : in_codes(s.dtype) ? 0.3f : 0.5f;
+    p.split_us = (float)((double)max_tokens * s.num_q_heads * 1024 / 7e6);
+    p.n_split = splits_worth((int)std::min<int64_t>(tiles, 1 << 25), p.tile_us, p.split_us, (int)most);
+    // A little more than a workgroup for each CU takes twice one's time.  In us, splits and times: 1024 tokens of 32 heads
+    // over 8 2 29.4, 1 25.2; 256 at the end of 2048 8 26.8, 5 26.4, 4 23.1, in 8 bits (32 rows) 2 25.2, 1 17.5; 1500 of 12
+    // heads over 1 1 33.7, 2 30.1, 3 27.6; 2 requests of 8 at the end of 1000, 16 heads over 2, 1 14.6, 4 10.7.
+    const int64_t groups = p.n_split * units;
+    if (groups > kCus && 2 * groups < 3 * kCus && 2 * units <= kCus) p.n_split = (int)(kCus / units);
     return p;
 }
 
 static size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Partials of the splits of this call and every smaller one: fewer rows may have more splits, but no more than kSplitGroups
+// Partials of the splits, and a row's number of them, of this call and every smaller one: fewer rows may have more splits, but no more than kSplitGroups
 // workgroups' rows, nor than the context has splits (calls of 256 rows a workgroup have no splits).
 size_t prompt_ws_bytes(const pulse_shape& s, int32_t B, int64_t max_tokens, int32_t max_blocks) {
     const int64_t most = key_tiles(s, max_blocks) / kLeastTiles;
     if (most <= 1) return 256;
     const size_t rows = (size_t)std::min<int64_t>((int64_t)kSplitGroups * kWaves * kRowsPerWave, most * max_tokens * s.num_q_heads);
-    return up256(rows * kHeadDim * sizeof(float)) + up256(rows * sizeof(float2));
+    return up256(rows * kHeadDim * sizeof(float)) + up256(rows * sizeof(float2)) + up256(rows * sizeof(int32_t));
 }
 
 template <int DT, int BS>
@@ -1081,10 +1097,13 @@ hipError_t launch_prompt_attn(const pulse_shape& s, const void* q, int64_t q_str
     const int32_t G = s.num_q_heads / s.num_kv_heads;
     PromptArgs a{(const uint16_t*)q, q_stride, tok_off, ctx_len, B, (int32_t)max_tokens, (const uint8_t*)pool, n_slots, table,
                  max_blocks, (int32_t)std::min<int64_t>((int64_t)max_blocks * s.block_size, INT32_MAX - 127), s.num_kv_heads, G, (((uint64_t)1 << 32) + G - 1) / G,
-                 sm_scale * 1.4426950408889634f, (uint16_t*)out, out_stride, lse, (float*)ws, nullptr, p.n_tiles, p.n_split,
-                 status};
-    if (p.n_split > 1)
-        a.ws_ml = ws_at<float2>(ws, up256((size_t)p.n_split * max_tokens * s.num_q_heads * kHeadDim * sizeof(float)));
+                 sm_scale * 1.4426950408889634f, (uint16_t*)out, out_stride, lse, (float*)ws, nullptr, nullptr, p.n_tiles,
+                 p.n_split, p.tile_us, p.split_us, status};
+    if (p.n_split > 1) {
+        const size_t parts = (size_t)p.n_split * max_tokens * s.num_q_heads, at = up256(parts * kHeadDim * sizeof(float));
+        a.ws_ml = ws_at<float2>(ws, at);
+        a.ws_n = ws_at<int32_t>(ws, at + up256(parts * sizeof(float2)));
+    }
     switch (s.dtype) {
         case PULSE_BF16: launch_prompt_bs<PULSE_BF16>(s.block_size, a, p.rows, st); break;
         case PULSE_F16: launch_prompt_bs<PULSE_F16>(s.block_size, a, p.rows, st); break;

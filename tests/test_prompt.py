@@ -366,6 +366,19 @@ def test_captured_calls_replay_as_eager(T, bits):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("new", [[7, 1, 5, 2], [400, 90, 300, 1]])
+def test_contexts_of_all_lengths_in_a_wide_table(new, bits):
+    """Rows that are split over their context beside rows that are not, and whatever was in the workspace before."""
+    c = Case([new[0] + 7000, new[1], new[2] + 1500, new[3] + 20], new, 16, 2, 16, "bf16", bits, 23, pad=2, mb=2000)
+    out, lse = c.run()
+    c.check(out, lse)
+    again, again_lse = c.run(fill=0)
+    n = sum(new)
+    assert torch.equal(out, again) and torch.equal(lse, again_lse) and (out[n:] == 3).all() and (lse[n:] == 3).all()
+
+
+@pytest.mark.gpu
 def test_two_calls_at_once():
     """Calls on two streams with workspaces of their own give what they give alone."""
     cases = [Case([5000, 3000], [7, 2], 16, 4, 64, "bf16", 8, 13), Case([300, 900], [300, 900], 8, 2, 16, "f16", 16, 14)]
