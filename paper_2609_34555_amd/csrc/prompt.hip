@@ -309,8 +309,8 @@ __device__ inline void tile_arrived() {
 // same rate.  Counted there: matrix units busy 51% of the cycles, vector instructions 45%, LDS reads about half, at a clock
 // that the load holds at 2.0 GHz; no LDS conflict, 92% of the reads from L2.  So a step issues a group of four products
 // beside each part of the exponentials and each read of operands, the next tile's logits among them, the maximum is followed
-// late (`prepare`), and no array is indexed at run time: 6.1 to 5.6 ms together.  64 rows a wave, which would halve the LDS
-// reads, do not fit the registers; priorities between waves and a fixed order of instructions cost 2 to 4%; two waves of a
+// late (`prepare`), and no array is indexed at run time: 6.1 to 5.6 ms together.  64 rows a wave, which halve the LDS reads,
+// leave one wave a SIMD and accumulators that have to be moved: 23% slower; priorities between waves and a fixed order of instructions cost 2 to 4%; two waves of a
 // SIMD that take turns at products and exponentials, a barrier a turn and three buffers, 18%: half the waves then read LDS
 // at twice the rate, which is all that it has.
 // grid = Hkv * n_tiles * n_split workgroups: neighbours take the KV heads of one tile (a head's tiles then mostly run on
