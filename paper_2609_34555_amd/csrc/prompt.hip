@@ -306,13 +306,14 @@ __device__ inline void tile_arrived() {
 // Bound: the matrix units, 4 * 128 operations a row and key, and beside them the vector units (an exponential, a
 // maximum, a sum, half a conversion a row and key).  8 prompts of 501 to 16000 tokens, 32 heads over 8 (5.75 TFLOP): 5.25 to
 // 5.5 ms, 1.05 PFLOP/s, of 1.31 to 1.39 that a large product reaches; 4096 tokens at the end of 32K in 4 bits 1.9 ms, the
-// same rate.  Counted there: matrix units busy 51% of the cycles, vector instructions 45%, LDS reads about half, at a clock
-// that the load holds at 2.0 GHz; no LDS conflict, 92% of the reads from L2.  So a step issues a group of four products
-// beside each part of the exponentials and each read of operands, the next tile's logits among them, the maximum is followed
-// late (`prepare`), and no array is indexed at run time: 6.1 to 5.6 ms together.  64 rows a wave, which halve the LDS reads,
-// leave one wave a SIMD and accumulators that have to be moved: 23% slower; priorities between waves and a fixed order of instructions cost 2 to 4%; two waves of a
-// SIMD that take turns at products and exponentials, a barrier a turn and three buffers, 18%: half the waves then read LDS
-// at twice the rate, which is all that it has.
+// same rate.  Counted there: matrix units busy 51% of the cycles, 23% with vector instructions beside them; vector
+// instructions 45%; LDS reads 26%; waves waiting for memory, LDS or a barrier 34%; no LDS conflict, 92% of the reads from L2;
+// a clock that the load holds at 2.0 GHz.  So a step issues a group of four products beside each part of the exponentials
+// and each read of operands, the next tile's logits among them, the maximum is followed late (`prepare`), and no array is
+// indexed at run time: 6.1 to 5.6 ms together.  What did not help, with three buffers of tiles: two waves of a SIMD half a
+// tile apart (the same time), or taking turns with a barrier a turn (18% slower); the first operands read before the next
+// loads are issued (2% slower); 64 rows a wave, which halve the LDS reads but leave a SIMD one wave and accumulators that
+// have to be moved (23%); priorities between waves, a fixed order of instructions (2 to 4%).
 // grid = Hkv * n_tiles * n_split workgroups: neighbours take the KV heads of one tile (a head's tiles then mostly run on
 // one XCD, whose L2 holds its keys), splits next, and the last tiles, which attend to the most keys, begin first.
 template <int DT, int BS, int W>
