@@ -166,6 +166,10 @@ CASES = [
     ([900, 30, 2000, 1], [200, 2, 3, 1], 8, 1, 16, "bf16"),
     ([260, 300, 280], None, 32, 8, 16, "bf16"),
     ([2000, 40, 1999], [64, 64 - 24, 64], 24, 8, 64, "f16"),
+    # 128 rows a workgroup, split over the context
+    ([6001], [300], 32, 8, 16, "bf16"),
+    ([6001], [300], 32, 8, 32, "f16"),
+    ([6001, 5300], [170, 150], 16, 4, 64, "bf16"),
 ]
 
 
