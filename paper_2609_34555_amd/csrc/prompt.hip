@@ -15,7 +15,7 @@
 //
 // Precision: products of 16-bit factors, exact, summed in fp32; maxima, sums and rescaling in fp32.  Probabilities are
 // rounded to the 16-bit type for the second product (half a step of it at most, beside half a step of the output's own
-// rounding to the same type); their sum is that of the values before rounding.
+// rounding to the same type; in prompt_few_kernel mostly in two parts); their sum is that of the values before rounding.
 #include <algorithm>
 #include <type_traits>
 
@@ -728,11 +728,15 @@ struct FewLoads {
     }
 };
 
+// Beside that reading a second product a value costs nothing, so a probability keeps 16 (bf16) or 22 bits, in two parts of the
+// 16-bit type (in us, one part and two: 16 requests of 5 at the end of 32K 367.6 and 367.9, in 8 bits 192.2 and 192.8; a
+// prompt of 512 14.7 and 15.4); not over a 4-bit cache (132.5 and 156.6), whose own values are off by far more.
 // grid as prompt_kernel's, with 32 rows a workgroup.
 template <int DT, int BS>
 __global__ __launch_bounds__(kWaves * kWave, 2) void prompt_few_kernel(PromptArgs a) {
     constexpr int ET = elem_type(DT);
     constexpr int W = kWaves, kRows = 32, kStep = 32;
+    constexpr bool kTwoParts = kv_bits(DT) != 4;
     constexpr int kPer = FewLoads<DT, BS>::kPer;
     using vec = typename Mfma<ET>::vec;
     __shared__ __align__(16) float s_o[W][kRows][kHeadDim];
@@ -846,8 +850,14 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void prompt_few_kernel(PromptArg
                 y[n] = __builtin_amdgcn_exp2f(fmaf(s[8 * st + n], scale, -m_use));
                 sum += y[n];
             }
-            const vec pv = __builtin_bit_cast(vec, u32x4{pack2<ET>(y[0], y[1]), pack2<ET>(y[2], y[3]),
-                                                         pack2<ET>(y[4], y[5]), pack2<ET>(y[6], y[7])});
+            u32x4 p1, p2;  // the probabilities, and what rounding took off them
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                p1[n] = pack2<ET>(y[2 * n], y[2 * n + 1]);
+                if constexpr (kTwoParts)
+                    p2[n] = pack2<ET>(y[2 * n] - elem_to_float<ET>((uint16_t)(p1[n] & 0xFFFF)),
+                                      y[2 * n + 1] - elem_to_float<ET>((uint16_t)(p1[n] >> 16)));
+            }
             u32x4 v[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) v[t] = now.value(st, t);
@@ -861,7 +871,10 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void prompt_few_kernel(PromptArg
                 }
             }
 #pragma unroll
-            for (int t = 0; t < 4; ++t) acc[t] = mac32<ET>(__builtin_bit_cast(vec, v[t]), pv, acc[t]);
+            for (int t = 0; t < 4; ++t) {
+                acc[t] = mac32<ET>(__builtin_bit_cast(vec, v[t]), __builtin_bit_cast(vec, p1), acc[t]);
+                if constexpr (kTwoParts) acc[t] = mac32<ET>(__builtin_bit_cast(vec, v[t]), __builtin_bit_cast(vec, p2), acc[t]);
+            }
         }
         l_run += sum;
     }

@@ -97,8 +97,8 @@ class Case:
         b = self.table[r, : -(-self.ctx[r] // self.bs)].long()
         return (x[b].transpose(0, 1).reshape(self.hkv, -1, D)[:, : self.ctx[r]] for x in (self.k, self.v))
 
-    def check(self, out, lse, scale=SCALE, requests=None, skip=None):
-        """`skip`: (request, mask of its tokens that count nothing)."""
+    def check(self, out, lse, scale=SCALE, requests=None, skip=None, parts=1):
+        """`skip`: (request, mask of its tokens that count nothing).  `parts`: of the 16-bit type that hold a probability."""
         u = torch.finfo(self.dtype).eps / 2
         out, lse = out.double().cpu(), lse.double().cpu()
         worst = [0.0, 0.0]
@@ -122,7 +122,7 @@ class Case:
                 # the denominator; the result is rounded once more
                 n = len(m)
                 logit = reach * 134 * 2.0**-24 + 2.0**-23
-                rel = (2 * logit + u + (n + 16) * 2.0**-23)[:, None]
+                rel = (2 * logit + u**parts + (n + 16) * 2.0**-23)[:, None]  # (each part rounds what the last left)
                 low = 2.0**-32 * v[:, m].abs().sum(1).repeat_interleave(self.hq // self.hkv, 0) if u < 2.0**-10 else 0
                 bound = (mass * rel + low) * (1 + u) + want.abs() * u + 2.0**-24
                 worst[0] = max(worst[0], ((got - want).abs() / bound).max().item())
@@ -313,6 +313,18 @@ def test_many_small_probabilities(new):
     c.q.view(c.T, c.hq, D)[..., 0] = 19.6424 / (16 * SCALE * 1.4426950408889634)
     c.d.update(q=c.q.to(DEV), pool=c.pool.to(DEV))
     c.check(*c.run())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("bits", [16, 8])
+def test_few_rows_keep_probabilities_in_two_parts(bits, dt):
+    c = Case([3000, 900, 6], [5, 3, 6], 16, 4, 16, dt, bits, 24)
+    # values of one sign, so that the bound is little more than the result's own rounding
+    c.v.abs_()
+    c.pool, c.k, c.v = pack(torch.stack([c.k, c.v]).to(c.dtype), bits, c.bs)
+    c.d.update(pool=c.pool.to(DEV))
+    c.check(*c.run(), parts=2)
 
 
 @pytest.mark.gpu
