@@ -728,15 +728,15 @@ struct FewLoads {
     }
 };
 
-// Beside that reading a second product a value costs nothing, so a probability keeps 16 (bf16) or 22 bits, in two parts of the
-// 16-bit type (in us, one part and two: 16 requests of 5 at the end of 32K 367.6 and 367.9, in 8 bits 192.2 and 192.8; a
-// prompt of 512 14.7 and 15.4); not over a 4-bit cache (132.5 and 156.6), whose own values are off by far more.
+// Beside that reading a second product a value costs nothing, so a probability keeps 16 (bf16) or 22 bits, in two PARTS of
+// the 16-bit type, where a request has few rows (in us, one part and two: 16 requests of 5 at the end of 32K 367.6 and
+// 367.9, in 8 bits 192.2 and 192.8); not over a 4-bit cache (132.5 and 156.6), whose own values are off by far more, nor in
+// short prompts, which are not bound by the reading (512 tokens, 8 bits: 11.9 and 12.6; 512 at the end of 4096 50.6, 59.7).
 // grid as prompt_kernel's, with 32 rows a workgroup.
-template <int DT, int BS>
+template <int DT, int BS, int PARTS>
 __global__ __launch_bounds__(kWaves * kWave, 2) void prompt_few_kernel(PromptArgs a) {
     constexpr int ET = elem_type(DT);
     constexpr int W = kWaves, kRows = 32, kStep = 32;
-    constexpr bool kTwoParts = kv_bits(DT) != 4;
     constexpr int kPer = FewLoads<DT, BS>::kPer;
     using vec = typename Mfma<ET>::vec;
     __shared__ __align__(16) float s_o[W][kRows][kHeadDim];
@@ -854,7 +854,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void prompt_few_kernel(PromptArg
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
                 p1[n] = pack2<ET>(y[2 * n], y[2 * n + 1]);
-                if constexpr (kTwoParts)
+                if constexpr (PARTS == 2)
                     p2[n] = pack2<ET>(y[2 * n] - elem_to_float<ET>((uint16_t)(p1[n] & 0xFFFF)),
                                       y[2 * n + 1] - elem_to_float<ET>((uint16_t)(p1[n] >> 16)));
             }
@@ -873,7 +873,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void prompt_few_kernel(PromptArg
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 acc[t] = mac32<ET>(__builtin_bit_cast(vec, v[t]), __builtin_bit_cast(vec, p1), acc[t]);
-                if constexpr (kTwoParts) acc[t] = mac32<ET>(__builtin_bit_cast(vec, v[t]), __builtin_bit_cast(vec, p2), acc[t]);
+                if constexpr (PARTS == 2) acc[t] = mac32<ET>(__builtin_bit_cast(vec, v[t]), __builtin_bit_cast(vec, p2), acc[t]);
             }
         }
         l_run += sum;
@@ -1011,7 +1011,7 @@ static void launch_join(const PromptArgs& a, hipStream_t st) {
 
 struct PromptPlan {
     int rows;  // of a workgroup: 32 (prompt_few_kernel), 128 or 256
-    int n_tiles, n_split;
+    int n_tiles, n_split, parts;
     float tile_us, split_us;
 };
 
@@ -1024,18 +1024,21 @@ constexpr int kCus = 256;
 //   out the keys of a workgroup of 128, or 512 unless prompts are so short that a workgroup is mostly its start; over a
 //   cache of codes, whose decoding is then shared out too, 512 and 1152, and up to 128 also tables of 16K tokens.
 // In us, 128 rows and 32, 16-bit and 8-bit cache, new tokens (of a context), query heads / KV heads:
-//   1 x 256    32/8    9.6   8.2    11.3   7.5      1 x 512    32/8   18.7  14.7    21.0  11.6
-//   1 x 1024   32/8   25.8  31.8    32.5  26.2      1 x 1024   16/2   24.7  21.5    25.1  15.4
+//   1 x 256    32/8    9.8   8.3    11.5   7.6      1 x 512    32/8   14.7  14.8    18.3  11.8
+//   1 x 1024   32/8   24.7  31.8    31.5  26.2      1 x 1024   16/2   24.6  21.5    29.6  15.4
 //   1 x 3000   12/1   63.1  72.5    81.9  53.2      8 x 100    32/8    8.7  13.6     9.7  13.1
-//   1 x 512 of 2048   33.4  42.0    34.8  28.2      1 x 512 of 4096   49.4  79.3    52.8  50.6
+//   1 x 512 of 2048   33.4  42.0    39.0  28.2      1 x 512 of 4096   49.4  79.3    52.8  50.6
 //   1 x 512 of 16K     149   294     162   187      1 x 256 of 16K      83   158      90   102
 //   1 x 64 of 16K      37    52      39    35      1 x 64 of 8000      28    33      30    24
 //   16 x 5 of 32K     366   369     246   193       16 x 16 of 32K    378   565     303   273
 //   1 x 200    64/8    9.6  10.4 (16 bits, blocks of 32)
+static bool few_each(const pulse_shape& s, int32_t B, int64_t max_tokens) {
+    return max_tokens * (s.num_q_heads / s.num_kv_heads) <= (in_codes(s.dtype) ? 64 : 32) * (int64_t)B;
+}
 static bool few_rows(const pulse_shape& s, int32_t B, int64_t max_tokens, int32_t max_blocks) {
     const int64_t rows = max_tokens * (s.num_q_heads / s.num_kv_heads), groups = (rows + 31) / 32 * s.num_kv_heads;
     const bool codes = in_codes(s.dtype);
-    if (rows <= (codes ? 64 : 32) * (int64_t)B) return true;
+    if (few_each(s, B, max_tokens)) return true;
     const int64_t tokens = (int64_t)max_blocks * s.block_size;
     if (codes && groups <= 128 && tokens <= 16384) return true;
     if (tokens > (codes ? 5120 : 1280)) return false;
@@ -1059,6 +1062,7 @@ static PromptPlan prompt_plan(const pulse_shape& s, int32_t B, int64_t max_token
     const int64_t G = s.num_q_heads / s.num_kv_heads;
     const int64_t all = max_tokens * G;
     p.rows = kWaves * kRowsPerWave;
+    p.parts = few_each(s, B, max_tokens) && !is_kv4(s.dtype) ? 2 : 1;
     if (few_rows(s, B, max_tokens, max_blocks)) p.rows = 32;
     else if (max_tokens >= (int64_t)kLongPrompt * B && all * s.num_kv_heads >= (int64_t)kLongGroups * 2 * p.rows) p.rows *= 2;
     const int64_t rows = p.rows;
@@ -1089,18 +1093,21 @@ size_t prompt_ws_bytes(const pulse_shape& s, int32_t B, int64_t max_tokens, int3
 }
 
 template <int DT, int BS>
-static void launch_prompt_t(const PromptArgs& a, int rows, hipStream_t st) {
+static void launch_prompt_t(const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
     const dim3 grid((unsigned)((int64_t)a.Hkv * a.n_tiles * a.n_split));
-    if (rows == 32) hipLaunchKernelGGL((prompt_few_kernel<DT, BS>), grid, dim3(kWaves * kWave), 0, st, a);
-    else if (rows == kWaves * kRowsPerWave) hipLaunchKernelGGL((prompt_kernel<DT, BS, kWaves>), grid, dim3(kWaves * kWave), 0, st, a);
-    else hipLaunchKernelGGL((prompt_kernel<DT, BS, 2 * kWaves>), grid, dim3(2 * kWaves * kWave), 0, st, a);
+    const dim3 threads(kWaves * kWave), twice(2 * kWaves * kWave);
+    constexpr int kParts = is_kv4(DT) ? 1 : 2;
+    if (p.rows == 32 && p.parts == 2) hipLaunchKernelGGL((prompt_few_kernel<DT, BS, kParts>), grid, threads, 0, st, a);
+    else if (p.rows == 32) hipLaunchKernelGGL((prompt_few_kernel<DT, BS, 1>), grid, threads, 0, st, a);
+    else if (p.rows == kWaves * kRowsPerWave) hipLaunchKernelGGL((prompt_kernel<DT, BS, kWaves>), grid, threads, 0, st, a);
+    else hipLaunchKernelGGL((prompt_kernel<DT, BS, 2 * kWaves>), grid, twice, 0, st, a);
 }
 
 template <int DT>
-static void launch_prompt_bs(int32_t bs, const PromptArgs& a, int rows, hipStream_t st) {
-    if (bs == 16) launch_prompt_t<DT, 16>(a, rows, st);
-    else if (bs == 32) launch_prompt_t<DT, 32>(a, rows, st);
-    else launch_prompt_t<DT, 64>(a, rows, st);
+static void launch_prompt_bs(int32_t bs, const PromptArgs& a, const PromptPlan& p, hipStream_t st) {
+    if (bs == 16) launch_prompt_t<DT, 16>(a, p, st);
+    else if (bs == 32) launch_prompt_t<DT, 32>(a, p, st);
+    else launch_prompt_t<DT, 64>(a, p, st);
 }
 
 hipError_t launch_prompt_attn(const pulse_shape& s, const void* q, int64_t q_stride, const int32_t* tok_off,
@@ -1120,12 +1127,12 @@ hipError_t launch_prompt_attn(const pulse_shape& s, const void* q, int64_t q_str
         a.ws_n = ws_at<int32_t>(ws, at + up256(parts * sizeof(float2)));
     }
     switch (s.dtype) {
-        case PULSE_BF16: launch_prompt_bs<PULSE_BF16>(s.block_size, a, p.rows, st); break;
-        case PULSE_F16: launch_prompt_bs<PULSE_F16>(s.block_size, a, p.rows, st); break;
-        case PULSE_BF16_KV8: launch_prompt_bs<PULSE_BF16_KV8>(s.block_size, a, p.rows, st); break;
-        case PULSE_F16_KV8: launch_prompt_bs<PULSE_F16_KV8>(s.block_size, a, p.rows, st); break;
-        case PULSE_BF16_KV4: launch_prompt_bs<PULSE_BF16_KV4>(s.block_size, a, p.rows, st); break;
-        case PULSE_F16_KV4: launch_prompt_bs<PULSE_F16_KV4>(s.block_size, a, p.rows, st); break;
+        case PULSE_BF16: launch_prompt_bs<PULSE_BF16>(s.block_size, a, p, st); break;
+        case PULSE_F16: launch_prompt_bs<PULSE_F16>(s.block_size, a, p, st); break;
+        case PULSE_BF16_KV8: launch_prompt_bs<PULSE_BF16_KV8>(s.block_size, a, p, st); break;
+        case PULSE_F16_KV8: launch_prompt_bs<PULSE_F16_KV8>(s.block_size, a, p, st); break;
+        case PULSE_BF16_KV4: launch_prompt_bs<PULSE_BF16_KV4>(s.block_size, a, p, st); break;
+        case PULSE_F16_KV4: launch_prompt_bs<PULSE_F16_KV4>(s.block_size, a, p, st); break;
         default: return hipErrorInvalidValue;
     }
     hipError_t e = hipGetLastError();
