@@ -696,9 +696,9 @@ PULSE_API pulse_status pulse_prompt_attn(const pulse_shape* shape, const void* q
  *   that no entry names any more go back to the free list: with k of them
  *   *free_head becomes h = *free_head - k, and free_slots[h .. h + k) are they, in the
  *   (request, block) order of their last entries.  An error if k exceeds
- *   *free_head, if a slot is freed more often than it is named, or if a kept
- *   length ends inside a block that is shared (the next token would be written
- *   into it).
+ *   *free_head, if a slot is freed more often than it is named, if a kept entry
+ *   still names a slot that would go back, or if a kept length ends inside a block
+ *   that is shared (the next token would be written into it).
  *   shared   may be NULL for a pool without forks
  * pulse_compact_blocks: live blocks in slots from n_keep on move to free slots
  *   below it, so that the pool may be cut to n_keep slots: the k-th of them in

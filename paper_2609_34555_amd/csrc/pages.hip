@@ -131,6 +131,15 @@ __device__ inline bool free_returns(const FreeArgs& a, int e, int s, bool& wrong
     wrong |= held < 0 || n > held + 1;
     return n == held + 1;
 }
+// Whether an entry that stays names a slot that goes back, which would be in the list and in the table.  Of a slot that is
+// not freed `last` and `cnt` are any numbers: it is freed if the entry that `last` names is one of its own that is.
+__device__ inline bool free_wrongs(const FreeArgs& a, int j, int s, int keep) {
+    if (j * (int64_t)a.bs >= keep || s < 0 || s >= a.n_slots) return false;
+    const int e = fresh_load(a.last + s);
+    if (e < 0 || e >= a.B * a.mb || a.table[e] != s) return false;
+    const int r = e / a.mb;
+    return (e - r * a.mb) * (int64_t)a.bs >= a.keep[r] && fresh_load(a.cnt + s) > (a.shared ? a.shared[s] : 0);
+}
 __device__ inline void free_apply(const FreeArgs& a, int e, int s, bool returns, int at) {
     if (a.shared && fresh_load(a.last + s) == e) a.shared[s] = max(a.shared[s] - fresh_load(a.cnt + s), 0);
     if (returns) a.free_slots[at] = s;
@@ -170,6 +179,7 @@ __global__ __launch_bounds__(kPlanThreads) void free_small_kernel(FreeArgs a) {
     for (int i = 0; i < N; ++i) {
         bool returns = false;
         if (s[i] >= 0) returns = free_returns(a, x.e[i], s[i], wrong);
+        else if (x.in[i]) wrong |= free_wrongs(a, x.j[i], x.slot[i], x.keep[i]);
         ret[i] = __ballot(returns);
         mine += __popcll(ret[i]);
     }
@@ -219,6 +229,7 @@ __global__ __launch_bounds__(kPageThreads) void free_kernel(FreeArgs a) {
     for (int i = 0; i < kEach; ++i) {
         bool returns = false;
         if (s[i] >= 0) returns = free_returns(a, x.e[i], s[i], wrong);
+        else if (PASS == 2 && x.in[i]) wrong |= free_wrongs(a, x.j[i], x.slot[i], x.keep[i]);
         ret[i] = __ballot(returns);
         mine += __popcll(ret[i]);
     }
