@@ -675,13 +675,14 @@ PULSE_API pulse_status pulse_prompt_attn(const pulse_shape* shape, const void* q
  * smaller.  The table and the free list are those of pulse_recall_gather and
  * pulse_build_tables.  `shared` (device int32 [n_slots], zero at the start)
  * counts of every slot the table entries that name it beyond the first, so a slot
- * that is taken from the free list has 0 and only these calls change it.  Every
- * length, entry, count and slot is checked before anything is written: on an
- * error (PULSE_ERR_BAD_INDEX unless said otherwise) nothing changes.  Not to be
- * called between a recall and its release, which undoes the last allocation.  ws:
- * pulse_pages_workspace_bytes() bytes of device memory, which serve any of the
- * three with the same or smaller B, max_blocks and n_slots.  B <= 4096,
- * B * max_blocks and n_slots <= 2^30 (else PULSE_ERR_UNSUPPORTED).  Any dtype.
+ * that is taken from the free list has 0 and only these calls change it.  The
+ * lengths, entries, counts and slots that a call uses are checked before anything is
+ * written, as said at each: on an error (PULSE_ERR_BAD_INDEX unless said otherwise)
+ * nothing changes.  Not to be called between a recall and its release, which undoes
+ * the last allocation.  ws: pulse_pages_workspace_bytes() bytes of device memory,
+ * which serve any of the three with the same or smaller B, max_blocks and n_slots.
+ * B <= 4096, B * max_blocks and n_slots <= 2^30 (else PULSE_ERR_UNSUPPORTED).  Any
+ * dtype.
  *
  * pulse_fork_blocks: for i < n <= B request dst[i] gets the first fork_len[i]
  *   tokens of request src[i].  Its row of the table has to be empty (all -1); it
@@ -690,7 +691,9 @@ PULSE_API pulse_status pulse_prompt_attn(const pulse_shape* shape, const void* q
  *   that block, which has to be resident, is copied to the next slot of the free
  *   list (in the order of i), so that either request may append to its own.
  *   src, dst, fork_len   device int32 [n]; no request twice in dst, none in both
- *   PULSE_ERR_POOL_EXHAUSTED if the free list has too few slots.
+ *   PULSE_ERR_POOL_EXHAUSTED if the free list has too few slots; an error if one of
+ *   those that are taken is there twice, has a count, or is named by any entry of
+ *   the table (the others of the list are not looked at).
  * pulse_free_blocks: request r keeps the blocks of its first keep_len[r] tokens
  *   (0: none; INT32_MAX: all).  The entries behind them become -1, and slots
  *   that no entry names any more go back to the free list: with k of them
@@ -698,7 +701,8 @@ PULSE_API pulse_status pulse_prompt_attn(const pulse_shape* shape, const void* q
  *   (request, block) order of their last entries.  An error if k exceeds
  *   *free_head, if a slot is freed more often than it is named, if a kept entry
  *   still names a slot that would go back, or if a kept length ends inside a block
- *   that is shared (the next token would be written into it).
+ *   that is shared (the next token would be written into it).  Slots of the free
+ *   list and kept entries out of range are not looked at.
  *   shared   may be NULL for a pool without forks
  * pulse_compact_blocks: live blocks in slots from n_keep on move to free slots
  *   below it, so that the pool may be cut to n_keep slots: the k-th of them in

@@ -284,13 +284,65 @@ struct ForkArgs {
     int32_t n_slots;
     int64_t U;
     int32_t* status;
-    int32_t* err;    // [n]
+    int32_t* err;       // [n]
+    int32_t* scan_err;  // [scans]
+    int32_t scans;
     int32_t* head0;
 };
 
-// A workgroup looks whether its fork can be made.
+constexpr int kScan = 1024;       // table entries that a workgroup looks at in a turn
+constexpr int kScanGroups = 512;
+constexpr int kSlotSet = 2 * kMaxBatch;
+
+// Whether a slot that the forks take is taken twice, is counted, or is one of the entries that this workgroup looks at.  The
+// slots are a set in LDS that is at most half full, searched from a place that depends on the slot until an empty one.
+__device__ inline bool taken_wrong(const ForkArgs& a, int scan, int* s_set, int* s_wave) {
+    int parts = 0;
+    for (int k = threadIdx.x; k < a.n; k += kPageThreads) parts += a.len[k] % a.bs != 0;
+    const int total = block_sum(parts, s_wave, kPageThreads / kWave);
+    const int head = *a.free_head;
+    if (total == 0 || head < 0 || head > a.n_free || total > a.n_free - head) return false;  // (for fork_kernel to report)
+    int size = kPageThreads;
+    while (size < 2 * total) size *= 2;
+    for (int k = threadIdx.x; k < size; k += kPageThreads) s_set[k] = -1;
+    __syncthreads();
+    auto place = [&](int s) { return (int)((uint32_t)s * 2654435761u >> 16) & (size - 1); };
+    bool wrong = false;
+    for (int k = threadIdx.x; k < total; k += kPageThreads) {
+        const int s = a.free_slots[head + k];
+        if (s < 0 || s >= a.n_slots) continue;
+        if (scan == 0) wrong |= a.shared[s] != 0;
+        int was = -1;
+        for (int at = place(s); (was = atomicCAS(s_set + at, -1, s)) != -1 && was != s;) at = (at + 1) & (size - 1);
+        wrong |= was == s;
+    }
+    __syncthreads();
+    const int n = a.B * a.mb;
+    for (int64_t e0 = (int64_t)scan * kScan + threadIdx.x; e0 < n; e0 += (int64_t)a.scans * kScan) {
+        int v[kScan / kPageThreads];
+#pragma unroll
+        for (int i = 0; i < kScan / kPageThreads; ++i) v[i] = a.table[min(e0 + i * kPageThreads, (int64_t)n - 1)];
+#pragma unroll
+        for (int i = 0; i < kScan / kPageThreads; ++i) {
+            if (v[i] < 0) continue;
+            int at = place(v[i]);
+            while (s_set[at] != -1 && s_set[at] != v[i]) at = (at + 1) & (size - 1);
+            wrong |= s_set[at] == v[i];
+        }
+    }
+    return wrong;
+}
+
+// A workgroup looks whether its fork can be made; those behind the forks' at the slots that they take.
 __global__ __launch_bounds__(kPageThreads) void fork_check_kernel(ForkArgs a) {
+    __shared__ int s_set[kSlotSet];
+    __shared__ int s_wave[kPageThreads / kWave];
     const int i = blockIdx.x;
+    if (i >= a.n) {
+        const int bad = __syncthreads_or(taken_wrong(a, i - a.n, s_set, s_wave));
+        if (threadIdx.x == 0) a.scan_err[i - a.n] = bad;
+        return;
+    }
     const int src = a.src[i], dst = a.dst[i], len = a.len[i];
     bool wrong = src < 0 || src >= a.B || dst < 0 || dst >= a.B || len < 0 ||
                  ((int64_t)len + a.bs - 1) / a.bs > a.mb;
@@ -326,6 +378,7 @@ __global__ __launch_bounds__(kPageThreads) void fork_kernel(ForkArgs a) {
         if (k < i) before += part;
         errs |= a.err[k];
     }
+    for (int k = threadIdx.x; k < a.scans; k += kPageThreads) errs |= a.scan_err[k];
     before = block_sum(before, s_wave, kPageThreads / kWave);
     total = block_sum(total, s_wave, kPageThreads / kWave);
     const int head = *a.head0;
@@ -651,9 +704,10 @@ hipError_t launch_fork_blocks(const int32_t* src, const int32_t* dst, const int3
                               int32_t* free_head, int32_t n_free, void* pool, int32_t n_slots, size_t unit_bytes,
                               int32_t* status, void* ws, hipStream_t st) {
     const PagesWs w(ws, B, max_blocks, n_slots);
+    const int32_t scans = (int32_t)std::min<int64_t>(kScanGroups, ((int64_t)B * max_blocks + kScan - 1) / kScan);
     const ForkArgs a{src, dst, len, n, bs, table, B, max_blocks, shared, free_slots, free_head, n_free, (uint8_t*)pool,
-                     n_slots, (int64_t)unit_bytes, status, w.requests, w.few};
-    hipLaunchKernelGGL(fork_check_kernel, dim3((unsigned)n), dim3(kPageThreads), 0, st, a);
+                     n_slots, (int64_t)unit_bytes, status, w.requests, w.tiles[0], scans, w.few};
+    hipLaunchKernelGGL(fork_check_kernel, dim3((unsigned)(n + scans)), dim3(kPageThreads), 0, st, a);
     const dim3 grid((unsigned)((unit_bytes + kChunk - 1) / kChunk), (unsigned)n);
     hipLaunchKernelGGL(fork_kernel, grid, dim3(kPageThreads), 0, st, a);
     return hipGetLastError();

@@ -20,6 +20,16 @@ class Strict(Pages):
             raise Wrong
         super().do_free(keep, with_shared)
 
+    def do_fork(self, src, dst, ln):
+        """The slots that are taken: none twice, none that an entry names, none with a count."""
+        need = sum(x % self.bs != 0 for x in ln)
+        if 0 <= self.head <= len(self.free) - need:
+            new = self.free[self.head:self.head + need]
+            inside = new[(new >= 0) & (new < self.n_slots)]
+            if len(set(new.tolist())) < need or np.isin(inside, self.table).any() or self.shared[inside].any():
+                raise Wrong
+        super().do_fork(src, dst, ln)
+
 
 def state(mb, **kw):
     p = small(mb=mb, **kw)
@@ -101,3 +111,67 @@ def test_lives_with_a_wrong_entry_now_and_then(B, mb, n_slots):
             both.p = p = copy.deepcopy(start)
             both.push()
     assert refused > 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("mb", WIDTHS)
+def test_slots_that_a_fork_takes(mb):
+    """A slot twice in the list would be two forks' block; one that an entry names would be written over."""
+    say(f"\n[gpu] forks over wrong lists, {mb} blocks a request")
+    ok = ([0, 1, 0], [3, 4, 5], [100, 63, 7])
+    assert state(mb).call("fork", *ok) == 0
+    for i, j in ((0, 1), (0, 2), (1, 2)):
+        b = state(mb)
+        b.p.free[b.p.head + i] = b.p.free[b.p.head + j]
+        b.push()
+        assert b.call("fork", *ok) == P.PULSE_ERR_BAD_INDEX
+        assert b.call("fork", [0, 1, 0], [3, 4, 5], [96, 64, 16]) == 0  # whole blocks alone: no slot is taken
+    for i in range(3):
+        for r, j in ((0, 0), (0, 6), (2, 1)):
+            b = state(mb)
+            b.p.free[b.p.head + i] = b.p.table[r, j]
+            b.push()
+            assert b.call("fork", *ok) == P.PULSE_ERR_BAD_INDEX
+        for count in (1, -1):
+            b = state(mb)
+            b.p.shared[b.p.free[b.p.head + i]] = count
+            b.push()
+            assert b.call("fork", *ok) == P.PULSE_ERR_BAD_INDEX
+    b = state(mb)  # a request that is no part of the call, at the end of its row
+    b.p.table[2, mb - 1] = b.p.free[b.p.head + 2]
+    b.push()
+    assert b.call("fork", *ok) == P.PULSE_ERR_BAD_INDEX
+    b = state(mb)  # what lies behind the taken slots is not looked at
+    b.p.free[b.p.head + 3:b.p.head + 6] = [b.p.free[b.p.head], b.p.table[0, 0], -7]
+    b.push()
+    assert b.call("fork", *ok) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [255, 256, 257, 2048, 4095])
+def test_many_forks_over_wrong_lists(n):
+    """As many forks as a table has rows, of one request, each with a slot of its own; one of them wrong, anywhere."""
+    say(f"\n[gpu] {n} forks")
+
+    def fresh():
+        p = Strict(n + 1, 2, n + 40, 16, n)
+        p.take(0, 20)
+        return Both(p)
+
+    call = ([0] * n, list(range(1, n + 1)), [5 + i % 11 + 16 * (i % 5 == 0) for i in range(n)])
+    b = fresh()
+    assert b.call("fork", *call) == 0
+    need = b.p.head - 2
+    assert need > n - 100
+    assert b.call("free", [KEEP_ALL] + [0] * n) == 0 and b.p.head == 2
+    rng = np.random.default_rng(n)
+    for _ in range(4):
+        i, j = rng.choice(need, 2, replace=False) + 2
+        b = fresh()
+        b.p.free[i] = b.p.free[j]
+        b.push()
+        assert b.call("fork", *call) == P.PULSE_ERR_BAD_INDEX
+        b = fresh()
+        b.p.free[i] = b.p.table[0, 1]
+        b.push()
+        assert b.call("fork", *call) == P.PULSE_ERR_BAD_INDEX
