@@ -638,10 +638,13 @@ PULSE_API pulse_status pulse_load_kv(const pulse_shape* shape, const void* slot_
  *   lse[row][hq] = log sum_t exp(logit_t)           (fp32, optional)
  * so the new tokens' own keys and values are in the cache before the call
  * (pulse_append_kv).  The cache may be in 16, 8 or 4 bits.  Products and sums in
- * fp32; probabilities are rounded to the 16-bit type before they meet V (over a 16-
- * or 8-bit cache a few rows' are kept in two parts of it).  Keys of tokens behind p
- * count nothing whatever they are, values as long as they are finite; what lies
- * behind the context's end may be anything.
+ * fp32; probabilities are rounded to the 16-bit type before they meet V, which moves
+ * a result by up to half a step of the type of sum_t p_t |V(h, t)| beside its own
+ * rounding; in a call of few rows a request, max_tokens * G <= 32 * B over a 16-bit
+ * cache and 64 * B over an 8-bit one, each is kept in two parts of the type (half a
+ * step of half a step).  Keys of tokens behind p count nothing whatever they are,
+ * values as long as they are finite; what lies behind the context's end may be
+ * anything.
  *   q            device rows of 16-bit elements, row i at i * q_stride elements,
  *                its heads one after another (out: the same at out_stride)
  *   tok_off      device int32 [B+1];  ctx_len  device int32 [B]
