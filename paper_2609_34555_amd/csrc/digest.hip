@@ -41,7 +41,9 @@ __device__ inline s16x2 order16(s16x2 x) { return x ^ ((x >> 15) & (int16_t)0x7F
 // turn: 24.2 us with both the look-up first and single values, 17.6 now (4.2 TB/s).  One batch
 // over and over, whose keys stay in the 256 MB Infinity Cache: 18.0 and 14.7.
 // DT: a 4-bit cache's keys are decoded as they are loaded (the same tokens, 26 MB, in blocks of 16: 11.5 us; of 64:
-// 10.1); 16-bit ones are taken as patterns, whatever their type.
+// 10.1); 16-bit ones are taken as patterns, whatever their type.  An 8-bit block's are 128 BS bytes in a row and one scale
+// byte elsewhere (42 MB in blocks of 16: 12.8 us, about 5 of them launch, look-ups and the one round trip of a wave; 32 x 32K,
+// beyond the Infinity Cache, 42 us, 4.0 TB/s; in blocks of 64, where a lane has 16 loads in flight for 4, 8.3 and 22.7, 6.3).
 template <int BS, int DT>
 __global__ __launch_bounds__(256) void build_digests_kernel(const uint16_t* __restrict__ kv,
                                                             const int64_t* __restrict__ blk_off,
