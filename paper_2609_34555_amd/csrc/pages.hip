@@ -6,10 +6,10 @@
 // shares them; the block that it ends inside is copied.
 //
 // Bound: tables, lists and counts are read once or twice from L2, a few microseconds of dependent round trips and
-// launches; copies run at the rate of HBM.  Nothing is written before everything is checked, which takes a pass (and,
+// launches; copies run at the rate of HBM.  Nothing is written before what a call uses is checked, which takes a pass (and,
 // beyond one workgroup, a launch) of its own.  No result depends on the order of atomics: counts, maxima and bits.
-// In the kernels, blocks of 64 KiB: 48 forks (as many blocks copied, 6 MB) 5.0 us of checks and 6.4, a free of 33K entries 3.7 +
-// 3.0 + 3.4 + 4.7 (one workgroup: 103), of 635 entries 4.0; a compaction of 6K entries plans in 6.5 and moves 131 MB read
+// In the kernels, blocks of 64 KiB: 48 forks (as many blocks copied, 6 MB) 4.9 us of checks and 6.5, a free of 33K entries 3.6 +
+// 2.9 + 3.9 + 4.4 (one workgroup: 103), of 635 entries 4.6; a compaction of 6K entries plans in 6.5 and moves 131 MB read
 // and 131 written in 48.4 (5.4 TB/s).
 #include <algorithm>
 
@@ -132,7 +132,9 @@ __device__ inline bool free_returns(const FreeArgs& a, int e, int s, bool& wrong
     return n == held + 1;
 }
 // Whether an entry that stays names a slot that goes back, which would be in the list and in the table.  Of a slot that is
-// not freed `last` and `cnt` are any numbers: it is freed if the entry that `last` names is one of its own that is.
+// not freed `last` and `cnt` are any numbers: it is freed if the entry that `last` names is one of its own that is.  A load
+// of 4 bytes an entry: frees of 4K, 33K and 262K entries 5.4, 12.6 and 12.6 us with and without it, of 2M 100 and 85; counted by
+// atomics instead 13.1, 12.9, 24.9 and 159.
 __device__ inline bool free_wrongs(const FreeArgs& a, int j, int s, int keep) {
     if (j * (int64_t)a.bs >= keep || s < 0 || s >= a.n_slots) return false;
     const int e = fresh_load(a.last + s);
@@ -295,7 +297,8 @@ constexpr int kScanGroups = 512;
 constexpr int kSlotSet = 2 * kMaxBatch;
 
 // Whether a slot that the forks take is taken twice, is counted, or is one of the entries that this workgroup looks at.  The
-// slots are a set in LDS that is at most half full, searched from a place that depends on the slot until an empty one.
+// slots are a set in LDS that is at most half full, searched from a place that depends on the slot until an empty one.  Beside
+// the forks' own checks: 48 forks in 33K entries 8.8 us with it and 8.3 without, 120 in 2M 21.5 and 18.3, 2000 of a call 81 and 70.
 __device__ inline bool taken_wrong(const ForkArgs& a, int scan, int* s_set, int* s_wave) {
     int parts = 0;
     for (int k = threadIdx.x; k < a.n; k += kPageThreads) parts += a.len[k] % a.bs != 0;
