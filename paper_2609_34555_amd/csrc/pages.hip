@@ -294,19 +294,23 @@ struct ForkArgs {
 
 constexpr int kScan = 1024;       // table entries that a workgroup looks at in a turn
 constexpr int kScanGroups = 512;
-constexpr int kSlotSet = 2 * kMaxBatch;
+// Places of the set below for up to n slots.
+__host__ __device__ inline int slot_places(int n) {
+    int size = kPageThreads;
+    while (size < 2 * n) size *= 2;
+    return size;
+}
 
 // Whether a slot that the forks take is taken twice, is counted, or is one of the entries that this workgroup looks at.  The
 // slots are a set in LDS that is at most half full, searched from a place that depends on the slot until an empty one.  Beside
-// the forks' own checks: 48 forks in 33K entries 8.8 us with it and 8.3 without, 120 in 2M 21.5 and 18.3, 2000 of a call 81 and 70.
+// the forks' own checks: 48 forks in 33K entries 9.6 us with it and 9.9 without, 120 in 2M 21.3 and 17.6, 2000 of a call 78 and 70.
 __device__ inline bool taken_wrong(const ForkArgs& a, int scan, int* s_set, int* s_wave) {
     int parts = 0;
     for (int k = threadIdx.x; k < a.n; k += kPageThreads) parts += a.len[k] % a.bs != 0;
     const int total = block_sum(parts, s_wave, kPageThreads / kWave);
     const int head = *a.free_head;
     if (total == 0 || head < 0 || head > a.n_free || total > a.n_free - head) return false;  // (for fork_kernel to report)
-    int size = kPageThreads;
-    while (size < 2 * total) size *= 2;
+    const int size = slot_places(total);
     for (int k = threadIdx.x; k < size; k += kPageThreads) s_set[k] = -1;
     __syncthreads();
     auto place = [&](int s) { return (int)((uint32_t)s * 2654435761u >> 16) & (size - 1); };
@@ -338,7 +342,7 @@ __device__ inline bool taken_wrong(const ForkArgs& a, int scan, int* s_set, int*
 
 // A workgroup looks whether its fork can be made; those behind the forks' at the slots that they take.
 __global__ __launch_bounds__(kPageThreads) void fork_check_kernel(ForkArgs a) {
-    __shared__ int s_set[kSlotSet];
+    extern __shared__ int s_set[];
     __shared__ int s_wave[kPageThreads / kWave];
     const int i = blockIdx.x;
     if (i >= a.n) {
@@ -710,7 +714,7 @@ hipError_t launch_fork_blocks(const int32_t* src, const int32_t* dst, const int3
     const int32_t scans = (int32_t)std::min<int64_t>(kScanGroups, ((int64_t)B * max_blocks + kScan - 1) / kScan);
     const ForkArgs a{src, dst, len, n, bs, table, B, max_blocks, shared, free_slots, free_head, n_free, (uint8_t*)pool,
                      n_slots, (int64_t)unit_bytes, status, w.requests, w.tiles[0], scans, w.few};
-    hipLaunchKernelGGL(fork_check_kernel, dim3((unsigned)(n + scans)), dim3(kPageThreads), 0, st, a);
+    hipLaunchKernelGGL(fork_check_kernel, dim3((unsigned)(n + scans)), dim3(kPageThreads), sizeof(int) * slot_places(n), st, a);
     const dim3 grid((unsigned)((unit_bytes + kChunk - 1) / kChunk), (unsigned)n);
     hipLaunchKernelGGL(fork_kernel, grid, dim3(kPageThreads), 0, st, a);
     return hipGetLastError();
